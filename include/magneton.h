@@ -714,6 +714,167 @@ int mag_stream_set_host_staging(mag_stream* handle, int64_t max_chunk, void* sta
 int mag_stream_push_host(mag_stream* handle, const double* t_host, const float* p_host,
                          int64_t n_chunk);
 
+/* ------------------------------------- operators of a feed-forward block */
+/*
+ * Efficient counterparts of operators that the paper finds wasteful: a product
+ * with a separate addition (Section 2.1, Case 1: torch.addmm against add and
+ * matmul), an activation in five kernels (Section 6.3), reductions in many
+ * passes.  A user who compares two systems runs these as the efficient side:
+ * their intervals go through mag_attribute, their outputs through
+ * mag_invariants and mag_match.  Forward and backward passes, and the
+ * orthogonalised update of a weight.
+ *
+ * Every call below is asynchronous: it is enqueued on `stream`, reads nothing
+ * back and allocates nothing, so it can be captured into a graph.  Arguments
+ * are checked on the host before any device work; values are not checked
+ * (infinities and NaN go through the arithmetic).  Sums are held in fp32 (norms
+ * of an update in fp64) and every output is rounded once.  Results do not
+ * depend on timing: no atomic sums.  Outputs may not overlap inputs except
+ * where a comment says so.
+ */
+#define MAG_F32 0
+#define MAG_F16 1
+#define MAG_BF16 2
+
+/* Activations: identity; max(z, 0) with slope 0 at 0; z Phi(z) with the normal
+   distribution's Phi; z s(2 sqrt(2/pi) (z + 0.044715 z^3)) and z s(z), with s
+   the logistic function. */
+#define MAG_ACT_NONE 0
+#define MAG_ACT_RELU 1
+#define MAG_ACT_GELU 2
+#define MAG_ACT_GELU_TANH 3
+#define MAG_ACT_SILU 4
+
+/* Largest extent of a matrix and largest reduction. */
+#define MAG_MAX_EXTENT (1LL << 30)
+
+/* A matrix on the device.  Element (i, j) is data[i * row_stride + j *
+   col_stride].  Inputs may have any strides >= 0 (0: one row or column read
+   again and again); outputs need col_stride 1 and rows that do not overlap.
+   data must be aligned to the element; rows that start at multiples of 16
+   bytes are read fastest.  Two of its fields may be anything where the matrix
+   has one row or one column: that one's stride. */
+typedef struct mag_matrix {
+    void* data;
+    int64_t rows, cols;
+    int64_t row_stride, col_stride; /* in elements */
+} mag_matrix;
+
+typedef struct mag_linear_args {
+    int32_t dtype;      /* MAG_F32 / MAG_F16 / MAG_BF16, of every array            */
+    int32_t activation; /* MAG_ACT_*                                               */
+    mag_matrix x;       /* [rows, in]                                              */
+    mag_matrix weight;  /* [out, in]                                               */
+    mag_matrix residual; /* [rows, out], data NULL: none; may be y itself (same    */
+                        /* data and strides)                                       */
+    mag_matrix pre;     /* output [rows, out], data NULL: none                     */
+    mag_matrix y;       /* output [rows, out]                                      */
+    const void* bias;   /* [out], contiguous, or NULL                              */
+} mag_linear_args;
+
+/*
+ * mag_linear -- z = x weight^T + bias, pre = z, y = act(z) + residual, in one
+ * pass over the product.  in = 0 gives z = bias; rows or out = 0: nothing is
+ * written.
+ *   mag_linear_workspace_size: bytes for args->x and args->weight (type, sizes,
+ *   strides and the 16-byte alignment of data count; the rest of args is not
+ *   read).
+ * fp32 operands are cut into three bfloat16 parts each, whose sum is the
+ * operand exactly, and the six largest of the nine products are summed in fp32
+ * (the rest is below 2^-24 of a product); a sum that is not finite is
+ * taken again from the operands themselves.
+ * Errors: MAG_E_NULL, MAG_E_SIZE (types, sizes, strides), MAG_E_ALIGN,
+ * MAG_E_WORKSPACE, MAG_E_HIP.
+ */
+int mag_linear_workspace_size(const mag_linear_args* args, size_t* bytes);
+int mag_linear(const mag_linear_args* args, void* workspace, size_t workspace_bytes,
+               hipStream_t stream);
+
+typedef struct mag_linear_backward_args {
+    int32_t dtype;
+    int32_t activation;
+    mag_matrix x;       /* [rows, in]                                              */
+    mag_matrix weight;  /* [out, in]; not read when dx.data is NULL                */
+    mag_matrix pre;     /* [rows, out], the forward pass's pre; not read with      */
+                        /* MAG_ACT_NONE                                            */
+    mag_matrix dy;      /* [rows, out]                                             */
+    mag_matrix dx;      /* output [rows, in], data NULL: not wanted                */
+    mag_matrix dweight; /* output [out, in], data NULL: not wanted                 */
+    void* dbias;        /* output [out], contiguous, or NULL                       */
+} mag_linear_backward_args;
+
+/*
+ * mag_linear_backward -- gradients of mag_linear: dz = dy act'(pre), dx = dz
+ * weight, dweight = dz^T x, dbias = the sum of dz over the rows (the residual's
+ * gradient is dy itself).  The products read dz rounded to the operands' type,
+ * as x and weight are held (fp32: the parts of mag_linear); dbias sums it
+ * unrounded.  rows = 0 gives dweight = 0 and dbias = 0.
+ *   workspace_size: of args' sizes, strides and alignments of x, weight and dy.
+ * Errors as mag_linear.
+ */
+int mag_linear_backward_workspace_size(const mag_linear_backward_args* args, size_t* bytes);
+int mag_linear_backward(const mag_linear_backward_args* args, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+typedef struct mag_norm_args {
+    int32_t dtype;        /* of x, y, dy, dx                                       */
+    int32_t weight_dtype; /* of weight, bias and their gradients: dtype or MAG_F32 */
+    mag_matrix x;         /* [rows, width], width >= 1                             */
+    mag_matrix y;         /* forward: output [rows, width]                         */
+    mag_matrix dy;        /* backward: [rows, width]                               */
+    mag_matrix dx;        /* backward: output [rows, width], data NULL: not wanted */
+    const void* weight;   /* [width] or NULL (ones)                                */
+    const void* bias;     /* forward: [width] or NULL (zeros)                      */
+    float* mean;          /* [rows]: written by the forward pass where not NULL,   */
+    float* rstd;          /* read by the backward pass                             */
+    void* dweight;        /* backward: output [width] or NULL                      */
+    void* dbias;          /* backward: output [width] or NULL                      */
+    double eps;           /* forward: > 0 or 0                                     */
+} mag_norm_args;
+
+/*
+ * mag_layer_norm -- per row: mean, rstd = 1 / sqrt(variance + eps) (the
+ * variance over all `width` values, from squares about the mean), y = (x -
+ * mean) rstd weight + bias.  y may be x itself (same data and strides).
+ * mag_layer_norm_backward -- with xh = (x - mean) rstd and h = dy weight: dx =
+ * rstd (h - mean(h) - xh mean(h xh)), dweight = the sum over the rows of dy xh,
+ * dbias = the sum of dy.  rows = 0 gives dweight = dbias = 0.  dx may be dy or
+ * x itself.  Only the backward pass has a workspace (sizes and types of args).
+ * Errors: MAG_E_NULL, MAG_E_SIZE, MAG_E_ALIGN, MAG_E_WORKSPACE, MAG_E_HIP.
+ */
+int mag_layer_norm(const mag_norm_args* args, hipStream_t stream);
+int mag_layer_norm_backward_workspace_size(const mag_norm_args* args, size_t* bytes);
+int mag_layer_norm_backward(const mag_norm_args* args, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream);
+
+typedef struct mag_orthogonalize_args {
+    int32_t dtype;     /* of g and out                                             */
+    int32_t steps;     /* 0 .. MAG_ORTH_MAX_STEPS                                  */
+    int64_t batch;     /* matrices of one shape, each on its own                   */
+    mag_matrix g;      /* [rows, cols], the first matrix                           */
+    mag_matrix out;    /* output [rows, cols]; may be g itself                     */
+    int64_t g_batch_stride, out_batch_stride; /* in elements                       */
+    double a, b, c;    /* the step's polynomial a s + b s^3 + c s^5                */
+    double eps;        /* >= 0, added to the norm                                  */
+} mag_orthogonalize_args;
+
+#define MAG_ORTH_MAX_STEPS 64
+
+/*
+ * mag_orthogonalize -- the update of a weight with its singular values driven
+ * towards one (Newton-Schulz iteration): X = g / (|g| + eps) with the Frobenius
+ * norm, then `steps` times X <- a X + (b A + c A A) X with A = X X^T, on the
+ * transpose where g is taller than wide.  mag_invariants of the result shows
+ * its singular values.  Operands of the products are held as the sum of two
+ * half-precision numbers (22 bits) under a power of two that follows from the
+ * polynomial's bound, sums in fp32.  steps = 0 gives g / (|g| + eps).
+ * Errors: MAG_E_NULL, MAG_E_SIZE (also a polynomial whose bound on X passes
+ * 2^60), MAG_E_ALIGN, MAG_E_WORKSPACE, MAG_E_HIP.
+ */
+int mag_orthogonalize_workspace_size(const mag_orthogonalize_args* args, size_t* bytes);
+int mag_orthogonalize(const mag_orthogonalize_args* args, void* workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+
 /* Static description of a status code. */
 const char* mag_strerror(int status);
 /* Detail of the last error on the calling thread ("" if none). */

@@ -18,7 +18,9 @@ from . import _native as N
 __all__ = ["MagnetonError", "KeyPlan", "attribute", "attribute_static", "attribute_counter", "diff", "diff_batch", "detect", "invariants",
            "match", "match_subgraphs", "Stream", "workspace_size",
            "stream_workspace_size", "diff_workspace_size", "counter_workspace_size", "version", "EQUAL_SPLIT",
-           "SKIP_VALIDATE"]
+           "SKIP_VALIDATE", "linear", "linear_workspace_size", "linear_backward",
+           "linear_backward_workspace_size", "layer_norm", "layer_norm_backward",
+           "layer_norm_backward_workspace_size", "orthogonalize", "orthogonalize_workspace_size"]
 
 EQUAL_SPLIT = N.MAG_EQUAL_SPLIT
 SKIP_VALIDATE = N.MAG_SKIP_VALIDATE
@@ -781,3 +783,9 @@ class Stream:
             self.abort()
         except Exception:
             pass
+
+
+# (at the end: the module takes the error class and helpers above)
+from ._block import (layer_norm, layer_norm_backward, layer_norm_backward_workspace_size,  # noqa: E402
+                     linear, linear_backward, linear_backward_workspace_size,
+                     linear_workspace_size, orthogonalize, orthogonalize_workspace_size)

@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 # MAG_LIBRARY_SO: another build of the library to load (the host-sanitizer run
@@ -37,6 +38,16 @@ MAG_WASTE = 1
 MAG_TRADEOFF = 2
 MAG_MAX_STREAMS = 32
 MAG_STATIC_SCRATCH_BYTES = 64 << 20
+MAG_F32 = 0
+MAG_F16 = 1
+MAG_BF16 = 2
+MAG_ACT_NONE = 0
+MAG_ACT_RELU = 1
+MAG_ACT_GELU = 2
+MAG_ACT_GELU_TANH = 3
+MAG_ACT_SILU = 4
+MAG_MAX_EXTENT = 1 << 30
+MAG_ORTH_MAX_STEPS = 64
 
 # every symbol include/magneton.h declares
 EXPORTED = (
@@ -52,6 +63,10 @@ EXPORTED = (
     "mag_stream_workspace_size", "mag_stream_begin", "mag_stream_push", "mag_stream_end",
     "mag_stream_abort", "mag_stream_state_export", "mag_stream_state_import",
     "mag_stream_host_staging_size", "mag_stream_set_host_staging", "mag_stream_push_host",
+    "mag_linear_workspace_size", "mag_linear",
+    "mag_linear_backward_workspace_size", "mag_linear_backward",
+    "mag_layer_norm", "mag_layer_norm_backward_workspace_size", "mag_layer_norm_backward",
+    "mag_orthogonalize_workspace_size", "mag_orthogonalize",
     "mag_strerror", "mag_last_error", "mag_version",
 )
 
@@ -111,6 +126,14 @@ class DetectOut(ctypes.Structure):
     _fields_ = [("rank", RankOut), ("latency_a", c_vp), ("latency_b", c_vp), ("verdict", c_vp),
                 ("n_flagged", c_i64), ("n_waste", c_i64), ("n_tradeoff", c_i64)]
 
+
+# The argument structs of the block's operators, packed in one go (native
+# alignment, pointers as integers): five fields a matrix.
+_MAT = "Pqqqq"
+LINEAR_ARGS = struct.Struct("@ii" + 5 * _MAT + "P")
+LINEAR_BACKWARD_ARGS = struct.Struct("@ii" + 6 * _MAT + "P")
+NORM_ARGS = struct.Struct("@ii" + 4 * _MAT + "PPPPPPd")
+ORTHOGONALIZE_ARGS = struct.Struct("@iiq" + 2 * _MAT + "qqdddd")
 
 _lib = None
 
@@ -203,6 +226,17 @@ def load(path: str = LIB_PATH):
     lib.mag_stream_set_host_staging.restype = ctypes.c_int
     lib.mag_stream_push_host.argtypes = [c_vp, c_vp, c_vp, c_i64]
     lib.mag_stream_push_host.restype = ctypes.c_int
+    # (the argument structs come packed, as bytes)
+    c_bytes, c_size = ctypes.c_char_p, ctypes.c_size_t
+    for name in ("linear", "linear_backward", "layer_norm_backward", "orthogonalize"):
+        size = getattr(lib, f"mag_{name}_workspace_size")
+        size.argtypes = [c_bytes, P(c_size)]
+        size.restype = ctypes.c_int
+        call = getattr(lib, f"mag_{name}")
+        call.argtypes = [c_bytes, c_vp, c_size, c_vp]
+        call.restype = ctypes.c_int
+    lib.mag_layer_norm.argtypes = [c_bytes, c_vp]
+    lib.mag_layer_norm.restype = ctypes.c_int
     lib.mag_strerror.argtypes = [ctypes.c_int]
     lib.mag_strerror.restype = ctypes.c_char_p
     lib.mag_last_error.argtypes = []

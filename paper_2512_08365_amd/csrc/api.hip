@@ -355,6 +355,10 @@ struct EventTimer {
 
 namespace mag {
 
+int set_error(int code, const char* msg) { return fail(code, msg); }
+int set_hip_error(hipError_t e, const char* where) { return hip_fail(e, where); }
+void clear_error() { g_last_error[0] = 0; }
+
 int device_cu_count()
 {
     static int cached[16] = {};  // per device, queried once
