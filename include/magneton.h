@@ -745,8 +745,10 @@ int mag_stream_push_host(mag_stream* handle, const double* t_host, const float* 
 #define MAG_ACT_GELU_TANH 3
 #define MAG_ACT_SILU 4
 
-/* Largest extent of a matrix and largest reduction. */
+/* Largest extent of a matrix, and of the two that are a layer's features (in,
+   out, the sides of an update). */
 #define MAG_MAX_EXTENT (1LL << 30)
+#define MAG_MAX_FEATURES (1LL << 22)
 
 /* A matrix on the device.  Element (i, j) is data[i * row_stride + j *
    col_stride].  Inputs may have any strides >= 0 (0: one row or column read
@@ -850,7 +852,7 @@ int mag_layer_norm_backward(const mag_norm_args* args, void* workspace, size_t w
 typedef struct mag_orthogonalize_args {
     int32_t dtype;     /* of g and out                                             */
     int32_t steps;     /* 0 .. MAG_ORTH_MAX_STEPS                                  */
-    int64_t batch;     /* matrices of one shape, each on its own                   */
+    int64_t batch;     /* matrices of one shape, each on its own; at most 65535    */
     mag_matrix g;      /* [rows, cols], the first matrix                           */
     mag_matrix out;    /* output [rows, cols]; may be g itself                     */
     int64_t g_batch_stride, out_batch_stride; /* in elements                       */

@@ -91,6 +91,115 @@ bool same_shape(const mag_matrix& m, int64_t rows, int64_t cols)
         if (e_ != hipSuccess) return set_hip_error(e_, where);    \
     } while (0)
 
+// ----------------------------------------------------------------- operands
+
+constexpr int64_t MOST_LD = 1LL << 22;  // 256 rows of it stay within 31 bits of bytes
+int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+int parts(int dtype) { return dtype == MAG_F32 ? 3 : 1; }
+
+// How a product reads a matrix: where it lies, or as rows packed into the
+// workspace (fp32, which is cut into parts, and strides, alignments and widths
+// that the 16-byte loads do not take).
+struct Operand {
+    bool packed;
+    size_t bytes;      // of the packed rows
+    mag::MmOperand op; // p NULL while packed rows have no place yet
+};
+
+// along: the reduction runs along the matrix's columns (else along its rows)
+Operand operand(const mag_matrix& m, int dtype, bool along)
+{
+    Operand o{};
+    if (dtype != MAG_F32 && aligned(m.data, 16)) {
+        const bool by_rows = (m.cols <= 1 || m.col_stride == 1) && m.cols % 8 == 0 &&
+                             (m.rows <= 1 || (m.row_stride % 8 == 0 && m.row_stride < MOST_LD));
+        const bool by_cols = m.row_stride == 1 && m.rows % 8 == 0 && m.rows > 1 &&
+                             (m.cols <= 1 || (m.col_stride % 8 == 0 && m.col_stride < MOST_LD));
+        if (by_rows || by_cols) {
+            o.op.p = m.data;
+            o.op.ld = by_rows ? (m.rows <= 1 ? 0 : m.row_stride) : (m.cols <= 1 ? 0 : m.col_stride);
+            o.op.mc = by_rows != along;
+            return o;
+        }
+    }
+    o.packed = true;
+    o.op.ld = up8(m.cols);
+    o.op.plane = m.rows * o.op.ld;
+    o.op.mc = !along;
+    o.bytes = (size_t)(o.op.plane * 2 * parts(dtype));
+    return o;
+}
+
+int pack(const Operand& o, const mag_matrix& m, int dtype, hipStream_t stream)
+{
+    mag::PackParams p{};
+    p.src = m.data;
+    p.rs = m.row_stride;
+    p.cs = m.col_stride;
+    p.rows = m.rows;
+    p.cols = m.cols;
+    p.dst = const_cast<void*>(o.op.p);
+    p.ld = o.op.ld;
+    p.plane = o.op.plane;
+    TRY_HIP(mag::launch_pack(p, dtype, stream), "pack launch");
+    return MAG_OK;
+}
+
+// the products of parts that fp32 operands take, smallest first: (0,2) (2,0)
+// (1,1) (0,1) (1,0) (0,0); of halves: (0,1) (1,0) (0,0)
+void set_products(mag::Mm& p, int n)
+{
+    p.products = n;
+    p.parts_a = n == 6 ? 0x010120 : n == 3 ? 0x010 : 0;
+    p.parts_b = n == 6 ? 0x001102 : n == 3 ? 0x001 : 0;
+}
+
+// Tile and splits of R x S x K.
+struct Shape {
+    int tile;
+    int splits;
+};
+
+Shape choose(int64_t R, int64_t S, int64_t K, int products, int64_t batch, bool may_split)
+{
+    auto tiles = [&](int t) {
+        const int64_t side = mag::TILE_SIDE[t];
+        return (R + side - 1) / side * ((S + side - 1) / side) * batch;
+    };
+    const int64_t steps = std::max<int64_t>(1, (K + 63) / 64) * products;
+    if (tiles(mag::TILE_256) >= 224) return {mag::TILE_256, 1};
+    if (tiles(mag::TILE_128) >= 224) return {mag::TILE_128, 1};
+    const int64_t n = std::max<int64_t>(1, tiles(mag::TILE_64));
+    if (!may_split || n >= 256) return {mag::TILE_64, 1};
+    return {mag::TILE_64, (int)std::max<int64_t>(1, std::min<int64_t>({512 / n, steps / 4, 64}))};
+}
+
+int launch_linear(const mag::Mm& p, int dtype, int tile, hipStream_t stream)
+{
+    if (p.splits > 1) {
+        TRY_HIP(mag::launch_mm_partial(p, dtype == MAG_F16 ? MAG_F16 : MAG_BF16, tile, stream),
+                "product launch");
+        TRY_HIP(mag::launch_mm_join(p, dtype, stream), "join launch");
+        return MAG_OK;
+    }
+    TRY_HIP(dtype == MAG_F32 ? mag::launch_mm_f32(p, tile, stream)
+            : dtype == MAG_F16 ? mag::launch_mm_f16(p, tile, stream)
+                               : mag::launch_mm_bf16(p, tile, stream),
+            "product launch");
+    return MAG_OK;
+}
+
+size_t partial_bytes(int64_t R, int64_t S, const Shape& s)
+{
+    return s.splits > 1 ? (size_t)(s.splits * R * ((S + 3) / 4 * 4) * 4) : 0;
+}
+
+// whether four neighbours of a row of width n can be moved at once
+bool vec4(const void* p, int64_t rows, int64_t row_stride, int64_t n, int dtype)
+{
+    return !p || (n % 4 == 0 && (rows <= 1 || row_stride % 4 == 0) && aligned(p, 4 * element(dtype)));
+}
+
 // ------------------------------------------------------------------- linear
 
 int check_linear(const mag_linear_args* a)
@@ -101,19 +210,67 @@ int check_linear(const mag_linear_args* a)
     TRY(check_shape(a->weight, false));
     if (a->x.cols != a->weight.cols)
         return set_error(MAG_E_SIZE, "x and weight differ in their columns");
+    if (a->weight.rows > MAG_MAX_FEATURES || a->weight.cols > MAG_MAX_FEATURES)
+        return set_error(MAG_E_SIZE, "in or out exceeds MAG_MAX_FEATURES");
     return MAG_OK;
+}
+
+struct LinearPlan {
+    Operand x, w;
+    Shape shape;
+    float* partial;
+};
+
+size_t plan_linear(const mag_linear_args* a, void* ws, LinearPlan& pl)
+{
+    pl.x = operand(a->x, a->dtype, true);
+    pl.w = operand(a->weight, a->dtype, true);
+    const int products = a->dtype == MAG_F32 ? 6 : 1;
+    pl.shape = choose(a->x.rows, a->weight.rows, a->x.cols, products, 1, true);
+    Carve c{static_cast<char*>(ws)};
+    for (Operand* o : {&pl.x, &pl.w})
+        if (o->packed) o->op.p = c.take(o->bytes);
+    pl.partial = c.take<float>(partial_bytes(a->x.rows, a->weight.rows, pl.shape));
+    return c.off;
 }
 
 // ------------------------------------------------------------------ backward
 
-struct BackwardWorkspace {
-    void* dz;
+struct BackwardPlan {
+    Operand x, w, dy;
+    bool own_dz;      // dz in the workspace (else dy is dz)
+    mag::MmOperand dz;
+    Shape dx, dw;
+    float* partial;
+    float* column_part;
 };
 
-size_t carve_backward(const mag_linear_backward_args* a, void* ws, BackwardWorkspace& w)
+size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& pl)
 {
+    const int64_t M = a->x.rows, N = a->weight.rows, K = a->x.cols;
+    const int products = a->dtype == MAG_F32 ? 6 : 1;
+    // x and weight are both read across the reduction of the product they enter
+    pl.x = operand(a->x, a->dtype, false);
+    pl.w = operand(a->weight, a->dtype, false);
+    pl.dy = operand(a->dy, a->dtype, true);
+    // (as for the sizes: room for dz whether or not dy can stand in for it)
+    pl.own_dz = a->activation != MAG_ACT_NONE || pl.dy.packed || !a->dy.data;
+    if (pl.own_dz) {
+        pl.dz = mag::MmOperand{};
+        pl.dz.ld = up8(N);
+        pl.dz.plane = M * pl.dz.ld;
+    } else {
+        pl.dz = pl.dy.op;
+    }
+    pl.dx = choose(M, K, N, products, 1, true);
+    pl.dw = choose(N, K, M, products, 1, true);
     Carve c{static_cast<char*>(ws)};
-    w.dz = c.take((size_t)a->x.rows * a->weight.rows * element(a->dtype));
+    for (Operand* o : {&pl.x, &pl.w})
+        if (o->packed) o->op.p = c.take(o->bytes);
+    void* dz = c.take((size_t)(M * up8(N) * 2 * parts(a->dtype)));
+    if (pl.own_dz) pl.dz.p = dz;
+    pl.column_part = c.take<float>((size_t)(mag::slope_chunks(M, N) * N * 4));
+    pl.partial = c.take<float>(std::max(partial_bytes(M, K, pl.dx), partial_bytes(N, K, pl.dw)));
     return c.off;
 }
 
@@ -125,6 +282,8 @@ int check_backward(const mag_linear_backward_args* a)
     TRY(check_shape(a->weight, false));
     if (a->x.cols != a->weight.cols)
         return set_error(MAG_E_SIZE, "x and weight differ in their columns");
+    if (a->weight.rows > MAG_MAX_FEATURES || a->weight.cols > MAG_MAX_FEATURES)
+        return set_error(MAG_E_SIZE, "in or out exceeds MAG_MAX_FEATURES");
     return MAG_OK;
 }
 
@@ -143,19 +302,27 @@ int check_norm(const mag_norm_args* a)
 
 // ------------------------------------------------------------- orthogonalize
 
-struct OrthWorkspace {
-    float* X[2];
-    float* A;
-    float* B;
+// g's orientation is kept: X is g or its transpose, read either way
+struct OrthPlan {
+    int64_t m, n;       // sides of X, m <= n
+    int64_t ld, lda;    // of g's rows and of A's and B's
+    double* part;
+    mag::f16* X[2];
+    mag::f16* A;
+    mag::f16* B;
 };
 
-size_t carve_orth(const mag_orthogonalize_args* a, void* ws, OrthWorkspace& w)
+size_t plan_orth(const mag_orthogonalize_args* a, void* ws, OrthPlan& pl)
 {
-    const size_t m = (size_t)std::min(a->g.rows, a->g.cols), n = (size_t)std::max(a->g.rows, a->g.cols);
+    pl.m = std::min(a->g.rows, a->g.cols);
+    pl.n = std::max(a->g.rows, a->g.cols);
+    pl.ld = up8(a->g.cols);
+    pl.lda = up8(pl.m);
     Carve c{static_cast<char*>(ws)};
-    for (auto& x : w.X) x = c.take<float>((size_t)a->batch * m * n * 4);
-    w.A = c.take<float>((size_t)a->batch * m * m * 4);
-    w.B = c.take<float>((size_t)a->batch * m * m * 4);
+    pl.part = c.take<double>((size_t)(a->batch * mag::ORTH_CHUNKS * 8));
+    for (auto& x : pl.X) x = c.take<mag::f16>((size_t)(a->batch * a->g.rows * pl.ld * 4));
+    pl.A = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 4));
+    pl.B = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 4));
     return c.off;
 }
 
@@ -163,10 +330,12 @@ int check_orth(const mag_orthogonalize_args* a)
 {
     if (!a) return set_error(MAG_E_NULL, "args is NULL");
     if (!known_dtype(a->dtype)) return set_error(MAG_E_SIZE, "unknown dtype");
-    if (a->batch < 0 || a->batch > MAX_DIM) return set_error(MAG_E_SIZE, "batch out of range");
+    if (a->batch < 0 || a->batch > 65535) return set_error(MAG_E_SIZE, "batch out of [0, 65535]");
     if (a->steps < 0 || a->steps > MAG_ORTH_MAX_STEPS)
         return set_error(MAG_E_SIZE, "steps out of [0, MAG_ORTH_MAX_STEPS]");
     TRY(check_shape(a->g, false));
+    if (a->g.rows > MAG_MAX_FEATURES || a->g.cols > MAG_MAX_FEATURES)
+        return set_error(MAG_E_SIZE, "a side exceeds MAG_MAX_FEATURES");
     if (a->g_batch_stride < 0 || a->g_batch_stride > (1LL << 62) / std::max<int64_t>(a->batch, 1))
         return set_error(MAG_E_SIZE, "g_batch_stride out of range");
     return MAG_OK;
@@ -195,7 +364,8 @@ int mag_linear_workspace_size(const mag_linear_args* args, size_t* bytes)
     clear_error();
     if (!bytes) return set_error(MAG_E_NULL, "bytes is NULL");
     TRY(check_linear(args));
-    *bytes = 0;
+    LinearPlan pl;
+    *bytes = plan_linear(args, nullptr, pl);
     return MAG_OK;
 }
 
@@ -223,20 +393,23 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     TRY(check_data(a->weight, a->dtype));
     TRY(check_data(a->y, a->dtype));
     TRY(check_vector(a->bias, a->dtype));
-    (void)workspace;
-    (void)workspace_bytes;
-    mag::Product p{};
-    p.a = a->x.data;
-    p.b = a->weight.data;
+    LinearPlan pl;
+    TRY(check_workspace(workspace, workspace_bytes, plan_linear(a, nullptr, pl)));
+    if (M == 0 || N == 0) return MAG_OK;
+    plan_linear(a, workspace, pl);
+    if (pl.x.packed) TRY(pack(pl.x, a->x, a->dtype, stream));
+    if (pl.w.packed) TRY(pack(pl.w, a->weight, a->dtype, stream));
+    mag::Mm p{};
+    p.a = pl.x.op;
+    p.b = pl.w.op;
     p.R = M;
     p.S = N;
     p.K = K;
     p.batch = 1;
-    p.a_rs = a->x.row_stride;
-    p.a_ks = a->x.col_stride;
-    p.b_ss = a->weight.row_stride;
-    p.b_ks = a->weight.col_stride;
-    p.e.scale = 1.0f;
+    set_products(p, a->dtype == MAG_F32 ? 6 : 1);
+    p.splits = pl.shape.splits;
+    p.partial = pl.partial;
+    p.partial_ld = (N + 3) / 4 * 4;
     p.e.bias = a->bias;
     p.e.act = a->activation;
     p.e.res = a->residual.data;
@@ -246,8 +419,10 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     p.e.pre_ld = a->pre.row_stride;
     p.e.y = a->y.data;
     p.e.y_ld = a->y.row_stride;
-    TRY_HIP(mag::launch_product(p, a->dtype, stream), "linear launch");
-    return MAG_OK;
+    p.e.vec = vec4(p.e.y, M, p.e.y_ld, N, a->dtype) && vec4(p.e.pre, M, p.e.pre_ld, N, a->dtype) &&
+              vec4(p.e.bias, 1, 0, N, a->dtype) && vec4(p.e.res, M, p.e.res_rs, N, a->dtype) &&
+              (!p.e.res || p.e.res_cs == 1);
+    return launch_linear(p, a->dtype, pl.shape.tile, stream);
 }
 
 int mag_linear_backward_workspace_size(const mag_linear_backward_args* args, size_t* bytes)
@@ -255,8 +430,8 @@ int mag_linear_backward_workspace_size(const mag_linear_backward_args* args, siz
     clear_error();
     if (!bytes) return set_error(MAG_E_NULL, "bytes is NULL");
     TRY(check_backward(args));
-    BackwardWorkspace w;
-    *bytes = carve_backward(args, nullptr, w);
+    BackwardPlan pl;
+    *bytes = plan_backward(args, nullptr, pl);
     return MAG_OK;
 }
 
@@ -288,52 +463,57 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         TRY(check_data(a->x, a->dtype));
     }
     TRY(check_vector(a->dbias, a->dtype));
-    BackwardWorkspace w;
-    TRY(check_workspace(workspace, workspace_bytes, carve_backward(a, nullptr, w)));
-    carve_backward(a, workspace, w);
-    mag::SlopeParams s{};
-    s.dy = a->dy.data;
-    s.dy_rs = a->dy.row_stride;
-    s.dy_cs = a->dy.col_stride;
-    s.pre = a->pre.data;
-    s.pre_rs = a->pre.row_stride;
-    s.pre_cs = a->pre.col_stride;
-    s.M = M;
-    s.N = N;
-    s.act = a->activation;
-    s.dz = w.dz;
-    s.ldz = N;
-    s.dbias = a->dbias;
-    TRY_HIP(mag::launch_slope(s, a->dtype, stream), "linear_backward launch");
-    mag::Product p{};
+    BackwardPlan pl;
+    TRY(check_workspace(workspace, workspace_bytes, plan_backward(a, nullptr, pl)));
+    if (N == 0 && !a->dx.data) return MAG_OK;
+    plan_backward(a, workspace, pl);
+    if (pl.own_dz || a->dbias) {
+        mag::SlopeParams s{};
+        s.dy = a->dy.data;
+        s.dy_rs = a->dy.row_stride;
+        s.dy_cs = a->dy.col_stride;
+        s.pre = a->pre.data;
+        s.pre_rs = a->pre.row_stride;
+        s.pre_cs = a->pre.col_stride;
+        s.M = M;
+        s.N = N;
+        s.act = a->activation;
+        s.dz = pl.own_dz && (a->dx.data || a->dweight.data) ? const_cast<void*>(pl.dz.p) : nullptr;
+        s.ldz = pl.dz.ld;
+        s.plane = pl.dz.plane;
+        s.dbias = a->dbias;
+        s.part = pl.column_part;
+        TRY_HIP(mag::launch_slope(s, a->dtype, stream), "linear_backward launch");
+    }
+    mag::Mm p{};
     p.batch = 1;
-    p.e.scale = 1.0f;
-    p.a = w.dz;
-    if (a->dx.data) {
+    set_products(p, a->dtype == MAG_F32 ? 6 : 1);
+    p.partial = pl.partial;
+    p.S = K;
+    p.partial_ld = (K + 3) / 4 * 4;
+    p.a = pl.dz;
+    if (a->dx.data && M > 0 && K > 0) {
+        if (pl.w.packed) TRY(pack(pl.w, a->weight, a->dtype, stream));
+        p.b = pl.w.op;
         p.R = M;
-        p.S = K;
         p.K = N;
-        p.a_rs = N;
-        p.a_ks = 1;
-        p.b = a->weight.data;
-        p.b_ss = a->weight.col_stride;
-        p.b_ks = a->weight.row_stride;
+        p.splits = pl.dx.splits;
         p.e.y = a->dx.data;
         p.e.y_ld = a->dx.row_stride;
-        TRY_HIP(mag::launch_product(p, a->dtype, stream), "linear_backward launch");
+        p.e.vec = vec4(p.e.y, M, p.e.y_ld, K, a->dtype);
+        TRY(launch_linear(p, a->dtype, pl.dx.tile, stream));
     }
-    if (a->dweight.data) {
+    if (a->dweight.data && N > 0 && K > 0) {
+        if (pl.x.packed) TRY(pack(pl.x, a->x, a->dtype, stream));
+        p.a.mc = !pl.dz.mc;
+        p.b = pl.x.op;
         p.R = N;
-        p.S = K;
         p.K = M;
-        p.a_rs = 1;
-        p.a_ks = N;
-        p.b = a->x.data;
-        p.b_ss = a->x.col_stride;
-        p.b_ks = a->x.row_stride;
+        p.splits = pl.dw.splits;
         p.e.y = a->dweight.data;
         p.e.y_ld = a->dweight.row_stride;
-        TRY_HIP(mag::launch_product(p, a->dtype, stream), "linear_backward launch");
+        p.e.vec = vec4(p.e.y, N, p.e.y_ld, K, a->dtype);
+        TRY(launch_linear(p, a->dtype, pl.dw.tile, stream));
     }
     return MAG_OK;
 }
@@ -427,8 +607,8 @@ int mag_orthogonalize_workspace_size(const mag_orthogonalize_args* args, size_t*
     clear_error();
     if (!bytes) return set_error(MAG_E_NULL, "bytes is NULL");
     TRY(check_orth(args));
-    OrthWorkspace w;
-    *bytes = carve_orth(args, nullptr, w);
+    OrthPlan pl;
+    *bytes = plan_orth(args, nullptr, pl);
     return MAG_OK;
 }
 
@@ -444,75 +624,114 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         return set_error(MAG_E_SIZE, "the matrices of out overlap");
     if (!isfinite(a->a) || !isfinite(a->b) || !isfinite(a->c) || !(a->eps >= 0.0) || isinf(a->eps))
         return set_error(MAG_E_SIZE, "coefficients must be finite and eps finite and >= 0");
-    double most = 1.0;  // bounds X's singular values, and with them its elements
+    // bounds of X's singular values step by step, and with them of its elements
+    double most[MAG_ORTH_MAX_STEPS + 1] = {1.001};
     for (int i = 0; i < a->steps; ++i) {
-        most = 1.001 * most_of_polynomial(a->a, a->b, a->c, most);
-        if (!(most < 0x1p60)) return set_error(MAG_E_SIZE, "the polynomial grows past 2^60 over these steps");
+        most[i + 1] = 1.001 * most_of_polynomial(a->a, a->b, a->c, most[i]);
+        const double u2 = most[i] * most[i];
+        if (!(most[i + 1] < 0x1p60 && fabs(a->b) * u2 + fabs(a->c) * u2 * u2 < 0x1p60))
+            return set_error(MAG_E_SIZE, "the polynomial grows past 2^60 over these steps");
     }
     if (a->batch == 0 || a->g.rows == 0 || a->g.cols == 0) return MAG_OK;
     TRY(check_data(a->g, a->dtype));
     TRY(check_data(a->out, a->dtype));
-    OrthWorkspace w;
-    TRY(check_workspace(workspace, workspace_bytes, carve_orth(a, nullptr, w)));
-    carve_orth(a, workspace, w);
+    OrthPlan pl;
+    TRY(check_workspace(workspace, workspace_bytes, plan_orth(a, nullptr, pl)));
+    plan_orth(a, workspace, pl);
     const bool tall = a->g.rows > a->g.cols;
-    const int64_t m = std::min(a->g.rows, a->g.cols), n = std::max(a->g.rows, a->g.cols);
+    const int64_t m = pl.m, n = pl.n;
+    const int64_t x_batch = a->g.rows * pl.ld, x_plane = a->batch * x_batch;
+    const int64_t a_batch = m * pl.lda, a_plane = a->batch * a_batch;
+    // halves hold a value times a power of two that takes its bound near 2^15
+    auto scale_for = [](double bound) { return ldexp(1.0, 15 - ilogb(bound) - 1); };
+
     mag::OrthParams o{};
     o.g = a->g.data;
     o.g_batch = a->g_batch_stride;
-    o.g_rs = tall ? a->g.col_stride : a->g.row_stride;
-    o.g_cs = tall ? a->g.row_stride : a->g.col_stride;
-    o.out = a->out.data;
-    o.out_batch = a->out_batch_stride;
-    o.out_rs = tall ? 1 : a->out.row_stride;
-    o.out_cs = tall ? a->out.row_stride : 1;
+    o.g_rs = a->g.row_stride;
+    o.g_cs = a->g.col_stride;
     o.batch = a->batch;
-    o.m = m;
-    o.n = n;
+    o.rows = a->g.rows;
+    o.cols = a->g.cols;
     o.eps = a->eps;
-    o.X = w.X[0];
+    o.part = pl.part;
+    double sx = scale_for(most[0]);
+    if (a->steps > 0) {
+        o.scale = (float)sx;
+        o.z = pl.X[0];
+        o.z_ld = pl.ld;
+        o.z_plane = x_plane;
+        o.z_batch = x_batch;
+    } else {
+        o.scale = 1.0f;
+        o.out = a->out.data;
+        o.out_ld = a->out.row_stride;
+        o.out_batch = a->out_batch_stride;
+    }
     TRY_HIP(mag::launch_orth_begin(o, a->dtype, stream), "orthogonalize launch");
+    const Shape side = choose(m, m, n, 3, a->batch, false);
+    const Shape whole = choose(a->g.rows, a->g.cols, m, 3, a->batch, false);
     for (int i = 0; i < a->steps; ++i) {
-        float* X = w.X[i & 1];
-        mag::Product p{};
-        p.batch = a->batch;
-        p.a_rs = p.b_ss = n;
-        p.a_ks = p.b_ks = 1;
+        const double u2 = most[i] * most[i];
+        const double sa = scale_for(1.01 * u2);
+        const double sb = scale_for(1.01 * (fabs(a->b) * u2 + fabs(a->c) * u2 * u2) + 0x1p-100);
+        const double next = scale_for(most[i + 1] + 0x1p-100);
+        const mag::MmOperand X{pl.X[i & 1], pl.ld, x_plane, x_batch, 0};
+        const mag::MmOperand A{pl.A, pl.lda, a_plane, a_batch, 0};
+        const mag::MmOperand B{pl.B, pl.lda, a_plane, a_batch, 0};
+        // A = X X^T
+        mag::Mm p{};
+        p.batch = (int)a->batch;
+        p.splits = 1;
+        set_products(p, 3);
         p.a = p.b = X;
-        p.a_batch = p.b_batch = m * n;
+        p.a.mc = p.b.mc = tall;
         p.R = p.S = m;
         p.K = n;
-        p.y_batch = p.mixed_batch = m * m;
-        p.e.scale = 1.0f;
-        p.e.y = w.A;
-        p.e.y_ld = m;
-        TRY_HIP(mag::launch_product(p, MAG_F32, stream), "orthogonalize launch");
-        p.a = p.b = w.A;
-        p.a_rs = p.b_ss = m;
-        p.a_batch = p.b_batch = m * m;
+        p.symmetric = 1;
+        p.o.scale = (float)(sa / (sx * sx));
+        p.o.z = pl.A;
+        p.o.z_ld = pl.lda;
+        p.o.z_plane = a_plane;
+        p.o.z_batch = a_batch;
+        TRY_HIP(mag::launch_mm_orth(p, side.tile, stream), "orthogonalize launch");
+        // B = b A + c A A
+        p.a = p.b = A;
         p.K = m;
-        p.e.scale = (float)a->c;
-        p.e.mix = (float)a->b;
-        p.e.mixed = w.A;
-        p.e.mixed_ld = m;
-        p.e.y = w.B;
-        TRY_HIP(mag::launch_product(p, MAG_F32, stream), "orthogonalize launch");
-        p.a = w.B;
-        p.b = X;
-        p.b_ss = 1;
-        p.b_ks = n;
-        p.b_batch = m * n;
-        p.S = n;
-        p.e.scale = 1.0f;
-        p.e.mix = (float)a->a;
-        p.e.mixed = X;
-        p.e.mixed_ld = n;
-        p.mixed_batch = p.y_batch = m * n;
-        p.e.y = o.X = w.X[(i + 1) & 1];
-        p.e.y_ld = n;
-        TRY_HIP(mag::launch_product(p, MAG_F32, stream), "orthogonalize launch");
+        p.o.scale = (float)(a->c * sb / (sa * sa));
+        p.o.mix = (float)(a->b * sb / sa);
+        p.o.m = pl.A;
+        p.o.m_ld = pl.lda;
+        p.o.m_plane = a_plane;
+        p.o.m_batch = a_batch;
+        p.o.z = pl.B;
+        TRY_HIP(mag::launch_mm_orth(p, side.tile, stream), "orthogonalize launch");
+        // X <- a X + B X, or its transpose <- a X^T + X^T B (B symmetric)
+        p.symmetric = 0;
+        p.a = tall ? X : B;
+        p.b = tall ? B : X;
+        p.b.mc = !tall;
+        p.R = a->g.rows;
+        p.S = a->g.cols;
+        const bool last = i + 1 == a->steps;
+        const double out = last ? 1.0 : next;
+        p.o.scale = (float)(out / (sb * sx));
+        p.o.mix = (float)(a->a * out / sx);
+        p.o.m = pl.X[i & 1];
+        p.o.m_ld = pl.ld;
+        p.o.m_plane = x_plane;
+        p.o.m_batch = x_batch;
+        p.o.z = last ? nullptr : pl.X[(i + 1) & 1];
+        p.o.z_ld = pl.ld;
+        p.o.z_plane = x_plane;
+        p.o.z_batch = x_batch;
+        p.o.out = a->out.data;
+        p.o.out_ld = a->out.row_stride;
+        p.o.out_batch = a->out_batch_stride;
+        p.o.dtype = a->dtype;
+        TRY_HIP(mag::launch_mm_orth(p, whole.tile, stream), "orthogonalize launch");
+        sx = next;
     }
-    TRY_HIP(mag::launch_orth_end(o, a->dtype, stream), "orthogonalize launch");
     return MAG_OK;
 }
 

@@ -14,34 +14,81 @@ namespace mag {
 using bf16 = __bf16;
 using f16 = _Float16;
 
-// what is stored of a product's sums (Product::acc) for element (r, s)
+// An operand of a product: element (row, k) at row * ld + k, or with mc at k *
+// ld + row (elements of two bytes; data and rows at multiples of 16 bytes, and
+// the run that is contiguous zero-padded to, or a multiple of, 8).  An fp32
+// operand is three such planes (bfloat16 parts), an update's two.
+struct MmOperand {
+    const void* p;
+    int64_t ld;
+    int64_t plane;  // elements from one part to the next
+    int64_t batch;  // elements from one matrix of a batch to the next
+    int32_t mc;
+};
+
+// z = sum + bias, pre = z, y = act(z) + res
 struct Epilogue {
-    float scale;          // z = scale * sum (+ bias[s]) (+ mix * mixed[r][s])
-    float mix;
-    const float* mixed;
-    int64_t mixed_ld;
-    const void* bias;     // T, or NULL
-    int32_t act;
-    const void* res;      // T, or NULL: y = act(z) + res
+    const void* bias;     // or NULL
+    const void* res;      // or NULL
     int64_t res_rs, res_cs;
-    void* pre;            // T, or NULL: z
+    void* pre;            // or NULL
     int64_t pre_ld;
-    void* y;              // T
+    void* y;
     int64_t y_ld;
+    int32_t act;
+    int32_t vec;          // four neighbours of a row can be moved at once everywhere
 };
 
-// out[r][s] = sum over k of a[r][k] b[s][k], any strides
-struct Product {
-    const void* a;
-    const void* b;
+// z = scale sum + mix M, as two halves (planes) or, for the result, one number
+struct OrthStore {
+    float scale, mix;
+    const f16* m;         // or NULL: its planes
+    int64_t m_ld, m_plane, m_batch;
+    f16* z;               // the planes, or NULL
+    int64_t z_ld, z_plane, z_batch;
+    void* out;            // the result (z NULL)
+    int64_t out_ld, out_batch;
+    int32_t dtype;        // of out
+};
+
+// out[r][s] = sum over k of a(r, k) b(s, k); with several parts an operand, the
+// sum over `products` pairs of parts (part i of the pairs: nibble i)
+struct Mm {
+    MmOperand a, b;
     int64_t R, S, K;
-    int64_t a_rs, a_ks, b_ss, b_ks;
-    int64_t batch, a_batch, b_batch, y_batch, mixed_batch;
+    int32_t batch;
+    int32_t products;
+    uint32_t parts_a, parts_b;
+    int32_t splits;       // of the reduction, each with its own sums in `partial`
+    int32_t symmetric;    // tiles on and above the diagonal only, mirrored (R = S)
+    float* partial;       // [batch][splits][R][partial_ld]
+    int64_t partial_ld;
     Epilogue e;
+    OrthStore o;
 };
+enum { MM_LINEAR, MM_PARTIAL, MM_ORTH };
+enum { TILE_64, TILE_128, TILE_256, TILES };
+constexpr int64_t TILE_SIDE[TILES] = {64, 128, 256};
+// type: of the operands' elements (MAG_BF16 or MAG_F16); tile: TILE_*
+hipError_t launch_mm_bf16(const Mm& p, int tile, hipStream_t stream);  // y bfloat16
+hipError_t launch_mm_f16(const Mm& p, int tile, hipStream_t stream);   // y half
+hipError_t launch_mm_f32(const Mm& p, int tile, hipStream_t stream);   // three parts, y float
+hipError_t launch_mm_partial(const Mm& p, int type, int tile, hipStream_t stream);
+hipError_t launch_mm_orth(const Mm& p, int tile, hipStream_t stream);
+// the partial sums of a split product added up and stored
+hipError_t launch_mm_join(const Mm& p, int dtype, hipStream_t stream);
 
-// dtype: of a, b, bias, res, pre and y (MAG_F32 ...)
-hipError_t launch_product(const Product& p, int dtype, hipStream_t stream);
+// rows x cols values of any strides as rows of ld elements (a multiple of 8,
+// zeros after the last column): two-byte types as they are, fp32 as three
+// bfloat16 planes
+struct PackParams {
+    const void* src;
+    int64_t rs, cs;
+    int64_t rows, cols;
+    void* dst;
+    int64_t ld, plane;
+};
+hipError_t launch_pack(const PackParams& p, int dtype, hipStream_t stream);
 
 // dz = dy act'(pre) (T, row stride ldz), and dbias = the column sums of dz
 struct SlopeParams {
@@ -51,10 +98,12 @@ struct SlopeParams {
     int64_t pre_rs, pre_cs;
     int64_t M, N;
     int32_t act;
-    void* dz;        // NULL: not wanted
-    int64_t ldz;
+    void* dz;        // NULL: not wanted; fp32: three bfloat16 planes
+    int64_t ldz, plane;
     void* dbias;     // NULL: not wanted
+    float* part;     // [slope_chunks(M)][N] column sums of the chunks of rows
 };
+int64_t slope_chunks(int64_t M, int64_t N);
 hipError_t launch_slope(const SlopeParams& p, int dtype, hipStream_t stream);
 
 struct NormParams {
@@ -77,18 +126,23 @@ hipError_t launch_norm(const NormParams& p, int dtype, int weight_dtype, hipStre
 hipError_t launch_norm_backward(const NormParams& p, int dtype, int weight_dtype,
                                 hipStream_t stream);
 
-// one update of `batch` matrices seen as m x n, m <= n
+// `batch` updates of rows x cols: their norms (part: [batch][ORTH_CHUNKS]
+// sums of squares), and scale g / (|g| + eps) as two halves (planes) or, with
+// out, as the result
+constexpr int ORTH_CHUNKS = 64;
 struct OrthParams {
     const void* g;
     int64_t g_batch, g_rs, g_cs;
-    void* out;
-    int64_t out_batch, out_rs, out_cs;
-    int64_t batch, m, n;
+    int64_t batch, rows, cols;
     double eps;
-    float* X;  // [batch][m][n]
+    double* part;
+    float scale;
+    f16* z;
+    int64_t z_ld, z_plane, z_batch;
+    void* out;
+    int64_t out_ld, out_batch;
 };
 hipError_t launch_orth_begin(const OrthParams& p, int dtype, hipStream_t stream);
-hipError_t launch_orth_end(const OrthParams& p, int dtype, hipStream_t stream);
 
 // the host's error record (api.hip)
 int set_error(int code, const char* msg);

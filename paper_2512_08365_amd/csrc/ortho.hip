@@ -1,67 +1,87 @@
-// ortho.hip -- the ends of the orthogonalised update: norm, scaling, result.
+// ortho.hip -- the beginning of an orthogonalised update: norms and scaling.
 
-#include "block.hpp"
+#include <algorithm>
+
+#include "mm.hpp"
 
 namespace mag {
 namespace {
 
+// sums of squares of one of ORTH_CHUNKS runs of rows of a matrix, in fp64 (the
+// squares of fp32 numbers pass its range)
 template <class T>
-__global__ __launch_bounds__(1024) void k_orth_begin(OrthParams p)
+__global__ __launch_bounds__(256) void k_orth_norm(OrthParams p)
 {
-    __shared__ double part[16];
-    const int64_t bt = blockIdx.x, n = p.m * p.n;
+    __shared__ double part[4];
+    const int64_t bt = blockIdx.y;
     const T* g = static_cast<const T*>(p.g) + bt * p.g_batch;
+    const int64_t n = p.rows * p.cols;
+    const int64_t i0 = n * blockIdx.x / ORTH_CHUNKS, i1 = n * (blockIdx.x + 1) / ORTH_CHUNKS;
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 1024) {
-        const double v = (double)(float)g[i / p.n * p.g_rs + i % p.n * p.g_cs];
-        s += v * v;
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += 256) {
+        const double v = (double)(float)g[i / p.cols * p.g_rs + i % p.cols * p.g_cs];
+        s = fma(v, v, s);
     }
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
     if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
     __syncthreads();
-    s = 0.0;
-    for (int w = 0; w < 16; ++w) s += part[w];
-    const double scale = 1.0 / (sqrt(s) + p.eps);
-    for (int64_t i = threadIdx.x; i < n; i += 1024)
-        p.X[bt * n + i] = (float)((double)(float)g[i / p.n * p.g_rs + i % p.n * p.g_cs] * scale);
+    if (threadIdx.x == 0)
+        p.part[bt * ORTH_CHUNKS + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// scale g / (|g| + eps), 8 neighbours of a row a thread
+template <class T>
+__global__ __launch_bounds__(256) void k_orth_scale(OrthParams p)
+{
+    typedef __attribute__((ext_vector_type(8))) f16 h8;
+    const int64_t bt = blockIdx.y;
+    double s = p.part[bt * ORTH_CHUNKS + threadIdx.x % 64];
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
+    const double scale = (double)p.scale / (sqrt(s) + p.eps);
+    const T* g = static_cast<const T*>(p.g) + bt * p.g_batch;
+    const int64_t per_row = (p.cols + 7) / 8, n = p.rows * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / per_row, j = i % per_row * 8;
+        h8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // (0 / 0 of a zero matrix without eps: NaN, as the formula says)
+            const float v = j + e < p.cols
+                ? (float)((double)(float)g[r * p.g_rs + (j + e) * p.g_cs] * scale) : 0.0f;
+            f16 h, l;
+            two_halves(v, h, l);
+            hi[e] = h;
+            lo[e] = l;
+            if (p.out && j + e < p.cols) static_cast<T*>(p.out)[bt * p.out_batch + r * p.out_ld + j + e] = (T)v;
+        }
+        if (p.z) {
+            f16* z = p.z + bt * p.z_batch + r * p.z_ld + j;
+            *(h8*)z = hi;
+            *(h8*)(z + p.z_plane) = lo;
+        }
+    }
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void k_orth_end(OrthParams p)
+hipError_t begin(const OrthParams& p, hipStream_t stream)
 {
-    const int64_t n = p.m * p.n;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n * p.batch;
-         i += (int64_t)gridDim.x * 256) {
-        const int64_t bt = i / n, e = i % n;
-        static_cast<T*>(p.out)[bt * p.out_batch + e / p.n * p.out_rs + e % p.n * p.out_cs] =
-            (T)p.X[i];
-    }
+    hipLaunchKernelGGL(k_orth_norm<T>, dim3(ORTH_CHUNKS, (unsigned)p.batch), dim3(256), 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t n = p.rows * ((p.cols + 7) / 8);
+    hipLaunchKernelGGL(k_orth_scale<T>,
+                       dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096), (unsigned)p.batch),
+                       dim3(256), 0, stream, p);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_orth_begin(const OrthParams& p, int dtype, hipStream_t stream)
 {
-    const dim3 grid((unsigned)p.batch);
-    if (dtype == MAG_F32)
-        hipLaunchKernelGGL(k_orth_begin<float>, grid, dim3(1024), 0, stream, p);
-    else if (dtype == MAG_F16)
-        hipLaunchKernelGGL(k_orth_begin<f16>, grid, dim3(1024), 0, stream, p);
-    else
-        hipLaunchKernelGGL(k_orth_begin<bf16>, grid, dim3(1024), 0, stream, p);
-    return hipGetLastError();
-}
-
-hipError_t launch_orth_end(const OrthParams& p, int dtype, hipStream_t stream)
-{
-    const dim3 grid(2048);
-    if (dtype == MAG_F32)
-        hipLaunchKernelGGL(k_orth_end<float>, grid, dim3(256), 0, stream, p);
-    else if (dtype == MAG_F16)
-        hipLaunchKernelGGL(k_orth_end<f16>, grid, dim3(256), 0, stream, p);
-    else
-        hipLaunchKernelGGL(k_orth_end<bf16>, grid, dim3(256), 0, stream, p);
-    return hipGetLastError();
+    if (dtype == MAG_F32) return begin<float>(p, stream);
+    if (dtype == MAG_F16) return begin<f16>(p, stream);
+    return begin<bf16>(p, stream);
 }
 
 }  // namespace mag
