@@ -191,13 +191,13 @@ int launch_linear(const mag::Mm& p, int dtype, int tile, hipStream_t stream)
 
 size_t partial_bytes(int64_t R, int64_t S, const Shape& s)
 {
-    return s.splits > 1 ? (size_t)(s.splits * R * ((S + 3) / 4 * 4) * 4) : 0;
+    return s.splits > 1 ? (size_t)(s.splits * R * up8(S) * 4) : 0;
 }
 
-// whether four neighbours of a row of width n can be moved at once
-bool vec4(const void* p, int64_t rows, int64_t row_stride, int64_t n, int dtype)
+// whether the rows of a matrix start at multiples of 16 bytes
+bool vec8(const void* p, int64_t rows, int64_t row_stride, int dtype)
 {
-    return !p || (n % 4 == 0 && (rows <= 1 || row_stride % 4 == 0) && aligned(p, 4 * element(dtype)));
+    return !p || ((rows <= 1 || row_stride * (int64_t)element(dtype) % 16 == 0) && aligned(p, 16));
 }
 
 // ------------------------------------------------------------------- linear
@@ -409,7 +409,7 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     set_products(p, a->dtype == MAG_F32 ? 6 : 1);
     p.splits = pl.shape.splits;
     p.partial = pl.partial;
-    p.partial_ld = (N + 3) / 4 * 4;
+    p.partial_ld = up8(N);
     p.e.bias = a->bias;
     p.e.act = a->activation;
     p.e.res = a->residual.data;
@@ -419,8 +419,8 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     p.e.pre_ld = a->pre.row_stride;
     p.e.y = a->y.data;
     p.e.y_ld = a->y.row_stride;
-    p.e.vec = vec4(p.e.y, M, p.e.y_ld, N, a->dtype) && vec4(p.e.pre, M, p.e.pre_ld, N, a->dtype) &&
-              vec4(p.e.bias, 1, 0, N, a->dtype) && vec4(p.e.res, M, p.e.res_rs, N, a->dtype) &&
+    p.e.vec = vec8(p.e.y, M, p.e.y_ld, a->dtype) && vec8(p.e.pre, M, p.e.pre_ld, a->dtype) &&
+              vec8(p.e.bias, 1, 0, a->dtype) && vec8(p.e.res, M, p.e.res_rs, a->dtype) &&
               (!p.e.res || p.e.res_cs == 1);
     return launch_linear(p, a->dtype, pl.shape.tile, stream);
 }
@@ -490,7 +490,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
     set_products(p, a->dtype == MAG_F32 ? 6 : 1);
     p.partial = pl.partial;
     p.S = K;
-    p.partial_ld = (K + 3) / 4 * 4;
+    p.partial_ld = up8(K);
     p.a = pl.dz;
     if (a->dx.data && M > 0 && K > 0) {
         if (pl.w.packed) TRY(pack(pl.w, a->weight, a->dtype, stream));
@@ -500,7 +500,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         p.splits = pl.dx.splits;
         p.e.y = a->dx.data;
         p.e.y_ld = a->dx.row_stride;
-        p.e.vec = vec4(p.e.y, M, p.e.y_ld, K, a->dtype);
+        p.e.vec = vec8(p.e.y, M, p.e.y_ld, a->dtype);
         TRY(launch_linear(p, a->dtype, pl.dx.tile, stream));
     }
     if (a->dweight.data && N > 0 && K > 0) {
@@ -512,7 +512,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         p.splits = pl.dw.splits;
         p.e.y = a->dweight.data;
         p.e.y_ld = a->dweight.row_stride;
-        p.e.vec = vec4(p.e.y, N, p.e.y_ld, K, a->dtype);
+        p.e.vec = vec8(p.e.y, N, p.e.y_ld, a->dtype);
         TRY(launch_linear(p, a->dtype, pl.dw.tile, stream));
     }
     return MAG_OK;

@@ -36,7 +36,7 @@ struct Epilogue {
     void* y;
     int64_t y_ld;
     int32_t act;
-    int32_t vec;          // four neighbours of a row can be moved at once everywhere
+    int32_t vec;          // 16 bytes of a row can be moved at once everywhere
 };
 
 // z = scale sum + mix M, as two halves (planes) or, for the result, one number

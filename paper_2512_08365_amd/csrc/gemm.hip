@@ -135,17 +135,23 @@ __global__ __launch_bounds__(256) void k_column_sums(const float* part, int64_t 
 template <class TO>
 __global__ __launch_bounds__(256) void k_mm_join(Mm p)
 {
-    const int64_t per_row = p.partial_ld / 4, n = p.R * per_row;
+    const int64_t per_row = p.partial_ld / 8, n = p.R * per_row;
     const int64_t plane = p.R * p.partial_ld;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per_row, s = i % per_row * 4;
+        const int64_t r = i / per_row, s = i % per_row * 8;
         const float* q = p.partial + r * p.partial_ld + s;
-        f32x4 v = *(const f32x4*)q;
-        for (int k = 1; k < p.splits; ++k) v += *(const f32x4*)(q + k * plane);
-        const int m = (int)min((int64_t)4, p.S - s);
+        float v[8], w[8];
+        load8(q, v);
+        for (int k = 1; k < p.splits; ++k) {
+            load8(q + k * plane, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += w[e];
+        }
+        const int m = (int)min((int64_t)8, p.S - s);
         if constexpr (sizeof(TO) == 4)
-            for (int e = 0; e < m; ++e)
-                if (!(fabsf(v[e]) < __builtin_inff())) v[e] = whole_sum(p, 0, r, s + e);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < m && !(fabsf(v[e]) < __builtin_inff())) v[e] = whole_sum(p, 0, r, s + e);
         store_linear<TO>(p.e, r, s, m, v);
     }
 }
@@ -204,7 +210,7 @@ hipError_t launch_slope(const SlopeParams& p, int dtype, hipStream_t stream)
 
 hipError_t launch_mm_join(const Mm& p, int dtype, hipStream_t stream)
 {
-    const dim3 grid(blocks_for(p.R * (p.partial_ld / 4))), block(256);
+    const dim3 grid(blocks_for(p.R * (p.partial_ld / 8))), block(256);
     if (dtype == MAG_F32)
         hipLaunchKernelGGL(k_mm_join<float>, grid, block, 0, stream, p);
     else if (dtype == MAG_F16)
