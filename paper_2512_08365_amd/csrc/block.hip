@@ -296,8 +296,14 @@ int check_norm(const mag_norm_args* a)
     if (a->weight_dtype != a->dtype && a->weight_dtype != MAG_F32)
         return set_error(MAG_E_SIZE, "weight_dtype must be dtype or MAG_F32");
     TRY(check_shape(a->x, false));
-    if (a->x.cols < 1) return set_error(MAG_E_SIZE, "width must be >= 1");
+    if (a->x.cols < 1 || a->x.cols > MAG_MAX_FEATURES)
+        return set_error(MAG_E_SIZE, "width out of [1, MAG_MAX_FEATURES]");
     return MAG_OK;
+}
+
+size_t norm_bytes(const mag_norm_args* a)
+{
+    return (size_t)mag::norm_parts(a->x.rows, a->x.cols) * 2 * (size_t)a->x.cols * 4;
 }
 
 // ------------------------------------------------------------- orthogonalize
@@ -554,7 +560,7 @@ int mag_layer_norm_backward_workspace_size(const mag_norm_args* args, size_t* by
     clear_error();
     if (!bytes) return set_error(MAG_E_NULL, "bytes is NULL");
     TRY(check_norm(args));
-    *bytes = 0;
+    *bytes = norm_bytes(args);
     return MAG_OK;
 }
 
@@ -579,9 +585,9 @@ int mag_layer_norm_backward(const mag_norm_args* a, void* workspace, size_t work
     TRY(check_vector(a->dbias, a->weight_dtype));
     TRY(check_vector(a->mean, MAG_F32));
     TRY(check_vector(a->rstd, MAG_F32));
-    (void)workspace;
-    (void)workspace_bytes;
+    TRY(check_workspace(workspace, workspace_bytes, norm_bytes(a)));
     mag::NormParams p{};
+    p.part = static_cast<float*>(workspace);
     p.x = a->x.data;
     p.x_rs = a->x.row_stride;
     p.x_cs = a->x.col_stride;

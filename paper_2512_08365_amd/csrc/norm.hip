@@ -1,109 +1,417 @@
 // norm.hip -- layer norm, forward and backward.
+//
+// Both passes are bound by memory: every row is read once into registers, and
+// what a row needs of its neighbours is one reduction (the backward pass's two
+// sums go together).  A row belongs to 64, 256 or 1,024 threads, the fewest
+// that hold it in 16 elements each: few enough registers that the rows'
+// weights stay in them from row to row (a 2-byte row's fp32 weight and bias are
+// four times its bytes, and would come from L2 each time), and so do the
+// backward pass's sums over the rows.  Workgroups walk the rows and load the
+// next one before they reduce the present one.
+//
+// A mean is a sum over 16 elements a thread and a tree; the variance is taken
+// from squares about it, both in fp32.
+
+#include <algorithm>
 
 #include "block.hpp"
 
 namespace mag {
 namespace {
 
-__device__ float block_sum(float v, float* lds)
+constexpr int HELD = 16;          // elements a thread
+constexpr int64_t MOST_HELD = 1024 * HELD;  // width of a row that 1,024 threads hold
+constexpr int BACK_WGS = 256;     // workgroups of 1,024 threads (half as many: twice this) of the
+                                  // backward pass, each with its own sums over rows
+
+// The G threads of a row hold V neighbours each, G V further on the next V, and
+// so on: 8 where the width is a multiple of 8 (the hardware takes vector loads
+// at any element), single elements otherwise.
+template <class T, int V>
+struct Held {
+    T v[HELD];
+};
+
+template <int G, int V>
+__device__ __forceinline__ int column(int lane, int e)
 {
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-    __syncthreads();
-    return lds[0] + lds[1] + lds[2] + lds[3];
+    return (e / V * G + lane) * V + e % V;
 }
 
-template <class T, class W>
-__global__ __launch_bounds__(256) void k_norm(NormParams p)
+template <int G, int V, class T>
+__device__ __forceinline__ void get(Held<T, V>& r, const T* row, int lane, int n)
 {
-    __shared__ float lds[4];
-    const int64_t i = blockIdx.x;
+#pragma unroll
+    for (int c = 0; c < HELD / V; ++c) {
+        const int j = (c * G + lane) * V;
+        if (j < n) {
+            __builtin_memcpy(r.v + c * V, row + j, V * sizeof(T));
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) r.v[c * V + i] = (T)0.0f;
+        }
+    }
+}
+
+template <int G, int V, class T>
+__device__ __forceinline__ void put(T* row, int lane, int n, const float* v)
+{
+#pragma unroll
+    for (int c = 0; c < HELD / V; ++c) {
+        const int j = (c * G + lane) * V;
+        T o[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = (T)v[c * V + i];
+        if (j < n) __builtin_memcpy(row + j, o, V * sizeof(T));
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// The sums of a and b over the G threads of a row.  lds: two floats a wave,
+// another place from one call to the next of the same row and the next row's
+// first (one barrier a call: a place is written again two calls later).
+template <int G>
+__device__ __forceinline__ void row_sums(float& a, float& b, float2* lds)
+{
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if constexpr (G > 64) {
+        constexpr int WAVES = G / 64;
+        const int wave = threadIdx.x / 64, first = wave / WAVES * WAVES;
+        if (threadIdx.x % 64 == 0) lds[wave] = float2{a, b};
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float2 s = lds[first + w];
+            a += s.x;
+            b += s.y;
+        }
+    }
+}
+
+template <class T, class W, int G, int V, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
+{
+    constexpr int ROWS = THREADS / G;  // at a time
+    __shared__ float2 lds[2][THREADS / 64];
+    const int lane = threadIdx.x % G, n = (int)p.N;
+    const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x / G);
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    const T* x = static_cast<const T*>(p.x);
+    float w[HELD], b[HELD];
+    {
+        Held<W, V> a{}, d{};
+        if (p.weight) get<G, V>(a, static_cast<const W*>(p.weight), lane, n);
+        if (p.bias) get<G, V>(d, static_cast<const W*>(p.bias), lane, n);
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) {
+            w[e] = p.weight ? (float)a.v[e] : 1.0f;
+            b[e] = (float)d.v[e];
+        }
+    }
+    Held<T, V> next{};
+    const int64_t i0 = (int64_t)blockIdx.x * ROWS;
+    if (i0 + sub < p.M) get<G, V>(next, x + (i0 + sub) * p.x_rs, lane, n);
+    // (the workgroup's rows go together: its barriers are everybody's)
+    for (int64_t base = i0; base < p.M; base += step) {
+        const int64_t i = base + sub;
+        float v[HELD], s = 0.0f, unused = 0.0f;
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) {
+            v[e] = (float)next.v[e];
+            s += v[e];
+        }
+        if (i + step < p.M) get<G, V>(next, x + (i + step) * p.x_rs, lane, n);
+        row_sums<G>(s, unused, lds[0]);
+        const float mean = s / (float)n;
+        s = 0.0f;
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) {
+            v[e] = column<G, V>(lane, e) < n ? v[e] - mean : 0.0f;
+            s = fmaf(v[e], v[e], s);
+        }
+        row_sums<G>(s, unused, lds[1]);
+        const float rstd = 1.0f / sqrtf(s / (float)n + p.eps);
+        if (i >= p.M) continue;
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) v[e] = fmaf(v[e] * rstd, w[e], b[e]);
+        put<G, V>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, v);
+        if (lane == 0) {
+            if (p.mean) p.mean[i] = mean;
+            if (p.rstd) p.rstd[i] = rstd;
+        }
+    }
+}
+
+// rows too wide for the threads' registers, or whose elements are not neighbours
+// in memory: read three times (the second and third time from L2)
+template <class T, class W>
+__global__ __launch_bounds__(1024) void k_norm_wide(NormParams p)
+{
+    __shared__ float2 lds[2][16];
+    const int64_t i = blockIdx.x, n = p.N;
     const T* x = static_cast<const T*>(p.x) + i * p.x_rs;
-    float s = 0.0f;
-    for (int64_t j = threadIdx.x; j < p.N; j += 256) s += (float)x[j * p.x_cs];
-    const float mean = block_sum(s, lds) / (float)p.N;
+    float s = 0.0f, unused = 0.0f;
+    for (int64_t j = threadIdx.x; j < n; j += 1024) s += (float)x[j * p.x_cs];
+    row_sums<1024>(s, unused, lds[0]);
+    const float mean = s / (float)n;
     s = 0.0f;
-    for (int64_t j = threadIdx.x; j < p.N; j += 256) {
+    for (int64_t j = threadIdx.x; j < n; j += 1024) {
         const float d = (float)x[j * p.x_cs] - mean;
         s = fmaf(d, d, s);
     }
-    const float rstd = 1.0f / sqrtf(block_sum(s, lds) / (float)p.N + p.eps);
-    for (int64_t j = threadIdx.x; j < p.N; j += 256) {
-        float y = ((float)x[j * p.x_cs] - mean) * rstd;
-        if (p.weight) y *= (float)static_cast<const W*>(p.weight)[j];
-        if (p.bias) y += (float)static_cast<const W*>(p.bias)[j];
-        static_cast<T*>(p.y)[i * p.y_ld + j] = (T)y;
-    }
+    row_sums<1024>(s, unused, lds[1]);
+    const float rstd = 1.0f / sqrtf(s / (float)n + p.eps);
+    const W *w = static_cast<const W*>(p.weight), *b = static_cast<const W*>(p.bias);
+    for (int64_t j = threadIdx.x; j < n; j += 1024)
+        static_cast<T*>(p.y)[i * p.y_ld + j] =
+            (T)fmaf(((float)x[j * p.x_cs] - mean) * rstd, w ? (float)w[j] : 1.0f, b ? (float)b[j] : 0.0f);
     if (threadIdx.x == 0) {
         if (p.mean) p.mean[i] = mean;
         if (p.rstd) p.rstd[i] = rstd;
     }
 }
 
-template <class T, class W>
-__global__ __launch_bounds__(256) void k_norm_weights(NormParams p)
+// Gradients: each workgroup walks its rows, keeps the sums
+// over them of its columns in registers, adds up the threads of one column at
+// the end through LDS (one set of threads after another: a fixed order) and
+// leaves one row of sums for weight and bias each.
+template <class T, class W, int G, int V, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_norm_back(NormParams p)
+{
+    constexpr int ROWS = THREADS / G;
+    // (1,024 threads have 128 registers each: no room for a row loaded ahead)
+    constexpr bool AHEAD = THREADS < 1024;
+    __shared__ float2 lds[2][THREADS / 64];
+    __shared__ float sums[ROWS == 1 ? 1 : 2][ROWS == 1 ? 1 : G * HELD];
+    const int lane = threadIdx.x % G, n = (int)p.N;
+    const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x / G);
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    const T *x = static_cast<const T*>(p.x), *dy = static_cast<const T*>(p.dy);
+    float w[HELD], dw[HELD] = {}, db[HELD] = {};
+    {
+        Held<W, V> a{};
+        if (p.weight) get<G, V>(a, static_cast<const W*>(p.weight), lane, n);
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) w[e] = p.weight ? (float)a.v[e] : 1.0f;
+    }
+    Held<T, V> nx{}, ny{};
+    auto load = [&](int64_t i) {
+        get<G, V>(nx, x + i * p.x_rs, lane, n);
+        get<G, V>(ny, dy + i * p.dy_rs, lane, n);
+    };
+    const int64_t i0 = (int64_t)blockIdx.x * ROWS;
+    if (AHEAD && i0 + sub < p.M) load(i0 + sub);
+    int turn = 0;
+    for (int64_t base = i0; base < p.M; base += step) {
+        const int64_t i = base + sub;
+        const bool on = i < p.M;
+        const float mean = on ? p.mean[i] : 0.0f, r = on ? p.rstd[i] : 0.0f;
+        if (!AHEAD && on) load(i);
+        float xh[HELD], h[HELD], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) {
+            // (beyond the width, and for a row beyond the last: 0)
+            const bool in = on && column<G, V>(lane, e) < n;
+            xh[e] = in ? ((float)nx.v[e] - mean) * r : 0.0f;
+            const float d = in ? (float)ny.v[e] : 0.0f;
+            dw[e] = fmaf(d, xh[e], dw[e]);
+            db[e] += d;
+            h[e] = d * w[e];
+            s1 += h[e];
+            s2 = fmaf(h[e], xh[e], s2);
+        }
+        if (AHEAD && i + step < p.M) load(i + step);
+        if (!p.y) continue;
+        row_sums<G>(s1, s2, lds[turn ^= 1]);
+        if (!on) continue;
+        s1 /= (float)n;
+        s2 /= (float)n;
+#pragma unroll
+        for (int e = 0; e < HELD; ++e) h[e] = r * (h[e] - s1 - xh[e] * s2);
+        put<G, V>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, h);
+    }
+    if (!p.dweight && !p.dbias) return;
+    float* part = p.part + (int64_t)blockIdx.x * 2 * n;
+    if constexpr (ROWS == 1) {
+        put<G, V>(part, lane, n, dw);
+        put<G, V>(part + n, lane, n, db);
+    } else {
+        for (int t = 0; t < ROWS; ++t) {
+            if (sub == t)
+#pragma unroll
+                for (int e = 0; e < HELD; ++e) {
+                    // (by element, so that neighbouring lanes meet no bank twice)
+                    const int at = e * G + lane;
+                    sums[0][at] = t ? sums[0][at] + dw[e] : dw[e];
+                    sums[1][at] = t ? sums[1][at] + db[e] : db[e];
+                }
+            __syncthreads();
+        }
+        for (int j = threadIdx.x; j < n; j += THREADS) {
+            const int at = (j / V / G * V + j % V) * G + j / V % G;
+            part[j] = sums[0][at];
+            part[n + j] = sums[1][at];
+        }
+    }
+}
+
+// the workgroups' sums added up: 16 waves of 64 columns
+template <class W>
+__global__ __launch_bounds__(1024) void k_norm_columns(const float* part, int parts, int64_t n,
+                                                       W* dweight, W* dbias)
+{
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t j = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (j < 2 * n)
+        for (int k = wave; k < parts; k += 16) s += part[(int64_t)k * 2 * n + j];
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave || j >= 2 * n) return;
+    s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += sums[k][lane];
+    if (j < n && dweight) dweight[j] = (W)s;
+    if (j >= n && dbias) dbias[j - n] = (W)s;
+}
+
+// rows as k_norm_wide's: the sums over the rows by column...
+template <class T>
+__global__ __launch_bounds__(256) void k_norm_back_wide_columns(NormParams p)
 {
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (j >= p.N) return;
     float sw = 0.0f, sb = 0.0f;
-    for (int64_t i = 0; i < p.M; ++i) {
+    for (int64_t i = blockIdx.y; i < p.M; i += gridDim.y) {
         const float d = (float)static_cast<const T*>(p.dy)[i * p.dy_rs + j * p.dy_cs];
         const float xh = ((float)static_cast<const T*>(p.x)[i * p.x_rs + j * p.x_cs] - p.mean[i]) *
                          p.rstd[i];
         sw = fmaf(d, xh, sw);
         sb += d;
     }
-    if (p.dweight) static_cast<W*>(p.dweight)[j] = (W)sw;
-    if (p.dbias) static_cast<W*>(p.dbias)[j] = (W)sb;
+    p.part[(int64_t)blockIdx.y * 2 * p.N + j] = sw;
+    p.part[(int64_t)blockIdx.y * 2 * p.N + p.N + j] = sb;
 }
 
+// ... and dx by row, after them (dx may be written over x or dy)
 template <class T, class W>
-__global__ __launch_bounds__(256) void k_norm_dx(NormParams p)
+__global__ __launch_bounds__(1024) void k_norm_back_wide(NormParams p)
 {
-    __shared__ float lds[4];
-    const int64_t i = blockIdx.x;
+    __shared__ float2 lds[16];
+    const int64_t i = blockIdx.x, n = p.N;
     const T* x = static_cast<const T*>(p.x) + i * p.x_rs;
     const T* dy = static_cast<const T*>(p.dy) + i * p.dy_rs;
-    const float mean = p.mean[i], rstd = p.rstd[i];
     const W* w = static_cast<const W*>(p.weight);
+    const float mean = p.mean[i], rstd = p.rstd[i];
     float s1 = 0.0f, s2 = 0.0f;
-    for (int64_t j = threadIdx.x; j < p.N; j += 256) {
+    for (int64_t j = threadIdx.x; j < n; j += 1024) {
         const float h = (float)dy[j * p.dy_cs] * (w ? (float)w[j] : 1.0f);
         s1 += h;
         s2 = fmaf(h, ((float)x[j * p.x_cs] - mean) * rstd, s2);
     }
-    s1 = block_sum(s1, lds) / (float)p.N;
-    s2 = block_sum(s2, lds) / (float)p.N;
-    for (int64_t j = threadIdx.x; j < p.N; j += 256) {
+    row_sums<1024>(s1, s2, lds);
+    s1 /= (float)n;
+    s2 /= (float)n;
+    for (int64_t j = threadIdx.x; j < n; j += 1024) {
         const float h = (float)dy[j * p.dy_cs] * (w ? (float)w[j] : 1.0f);
         const float xh = ((float)x[j * p.x_cs] - mean) * rstd;
         static_cast<T*>(p.y)[i * p.y_ld + j] = (T)(rstd * (h - s1 - xh * s2));
     }
 }
 
+// threads of a row of width n
+int threads_of(int64_t n) { return n <= 64 * HELD ? 64 : n <= 256 * HELD ? 256 : 1024; }
+// rows that a workgroup of the backward pass takes at a time
+int back_rows(int64_t n) { return n <= 64 * HELD ? 8 : n <= 256 * HELD ? 2 : 1; }
+
+template <class T, class W, int V>
+void forward_held(const NormParams& p, hipStream_t stream)
+{
+    // as many workgroups as the device holds at once, the rows spread evenly
+    // over them
+    const int G = threads_of(p.N), rows = G == 64 ? 4 : 1;
+    const int64_t groups = (p.M + rows - 1) / rows;
+    const int64_t most = G == 1024 ? 512 : 2048, rounds = (groups + most - 1) / most;
+    const dim3 grid((unsigned)((groups + rounds - 1) / rounds));
+    if (G == 64)
+        hipLaunchKernelGGL((k_norm<T, W, 64, V, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 256)
+        hipLaunchKernelGGL((k_norm<T, W, 256, V, 256>), grid, dim3(256), 0, stream, p);
+    else
+        hipLaunchKernelGGL((k_norm<T, W, 1024, V, 1024>), grid, dim3(1024), 0, stream, p);
+}
+
 template <class T, class W>
 hipError_t forward(const NormParams& p, hipStream_t stream)
 {
-    hipLaunchKernelGGL((k_norm<T, W>), dim3((unsigned)p.M), dim3(256), 0, stream, p);
+    if (p.N > MOST_HELD || p.x_cs != 1)
+        hipLaunchKernelGGL((k_norm_wide<T, W>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
+    else if (p.N % 8 == 0)
+        forward_held<T, W, 8>(p, stream);
+    else
+        forward_held<T, W, 1>(p, stream);
     return hipGetLastError();
+}
+
+template <class T, class W, int V>
+void backward_held(const NormParams& p, int parts, hipStream_t stream)
+{
+    const int G = threads_of(p.N);
+    const dim3 grid(parts);
+    if (G == 64)
+        hipLaunchKernelGGL((k_norm_back<T, W, 64, V, 512>), grid, dim3(512), 0, stream, p);
+    else if (G == 256)
+        hipLaunchKernelGGL((k_norm_back<T, W, 256, V, 512>), grid, dim3(512), 0, stream, p);
+    else
+        hipLaunchKernelGGL((k_norm_back<T, W, 1024, V, 1024>), grid, dim3(1024), 0, stream, p);
 }
 
 template <class T, class W>
 hipError_t backward(const NormParams& p, hipStream_t stream)
 {
-    if (p.dweight || p.dbias) {
-        hipLaunchKernelGGL((k_norm_weights<T, W>), dim3((unsigned)((p.N + 255) / 256)), dim3(256),
-                           0, stream, p);
-        const hipError_t e = hipGetLastError();
+    const bool sums = p.dweight || p.dbias;
+    const bool wide = p.N > MOST_HELD || p.x_cs != 1 || p.dy_cs != 1;
+    const int parts = norm_parts(p.M, p.N);
+    if (wide && sums)
+        hipLaunchKernelGGL(k_norm_back_wide_columns<T>, dim3((unsigned)((p.N + 255) / 256), parts),
+                           dim3(256), 0, stream, p);
+    else if (!wide && (p.y || sums)) {
+        if (p.N % 8 == 0)
+            backward_held<T, W, 8>(p, parts, stream);
+        else
+            backward_held<T, W, 1>(p, parts, stream);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (sums) {
+        hipLaunchKernelGGL(k_norm_columns<W>, dim3((unsigned)((2 * p.N + 63) / 64)), dim3(1024), 0,
+                           stream, p.part, parts, p.N, static_cast<W*>(p.dweight),
+                           static_cast<W*>(p.dbias));
+        e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (p.M > 0 && p.y)
-        hipLaunchKernelGGL((k_norm_dx<T, W>), dim3((unsigned)p.M), dim3(256), 0, stream, p);
+    if (wide && p.y && p.M > 0)
+        hipLaunchKernelGGL((k_norm_back_wide<T, W>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
     return hipGetLastError();
 }
 
 }  // namespace
+
+int norm_parts(int64_t M, int64_t N)
+{
+    const int rows = back_rows(N);
+    return (int)std::max<int64_t>(1, std::min<int64_t>((M + rows - 1) / rows,
+                                                       rows == 1 ? BACK_WGS : 2 * BACK_WGS));
+}
 
 hipError_t launch_norm(const NormParams& p, int dtype, int weight_dtype, hipStream_t stream)
 {
