@@ -312,6 +312,7 @@ size_t norm_bytes(const mag_norm_args* a)
 struct OrthPlan {
     int64_t m, n;       // sides of X, m <= n
     int64_t ld, lda;    // of g's rows and of A's and B's
+    int chunks;         // sums of squares of a matrix
     double* part;
     mag::f16* X[2];
     mag::f16* A;
@@ -325,7 +326,11 @@ size_t plan_orth(const mag_orthogonalize_args* a, void* ws, OrthPlan& pl)
     pl.ld = up8(a->g.cols);
     pl.lda = up8(pl.m);
     Carve c{static_cast<char*>(ws)};
-    pl.part = c.take<double>((size_t)(a->batch * mag::ORTH_CHUNKS * 8));
+    // (8,192 elements each, 1,024 in all the batch: a few rounds of the device)
+    const int64_t most = std::max<int64_t>(1, 1024 / std::max<int64_t>(a->batch, 1));
+    pl.chunks = (int)std::min<int64_t>(most, (a->g.rows * a->g.cols + 8191) / 8192);
+    pl.chunks = std::max(pl.chunks, 1);
+    pl.part = c.take<double>((size_t)(a->batch * pl.chunks * 8));
     for (auto& x : pl.X) x = c.take<mag::f16>((size_t)(a->batch * a->g.rows * pl.ld * 4));
     pl.A = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 4));
     pl.B = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 4));
@@ -661,6 +666,7 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
     o.cols = a->g.cols;
     o.eps = a->eps;
     o.part = pl.part;
+    o.chunks = pl.chunks;
     double sx = scale_for(most[0]);
     if (a->steps > 0) {
         o.scale = (float)sx;

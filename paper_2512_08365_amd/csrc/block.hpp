@@ -128,16 +128,16 @@ hipError_t launch_norm(const NormParams& p, int dtype, int weight_dtype, hipStre
 hipError_t launch_norm_backward(const NormParams& p, int dtype, int weight_dtype,
                                 hipStream_t stream);
 
-// `batch` updates of rows x cols: their norms (part: [batch][ORTH_CHUNKS]
-// sums of squares), and scale g / (|g| + eps) as two halves (planes) or, with
+// `batch` updates of rows x cols: their norms (part: [batch][chunks] sums of
+// squares), and scale g / (|g| + eps) as two halves (planes) or, with
 // out, as the result
-constexpr int ORTH_CHUNKS = 64;
 struct OrthParams {
     const void* g;
     int64_t g_batch, g_rs, g_cs;
     int64_t batch, rows, cols;
     double eps;
     double* part;
+    int32_t chunks;
     float scale;
     f16* z;
     int64_t z_ld, z_plane, z_batch;
@@ -148,6 +148,7 @@ hipError_t launch_orth_begin(const OrthParams& p, int dtype, hipStream_t stream)
 
 // the host's error record (api.hip)
 int set_error(int code, const char* msg);
+int device_cu_count();
 int set_hip_error(hipError_t e, const char* where);
 void clear_error();
 

@@ -57,14 +57,6 @@ __device__ __forceinline__ void put8(const float* v, short* dst, int64_t plane)
     *(h8*)dst = o;
 }
 
-// eight neighbours from column j on (zeros from column `cols` on)
-template <class T>
-__device__ __forceinline__ void get8(const T* p, int64_t cs, int64_t j, int64_t cols, float* v)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = j + i < cols ? (float)p[(j + i) * cs] : 0.0f;
-}
-
 // Bandwidth bound: each thread moves 8 neighbours of a row.
 template <class T>
 __global__ __launch_bounds__(256) void k_pack(PackParams p)

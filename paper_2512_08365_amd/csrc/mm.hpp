@@ -23,6 +23,19 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c)
                                                       __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// The same with the sums in accumulation registers, in place: left to itself the
+// compiler copies a large tile's sums from registers to registers in the loop.
+// It does not see what this writes and when: the sums are only read behind
+// settle(), and none is added to twice within four products.
+template <class T>
+__device__ __forceinline__ void mfma_in_place(s16x8 a, s16x8 b, f32x4& c)
+{
+    if constexpr (__is_same(T, bf16))
+        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    else
+        asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+
 // ------------------------------------------------------------------- operands
 // A tile of an operand is 64 steps of the reduction by ROWS rows of the output,
 // in LDS as 16-byte chunks of 8 elements, filled by loads that go from memory
@@ -32,11 +45,19 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c)
 //     chunk c of row r sits at c ^ (r & 7), so 8 rows' chunks of one k cover
 //     all banks.  Read as they are: 8 consecutive k of a row a lane.
 //   along rows (MC true): element at k * ld + row.  LDS row (one k) of ROWS / 8
-//     chunks; chunk c of step k sits at c ^ 2 (k & 3).  Read through the
+//     chunks; chunk c of step k sits at c ^ mc_swizzle(k).  Read through the
 //     transposing LDS load: 16 lanes hand in 4 steps of 16 rows and get 4
 //     consecutive k of a row each.
 constexpr int STEP = 64;                     // reduction per tile
 constexpr uint32_t NOWHERE = 0x80000000u;    // a buffer offset past every extent: reads zeros
+
+// what chunk c of step k is XORed with: 16 lanes read 4 steps' 32 bytes each, 32
+// lanes those of 8 steps further on too
+template <int ROWS>
+__device__ __forceinline__ int mc_swizzle(int k)
+{
+    return 2 * ((k & 3) | (ROWS >= 128 ? k >> 1 & 4 : 0));
+}
 
 template <int ROWS, bool MC, int THREADS>
 struct Tile {
@@ -45,74 +66,84 @@ struct Tile {
     static constexpr int CH = MC ? ROWS / 8 : 8;        // chunks an LDS row
 
     uint32_t off[LOADS];  // byte offset of the thread's chunks in a tile of the operand
-    int kk[LOADS];        // their first k
+    int first;            // k of the first one (along k: of all)
 
     // rows of the operand from this tile's first one on; ld in elements
-    __device__ void init(int64_t ld, int64_t rows_left)
+    __device__ __forceinline__ void init(int64_t ld, int64_t rows_left)
     {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int f = i * THREADS + (int)threadIdx.x;
             const int line = f / CH, pos = f % CH;
             if constexpr (MC) {
-                int c = pos ^ (2 * (line & 3));
+                int c = pos ^ mc_swizzle<ROWS>(line);
                 // (rows past the last one: any others, nothing of theirs is stored)
                 if ((int64_t)c * 8 >= rows_left) c = 0;
-                kk[i] = line;
+                if (i == 0) first = line;
                 off[i] = (uint32_t)(line * ld * 2 + c * 16);
             } else {
                 const int c = pos ^ (line & 7);
                 const int64_t r = line < rows_left ? line : rows_left - 1;
-                kk[i] = c * 8;
+                if (i == 0) first = c * 8;
                 off[i] = (uint32_t)(r * ld * 2 + c * 16);
             }
         }
     }
 
-    // base: the operand at this tile's first row and step's first k; k_left:
-    // steps of the reduction from there on
-    __device__ __forceinline__ void load(const char* base, int k_left, char* lds) const
+    // The thread's i-th chunk.  base: the operand at this tile's first row and
+    // the step's first k; k_left: of the reduction from there on (zeros behind).
+    // No branch: what a step costs beside its products is paid by every wave.
+    __device__ __forceinline__ void load(const char* base, int k_left, char* lds, int wave, int i) const
     {
         const __amdgpu_buffer_rsrc_t rs =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0x7fffffff, 0x00020000);
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-        if (k_left >= STEP) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    rs, (__attribute__((address_space(3))) void*)(lds + (i * THREADS + wave * 64) * 16),
-                    16, off[i], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    rs, (__attribute__((address_space(3))) void*)(lds + (i * THREADS + wave * 64) * 16),
-                    16, kk[i] < k_left ? off[i] : NOWHERE, 0, 0, 0);
-        }
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rs, (__attribute__((address_space(3))) void*)(lds + (i * THREADS + wave * 64) * 16), 16,
+            first + (MC ? i * (THREADS / CH) : 0) < k_left ? off[i] : NOWHERE, 0, 0, 0);
     }
 };
 
-// the 16 rows from `row`, 32 steps from 32 s: row lane % 16, k 8 (lane / 16) ..
+// Fragments of a wave's part of a tile: 16 rows, 32 k; row lane % 16, k 8 (lane /
+// 16) on.  What depends on the lane is worked out once, the rest is the load's
+// own constant offset.
 template <int ROWS, bool MC>
-__device__ __forceinline__ s16x8 fragment(const char* lds, int row, int s)
-{
-    const int lane = (int)threadIdx.x & 63;
-    if constexpr (MC) {
-        const int q = lane & 15;
-        const int k = s * 32 + (lane >> 4) * 8 + (q >> 2);
-        const int c = (row >> 3) + ((q & 3) >> 1);
-        const int at = ((c ^ (2 * (k & 3))) << 4) + ((q & 1) << 3);
-        const char* p = lds + k * (ROWS * 2) + at;  // (k + 4 has the same place in its row)
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(p + 4 * ROWS * 2));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
-        const int r = row + (lane & 15), c = s * 4 + (lane >> 4);
-        return *(const s16x8*)(lds + r * 128 + ((c ^ (r & 7)) << 4));
+struct Reader {
+    static constexpr int KEPT = MC ? (ROWS >= 256 ? 8 : ROWS >= 128 ? 4 : 2) : 2;
+    uint32_t at[KEPT];
+
+    __device__ __forceinline__ void init(int row)
+    {
+        const int lane = (int)threadIdx.x & 63, q = lane & 15;
+        if constexpr (MC) {
+            const int k = (lane >> 4) * 8 + (q >> 2);
+#pragma unroll
+            for (int i = 0; i < KEPT; ++i) {
+                const int c = (row >> 3) + 2 * i + ((q & 3) >> 1);
+                // (k + 4 and k + 32 have the same place in their rows)
+                at[i] = (uint32_t)(k * (ROWS * 2) + ((c ^ mc_swizzle<ROWS>(k)) << 4) + ((q & 1) << 3));
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                at[s] = (uint32_t)((row + q) * 128 + (((s * 4 + (lane >> 4)) ^ (q & 7)) << 4));
+        }
     }
-}
+
+    // rows 16 i on, half s of the step
+    __device__ __forceinline__ s16x8 get(const char* lds, int i, int s) const
+    {
+        if constexpr (MC) {
+            const char* p = lds + at[i % KEPT] + (i / KEPT * KEPT * 32 + s * 32 * ROWS * 2);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)p);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)(p + 4 * ROWS * 2));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            return *(const s16x8*)(lds + at[s] + i * 2048);
+        }
+    }
+};
 
 // ------------------------------------------------------------------ epilogues
 
@@ -144,6 +175,22 @@ __device__ __forceinline__ void fix(float* v, int e, float x)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i == e ? x : v[i];
+}
+
+// eight neighbours from column j on (zeros from column `cols` on); neighbours in
+// memory are loaded at once, whatever their alignment
+template <class T>
+__device__ __forceinline__ void get8(const T* p, int64_t cs, int64_t j, int64_t cols, float* v)
+{
+    if (cs == 1 && j + 8 <= cols) {
+        T t[8];
+        __builtin_memcpy(t, p + j, sizeof(t));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = j + i < cols ? (float)p[(j + i) * cs] : 0.0f;
+    }
 }
 
 // eight neighbours of a row, two bytes or four each
@@ -266,8 +313,8 @@ static __device__ __forceinline__ void store_orth(const Mm& p, int64_t bt, int64
 
 // ------------------------------------------------------------------ the kernel
 
-// Workgroup number -> tile: the XCDs (workgroups go round them) get runs of
-// neighbouring tiles, and a run walks bands of 8 tile rows, so that an XCD's
+// Tile number -> tile: the XCDs (workgroups go round them, 8 at a time) get runs
+// of neighbouring tiles, and a run walks bands of 8 tile rows, so that an XCD's
 // L2 holds the operands of what runs on it together.
 __device__ __forceinline__ void tile_of(uint32_t b, uint32_t count, uint32_t tr, uint32_t ts,
                                         uint32_t& ti, uint32_t& tj)
@@ -291,188 +338,250 @@ __device__ __forceinline__ void tile_above(uint32_t b, uint32_t& ti, uint32_t& t
     ti = b - tj * (tj + 1) / 2;
 }
 
-template <class T, class TO, int EPI, int BM, int BN, int WM, int WN, bool AMC, bool BMC>
-__global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_mm(Mm p)
+// Workgroups that the device holds at once, by tile.
+constexpr int wgs_per_cu(int side) { return side == 256 ? 1 : side == 128 ? 2 : 4; }
+
+// Workgroups (as many as fit) walk the tiles.  Four waves hold a quarter of a
+// tile's sums each.  Two steps' operands are in LDS; a step's 64 k are taken as
+// two halves, and the fragments of a half are read from LDS, a few at a time,
+// while the products of the half before it run, as are the loads of the step
+// after the next issued: one barrier a step, where everybody is done reading one
+// step and has the next.  The next tile's first steps are loaded before the
+// present one's sums are stored, through LDS of their own.
+template <class T, class TO, int EPI, int SIDE, bool AMC, bool BMC>
+__global__ __launch_bounds__(256, SIDE == 256 ? 1 : SIDE == 128 ? 2 : 4) void k_mm(Mm p)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int THREADS = WM * WN * 64;
-    constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-    using TA = Tile<BM, AMC, THREADS>;
-    using TB = Tile<BN, BMC, THREADS>;
+    constexpr int THREADS = 256, W = 2;          // 2 x 2 waves
+    constexpr int COLS = SIDE / W, F = COLS / 16;  // a wave's rows and columns, in 16s
+    constexpr bool IN_PLACE = F >= 8;
+    using TA = Tile<SIDE, AMC, THREADS>;
+    using TB = Tile<SIDE, BMC, THREADS>;
     // two tiles of each operand, as separate arrays: what one is read from is
     // not what is being filled
     __shared__ __attribute__((aligned(1024))) char la0[TA::BYTES], lb0[TB::BYTES];
     __shared__ __attribute__((aligned(1024))) char la1[TA::BYTES], lb1[TB::BYTES];
+    __shared__ __attribute__((aligned(1024))) char lo[4 * 16 * COLS * 4];
 
-    const uint32_t tr = (uint32_t)((p.R + BM - 1) / BM), ts = (uint32_t)((p.S + BN - 1) / BN);
-    uint32_t ti, tj;
-    if (EPI == MM_ORTH && p.symmetric)
-        tile_above(blockIdx.x, ti, tj);
-    else
-        tile_of(blockIdx.x, tr * ts, tr, ts, ti, tj);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int lane = (int)threadIdx.x & 63;
+    const int wr = wave / W * COLS, ws = wave % W * COLS;
+    const uint32_t tr = (uint32_t)((p.R + SIDE - 1) / SIDE), ts = (uint32_t)((p.S + SIDE - 1) / SIDE);
+    const uint32_t tiles = EPI == MM_ORTH && p.symmetric ? tr * (tr + 1) / 2 : tr * ts;
     const int64_t bt = blockIdx.z;
-    const int64_t r0 = (int64_t)ti * BM, s0 = (int64_t)tj * BN;
     // this workgroup's share of the steps: all products of parts, K each
     const int per_product = max(1, (int)((p.K + STEP - 1) / STEP));
     const int64_t steps = (int64_t)per_product * p.products;
     const int64_t t0 = steps * blockIdx.y / p.splits, t1 = steps * (blockIdx.y + 1) / p.splits;
+    const int count = (int)(t1 - t0);
+    const int64_t a_step = AMC ? STEP * p.a.ld * 2 : STEP * 2;
+    const int64_t b_step = BMC ? STEP * p.b.ld * 2 : STEP * 2;
 
     TA ta;
     TB tb;
-    ta.init(p.a.ld, p.R - r0);
-    tb.init(p.b.ld, p.S - s0);
-    const char* A = static_cast<const char*>(p.a.p) +
-                    2 * (bt * p.a.batch + (AMC ? r0 : r0 * p.a.ld));
-    const char* B = static_cast<const char*>(p.b.p) +
-                    2 * (bt * p.b.batch + (BMC ? s0 : s0 * p.b.ld));
-    const int64_t a_step = AMC ? STEP * p.a.ld * 2 : STEP * 2;
-    const int64_t b_step = BMC ? STEP * p.b.ld * 2 : STEP * 2;
-    int product = (int)(t0 / per_product), kstep = (int)(t0 % per_product);
-    const char *pa, *pb;
-    auto begin_product = [&] {
+    Reader<SIDE, AMC> ra;
+    Reader<SIDE, BMC> rb;
+    ra.init(wr);
+    rb.init(ws);
+    int64_t r0, s0;
+    bool mirror;
+    const char *A, *B, *pa, *pb;
+    int product, k_left, steps_left;
+    auto begin_product = [&](int kstep) {
         pa = A + 2 * (p.parts_a >> (4 * product) & 15) * p.a.plane + kstep * a_step;
         pb = B + 2 * (p.parts_b >> (4 * product) & 15) * p.b.plane + kstep * b_step;
+        k_left = (int)(p.K - (int64_t)kstep * STEP);
     };
-    begin_product();
-    const int k_last = (int)(p.K - (int64_t)(per_product - 1) * STEP);  // of a product's last step
-
+    auto advance = [&] {
+        pa += a_step;
+        pb += b_step;
+        k_left -= STEP;
+        --steps_left;
+        if (__builtin_expect(k_left <= 0, 0)) {
+            product = min(product + 1, p.products - 1);
+            begin_product(0);
+        }
+    };
     auto load = [&](char* la, char* lb) {
-        const bool last = kstep + 1 == per_product;
-        const int left = last ? k_last : STEP;
-        ta.load(pa, left, la);
-        tb.load(pb, left, lb);
-        if (last) {
-            kstep = 0;
-            ++product;
-            begin_product();
-        } else {
-            ++kstep;
-            pa += a_step;
-            pb += b_step;
-        }
+        const int have = steps_left > 0 ? k_left : 0;
+#pragma unroll
+        for (int i = 0; i < TA::LOADS; ++i) ta.load(pa, have, la, wave, i);
+#pragma unroll
+        for (int i = 0; i < TB::LOADS; ++i) tb.load(pb, have, lb, wave, i);
+        advance();
     };
-
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-    const int wr = wave / WN * (BM / WM), ws = wave % WN * (BN / WN);
-    f32x4 acc[FM][FN] = {};
-    auto multiply = [&](const char* la, const char* lb) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            // (the second half's fragments not before the first half is done
-            // with its own: registers)
-            if (s) __builtin_amdgcn_sched_barrier(0);
-            s16x8 fa[FM], fb[FN];
-#pragma unroll
-            for (int i = 0; i < FM; ++i) fa[i] = fragment<BM, AMC>(la, wr + i * 16, s);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) fb[j] = fragment<BN, BMC>(lb, ws + j * 16, s);
-            // (b first: a lane then holds four neighbours of one output row)
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mfma<T>(fb[j], fa[i], acc[i][j]);
-        }
-    };
-    auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-
-    // meet: what was loaded has arrived, and nobody reads the other tiles any more
-    const int count = (int)(t1 - t0);
-    if (count > 0) load(la0, lb0);
-    int step = 0;
-    for (; step + 1 < count; step += 2) {
-        meet();
+    auto begin_tile = [&](uint32_t g) {
+        uint32_t ti, tj;
+        if (EPI == MM_ORTH && p.symmetric)
+            tile_above(g, ti, tj);
+        else
+            tile_of(g, tiles, tr, ts, ti, tj);
+        mirror = EPI == MM_ORTH && p.symmetric && ti != tj;
+        r0 = (int64_t)ti * SIDE;
+        s0 = (int64_t)tj * SIDE;
+        ta.init(p.a.ld, p.R - r0);
+        tb.init(p.b.ld, p.S - s0);
+        A = static_cast<const char*>(p.a.p) + 2 * (bt * p.a.batch + (AMC ? r0 : r0 * p.a.ld));
+        B = static_cast<const char*>(p.b.p) + 2 * (bt * p.b.batch + (BMC ? s0 : s0 * p.b.ld));
+        product = (int)(t0 / per_product);
+        steps_left = count;
+        begin_product((int)(t0 % per_product));
+        load(la0, lb0);
         load(la1, lb1);
-        multiply(la0, lb0);
-        meet();
-        if (step + 2 < count) load(la0, lb0);
-        multiply(la1, lb1);
-    }
-    if (step < count) {
-        meet();
-        multiply(la0, lb0);
-    }
+    };
 
-    // The sums go through LDS, where the tiles were, a wave's own part of it at a
-    // time: 64 or 32 columns a row, in 16-byte chunks that sit at (chunk ^ row),
-    // and come back as 8 neighbours of a row a lane.
-    meet();
-    constexpr int COLS = BN / WN, CHUNKS = COLS / 4;
-    constexpr int WAVES = WM * WN, REGION = 2 * (TA::BYTES + TB::BYTES) / WAVES;
-    constexpr int PHASES = (FM * 16 * COLS * 4 + REGION - 1) / REGION, FI = FM / PHASES;
-    static_assert(TA::BYTES == TB::BYTES && WAVES % 4 == 0 && FM % PHASES == 0 &&
-                  FI * 16 * COLS * 4 <= REGION, "a wave's region lies within one array");
-    const int array = wave / (WAVES / 4);
-    char* mine = (array == 0 ? la0 : array == 1 ? lb0 : array == 2 ? la1 : lb1) +
-                 wave % (WAVES / 4) * REGION;
-    auto at = [&](int row, int chunk) { return mine + (row * CHUNKS + (chunk ^ (row & (CHUNKS - 1)))) * 16; };
-    const int lane = (int)threadIdx.x & 63;
-    const bool mirror = EPI == MM_ORTH && p.symmetric && ti != tj;
+    f32x4 acc[F][F];
+    s16x8 a0[F], b0[F], a1[F], b1[F];  // fragments of a step's halves
+    auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    auto product_of = [&](s16x8 a, s16x8 b, f32x4& c) {
+        // (b first: a lane then holds four neighbours of one output row)
+        if constexpr (IN_PLACE)
+            mfma_in_place<T>(b, a, c);
+        else
+            c = mfma<T>(b, a, c);
+    };
+    // what wrote the sums is done, whatever reads them comes later
+    auto settle = [&] {
+        if constexpr (IN_PLACE) {
+            auto hold = [&] {
 #pragma unroll
-    for (int ph = 0; ph < PHASES; ++ph) {
+                for (int i = 0; i < F; ++i)
 #pragma unroll
-        for (int i = 0; i < FI; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-                *(f32x4*)at(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[ph * FI + i][j];
-        const int64_t rp = r0 + wr + ph * FI * 16, sp = s0 + ws;
-        constexpr int LANES = COLS / 8;  // of a row
-#pragma unroll 1
-        for (int row = lane / LANES; row < FI * 16; row += 64 / LANES) {
-            const int64_t r = rp + row, s = sp + lane % LANES * 8;
-            float v[8];
-            *(f32x4*)v = *(const f32x4*)at(row, lane % LANES * 2);
-            *(f32x4*)(v + 4) = *(const f32x4*)at(row, lane % LANES * 2 + 1);
-            if (r >= p.R || s >= (EPI == MM_ORTH && p.o.z ? p.o.z_ld : p.S)) continue;
-            const int n = (int)max((int64_t)0, min((int64_t)8, p.S - s));
-            if constexpr (EPI == MM_PARTIAL) {
-                // (the rows of the partial sums are padded to 8)
-                float* q = p.partial + ((blockIdx.z * p.splits + blockIdx.y) * p.R + r) * p.partial_ld + s;
-                *(f32x4*)q = *(f32x4*)v;
-                *(f32x4*)(q + 4) = *(f32x4*)(v + 4);
-            } else if constexpr (EPI == MM_LINEAR) {
-                if constexpr (sizeof(TO) == 4)
-#pragma unroll 1
-                    for (int e = 0; e < n; ++e)
-                        if (!(fabsf(*(const float*)(at(row, lane % LANES * 2 + e / 4) + e % 4 * 4)) < __builtin_inff()))
-                            fix(v, e, whole_sum(p, bt, r, s + e));
-                store_linear<TO>(p.e, r, s, n, v);
-            } else {
-                store_orth(p, bt, r, s, n, v);
-            }
+                    for (int j = 0; j < F; ++j) asm volatile("" : "+a"(acc[i][j]));
+            };
+            asm volatile("s_nop 15\n\ts_nop 15");
+            hold();
         }
-        if (EPI == MM_ORTH && mirror) {
-            // the transpose: 8 neighbours of a column a lane
+    };
+    // a step in la, lb, whose first half is in a0, b0; the next one's is left there
+    auto step = [&](char* la, char* lb, char* na, char* nb) {
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            b1[i] = rb.get(lb, i, 1);
+            a1[i] = ra.get(la, i, 1);
+#pragma unroll
+            for (int j = 0; j < F; ++j) product_of(a0[i], b0[j], acc[i][j]);
+        }
+        meet();
+        const int have = steps_left > 0 ? k_left : 0;
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            b0[i] = rb.get(nb, i, 0);
+            a0[i] = ra.get(na, i, 0);
+#pragma unroll
+            for (int l = i * TA::LOADS / F; l < (i + 1) * TA::LOADS / F; ++l) {
+                ta.load(pa, have, la, wave, l);
+                tb.load(pb, have, lb, wave, l);
+            }
+#pragma unroll
+            for (int j = 0; j < F; ++j) product_of(a1[i], b1[j], acc[i][j]);
+        }
+        advance();
+    };
+
+    uint32_t g = blockIdx.x;
+    begin_tile(g);
+    while (true) {
+        meet();
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            b0[i] = rb.get(lb0, i, 0);
+            a0[i] = ra.get(la0, i, 0);
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        settle();
+        // (steps are taken two by two: behind the last one come zeros)
+        for (int t = 0; t < count; t += 2) {
+            step(la0, lb0, la1, lb1);
+            step(la1, lb1, la0, lb0);
+        }
+        meet();
+        settle();
+        const int64_t rt = r0 + wr, st = s0 + ws;
+        const bool mirrored = mirror;
+        g += gridDim.x;
+        if (g < tiles) begin_tile(g);
+
+        // The sums go to rows through a wave's own piece of LDS, 16 rows at a
+        // time in 16-byte chunks that sit at (chunk ^ row): 8 neighbours of a
+        // row a lane.
+        constexpr int CHUNKS = COLS / 4, LANES = COLS / 8;
+        char* mine = lo + wave * (16 * COLS * 4);
+        auto at = [&](int row, int chunk) {
+            return mine + (row * CHUNKS + (chunk ^ (row & (CHUNKS - 1)))) * 16;
+        };
 #pragma unroll 1
-            for (int i = lane; i < COLS * FI * 2; i += 64) {
-                const int c = i / (FI * 2), g = i % (FI * 2) * 8;
-                const int64_t r = sp + c, s = rp + g;
+        for (int ph = 0; ph < F; ++ph) {
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+                if (i == ph)
+#pragma unroll
+                    for (int j = 0; j < F; ++j)
+                        *(f32x4*)at(lane & 15, j * 4 + (lane >> 4)) = acc[i][j];
+            const int64_t rp = rt + ph * 16;
+#pragma unroll 2
+            for (int row = lane / LANES; row < 16; row += 64 / LANES) {
+                const int64_t r = rp + row, s = st + lane % LANES * 8;
                 float v[8];
+                *(f32x4*)v = *(const f32x4*)at(row, lane % LANES * 2);
+                *(f32x4*)(v + 4) = *(const f32x4*)at(row, lane % LANES * 2 + 1);
+                if (r >= p.R || s >= (EPI == MM_ORTH && p.o.z ? p.o.z_ld : p.S)) continue;
+                const int n = (int)max((int64_t)0, min((int64_t)8, p.S - s));
+                if constexpr (EPI == MM_PARTIAL) {
+                    // (the rows of the partial sums are padded to 8)
+                    float* q = p.partial + ((blockIdx.z * p.splits + blockIdx.y) * p.R + r) * p.partial_ld + s;
+                    *(f32x4*)q = *(f32x4*)v;
+                    *(f32x4*)(q + 4) = *(f32x4*)(v + 4);
+                } else if constexpr (EPI == MM_LINEAR) {
+                    if constexpr (sizeof(TO) == 4)
+#pragma unroll 1
+                        for (int e = 0; e < n; ++e)
+                            if (!(fabsf(*(const float*)(at(row, lane % LANES * 2 + e / 4) + e % 4 * 4)) < __builtin_inff()))
+                                fix(v, e, whole_sum(p, bt, r, s + e));
+                    store_linear<TO>(p.e, r, s, n, v);
+                } else {
+                    store_orth(p, bt, r, s, n, v);
+                }
+            }
+            if (EPI == MM_ORTH && mirrored) {
+                // the transpose: 8 neighbours of a column a lane
+#pragma unroll 1
+                for (int i = lane; i < COLS * 2; i += 64) {
+                    const int c = i / 2, e0 = i % 2 * 8;
+                    const int64_t r = st + c, s = rp + e0;
+                    float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = *(const float*)(at(g + e, c / 4) + c % 4 * 4);
-                if (r >= p.S || s >= p.R) continue;
-                store_orth(p, bt, r, s, (int)min((int64_t)8, p.R - s), v);
+                    for (int e = 0; e < 8; ++e) v[e] = *(const float*)(at(e0 + e, c / 4) + c % 4 * 4);
+                    if (r >= p.S || s >= p.R) continue;
+                    store_orth(p, bt, r, s, (int)min((int64_t)8, p.R - s), v);
+                }
             }
         }
+        if (g >= tiles) break;
     }
 #endif
 }
 
-template <class T, class TO, int EPI, int BM, int BN, int WM, int WN>
+template <class T, class TO, int EPI, int SIDE>
 hipError_t launch_mm_tile(const Mm& p, hipStream_t stream)
 {
-    const int64_t tr = (p.R + BM - 1) / BM, ts = (p.S + BN - 1) / BN;
+    const int64_t tr = (p.R + SIDE - 1) / SIDE, ts = (p.S + SIDE - 1) / SIDE;
     const int64_t tiles = p.symmetric ? tr * (tr + 1) / 2 : tr * ts;
     if (tiles > 0x7fffffffLL || p.batch > 65535) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)tiles, (unsigned)p.splits, (unsigned)p.batch), block(WM * WN * 64);
+    const int64_t fit = (int64_t)device_cu_count() * wgs_per_cu(SIDE);
+    const int64_t each = (fit + (int64_t)p.splits * p.batch - 1) / ((int64_t)p.splits * p.batch);
+    const dim3 grid((unsigned)(tiles < each ? tiles : each), (unsigned)p.splits, (unsigned)p.batch);
+    const dim3 block(256);
     if (p.a.mc)
         if (p.b.mc)
-            hipLaunchKernelGGL((k_mm<T, TO, EPI, BM, BN, WM, WN, true, true>), grid, block, 0, stream, p);
+            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, true, true>), grid, block, 0, stream, p);
         else
-            hipLaunchKernelGGL((k_mm<T, TO, EPI, BM, BN, WM, WN, true, false>), grid, block, 0, stream, p);
+            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, true, false>), grid, block, 0, stream, p);
     else if (p.b.mc)
-        hipLaunchKernelGGL((k_mm<T, TO, EPI, BM, BN, WM, WN, false, true>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, false, true>), grid, block, 0, stream, p);
     else
-        hipLaunchKernelGGL((k_mm<T, TO, EPI, BM, BN, WM, WN, false, false>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, false, false>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 

@@ -6,9 +6,9 @@ namespace mag {
 hipError_t launch_mm_bf16(const Mm& p, int tile, hipStream_t stream)
 {
     switch (tile) {
-    case TILE_256: return launch_mm_tile<bf16, bf16, MM_LINEAR, 256, 256, 2, 4>(p, stream);
-    case TILE_128: return launch_mm_tile<bf16, bf16, MM_LINEAR, 128, 128, 2, 2>(p, stream);
-    default: return launch_mm_tile<bf16, bf16, MM_LINEAR, 64, 64, 2, 2>(p, stream);
+    case TILE_256: return launch_mm_tile<bf16, bf16, MM_LINEAR, 256>(p, stream);
+    case TILE_128: return launch_mm_tile<bf16, bf16, MM_LINEAR, 128>(p, stream);
+    default: return launch_mm_tile<bf16, bf16, MM_LINEAR, 64>(p, stream);
     }
 }
 

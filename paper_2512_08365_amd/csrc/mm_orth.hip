@@ -6,9 +6,9 @@ namespace mag {
 hipError_t launch_mm_orth(const Mm& p, int tile, hipStream_t stream)
 {
     switch (tile) {
-    case TILE_256: return launch_mm_tile<f16, f16, MM_ORTH, 256, 256, 2, 4>(p, stream);
-    case TILE_128: return launch_mm_tile<f16, f16, MM_ORTH, 128, 128, 2, 2>(p, stream);
-    default: return launch_mm_tile<f16, f16, MM_ORTH, 64, 64, 2, 2>(p, stream);
+    case TILE_256: return launch_mm_tile<f16, f16, MM_ORTH, 256>(p, stream);
+    case TILE_128: return launch_mm_tile<f16, f16, MM_ORTH, 128>(p, stream);
+    default: return launch_mm_tile<f16, f16, MM_ORTH, 64>(p, stream);
     }
 }
 

@@ -7,15 +7,15 @@ hipError_t launch_mm_partial(const Mm& p, int type, int tile, hipStream_t stream
 {
     if (type == MAG_F16) {
         switch (tile) {
-        case TILE_256: return launch_mm_tile<f16, f16, MM_PARTIAL, 256, 256, 2, 4>(p, stream);
-        case TILE_128: return launch_mm_tile<f16, f16, MM_PARTIAL, 128, 128, 2, 2>(p, stream);
-        default: return launch_mm_tile<f16, f16, MM_PARTIAL, 64, 64, 2, 2>(p, stream);
+        case TILE_256: return launch_mm_tile<f16, f16, MM_PARTIAL, 256>(p, stream);
+        case TILE_128: return launch_mm_tile<f16, f16, MM_PARTIAL, 128>(p, stream);
+        default: return launch_mm_tile<f16, f16, MM_PARTIAL, 64>(p, stream);
         }
     }
     switch (tile) {
-    case TILE_256: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 256, 256, 2, 4>(p, stream);
-    case TILE_128: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 128, 128, 2, 2>(p, stream);
-    default: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 64, 64, 2, 2>(p, stream);
+    case TILE_256: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 256>(p, stream);
+    case TILE_128: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 128>(p, stream);
+    default: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 64>(p, stream);
     }
 }
 

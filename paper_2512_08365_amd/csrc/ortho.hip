@@ -7,7 +7,7 @@
 namespace mag {
 namespace {
 
-// sums of squares of one of ORTH_CHUNKS runs of rows of a matrix, in fp64 (the
+// sums of squares of one of a matrix's `chunks` runs of rows, in fp64 (the
 // squares of fp32 numbers pass its range)
 template <class T>
 __global__ __launch_bounds__(256) void k_orth_norm(OrthParams p)
@@ -15,18 +15,20 @@ __global__ __launch_bounds__(256) void k_orth_norm(OrthParams p)
     __shared__ double part[4];
     const int64_t bt = blockIdx.y;
     const T* g = static_cast<const T*>(p.g) + bt * p.g_batch;
-    const int64_t n = p.rows * p.cols;
-    const int64_t i0 = n * blockIdx.x / ORTH_CHUNKS, i1 = n * (blockIdx.x + 1) / ORTH_CHUNKS;
+    const int64_t per_row = (p.cols + 7) / 8, n = p.rows * per_row;
+    const int64_t i0 = n * blockIdx.x / p.chunks, i1 = n * (blockIdx.x + 1) / p.chunks;
     double s = 0.0;
     for (int64_t i = i0 + threadIdx.x; i < i1; i += 256) {
-        const double v = (double)(float)g[i / p.cols * p.g_rs + i % p.cols * p.g_cs];
-        s = fma(v, v, s);
+        float v[8];
+        get8(g + i / per_row * p.g_rs, p.g_cs, i % per_row * 8, p.cols, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fma((double)v[e], (double)v[e], s);
     }
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
     if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
     __syncthreads();
     if (threadIdx.x == 0)
-        p.part[bt * ORTH_CHUNKS + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+        p.part[bt * p.chunks + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 // scale g / (|g| + eps), 8 neighbours of a row a thread
@@ -35,7 +37,8 @@ __global__ __launch_bounds__(256) void k_orth_scale(OrthParams p)
 {
     typedef __attribute__((ext_vector_type(8))) f16 h8;
     const int64_t bt = blockIdx.y;
-    double s = p.part[bt * ORTH_CHUNKS + threadIdx.x % 64];
+    double s = 0.0;
+    for (int c = (int)threadIdx.x % 64; c < p.chunks; c += 64) s += p.part[bt * p.chunks + c];
     for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
     const double scale = (double)p.scale / (sqrt(s) + p.eps);
     const T* g = static_cast<const T*>(p.g) + bt * p.g_batch;
@@ -43,11 +46,12 @@ __global__ __launch_bounds__(256) void k_orth_scale(OrthParams p)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / per_row, j = i % per_row * 8;
         h8 hi, lo;
+        float x[8];
+        get8(g + r * p.g_rs, p.g_cs, j, p.cols, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             // (0 / 0 of a zero matrix without eps: NaN, as the formula says)
-            const float v = j + e < p.cols
-                ? (float)((double)(float)g[r * p.g_rs + (j + e) * p.g_cs] * scale) : 0.0f;
+            const float v = j + e < p.cols ? (float)((double)x[e] * scale) : 0.0f;
             f16 h, l;
             two_halves(v, h, l);
             hi[e] = h;
@@ -65,7 +69,7 @@ __global__ __launch_bounds__(256) void k_orth_scale(OrthParams p)
 template <class T>
 hipError_t begin(const OrthParams& p, hipStream_t stream)
 {
-    hipLaunchKernelGGL(k_orth_norm<T>, dim3(ORTH_CHUNKS, (unsigned)p.batch), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(k_orth_norm<T>, dim3((unsigned)p.chunks, (unsigned)p.batch), dim3(256), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t n = p.rows * ((p.cols + 7) / 8);
