@@ -5,38 +5,59 @@
 
 namespace mag {
 
-__device__ __forceinline__ float logistic(float z) { return 1.0f / (1.0f + __expf(-z)); }
+// (the hardware's reciprocal, off by one unit of the last place; 1 / inf = 0)
+__device__ __forceinline__ float logistic(float z)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+}
 
 constexpr float GELU_2K = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float GELU_C = 0.044715f;
 
-__device__ __forceinline__ float activation(float z, int act)
+// one activation or slope of N values: the kind is looked at once
+template <int N, class F>
+__device__ __forceinline__ void each(float* z, F f)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = f(z[i]);
+}
+
+template <int N>
+__device__ __forceinline__ void activate(float* z, int act)
 {
     switch (act) {
-    case MAG_ACT_RELU: return z > 0.0f ? z : (z != z ? z : 0.0f);
-    case MAG_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    case MAG_ACT_GELU_TANH: return z * logistic(GELU_2K * (z + GELU_C * z * z * z));
-    case MAG_ACT_SILU: return z * logistic(z);
-    default: return z;
+    case MAG_ACT_RELU: return each<N>(z, [](float v) { return v > 0.0f ? v : (v != v ? v : 0.0f); });
+    case MAG_ACT_GELU:
+        return each<N>(z, [](float v) { return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f)); });
+    case MAG_ACT_GELU_TANH:
+        return each<N>(z, [](float v) { return v * logistic(GELU_2K * (v + GELU_C * v * v * v)); });
+    case MAG_ACT_SILU: return each<N>(z, [](float v) { return v * logistic(v); });
+    default: return;
     }
 }
 
-__device__ __forceinline__ float slope(float z, int act)
+// z -> the activation's slope at z
+template <int N>
+__device__ __forceinline__ void slopes(float* z, int act)
 {
     switch (act) {
-    case MAG_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
+    case MAG_ACT_RELU: return each<N>(z, [](float v) { return v > 0.0f ? 1.0f : 0.0f; });
     case MAG_ACT_GELU:
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) +
-               z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-    case MAG_ACT_GELU_TANH: {
-        const float s = logistic(GELU_2K * (z + GELU_C * z * z * z));
-        return s + z * s * (1.0f - s) * GELU_2K * (1.0f + 3.0f * GELU_C * z * z);
-    }
-    case MAG_ACT_SILU: {
-        const float s = logistic(z);
-        return s + z * s * (1.0f - s);
-    }
-    default: return 1.0f;
+        return each<N>(z, [](float v) {
+            return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) +
+                   v * __expf(-0.5f * v * v) * 0.39894228040143268f;
+        });
+    case MAG_ACT_GELU_TANH:
+        return each<N>(z, [](float v) {
+            const float s = logistic(GELU_2K * (v + GELU_C * v * v * v));
+            return s + v * s * (1.0f - s) * GELU_2K * (1.0f + 3.0f * GELU_C * v * v);
+        });
+    case MAG_ACT_SILU:
+        return each<N>(z, [](float v) {
+            const float s = logistic(v);
+            return s + v * s * (1.0f - s);
+        });
+    default: return each<N>(z, [](float) { return 1.0f; });
     }
 }
 

@@ -89,8 +89,9 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
             if (p.act != MAG_ACT_NONE) {
                 float z[8];
                 get8(static_cast<const T*>(p.pre) + i * p.pre_rs, p.pre_cs, j, p.N, z);
+                slopes<8>(z, p.act);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] *= slope(z[e], p.act);
+                for (int e = 0; e < 8; ++e) d[e] *= z[e];
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += d[e];

@@ -237,9 +237,7 @@ __device__ __forceinline__ void store_linear(const Epilogue& e, int64_t r, int64
             for (int i = 0; i < 8; ++i) z[i] += b[i];
         }
         if (e.pre) store8(static_cast<T*>(e.pre) + r * e.pre_ld + s, z);
-        if (e.act != MAG_ACT_NONE)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = activation(z[i], e.act);
+        activate<8>(z, e.act);
         if (e.res) {
             load8(static_cast<const T*>(e.res) + r * e.res_rs + s, b);
 #pragma unroll
@@ -253,7 +251,7 @@ __device__ __forceinline__ void store_linear(const Epilogue& e, int64_t r, int64
             float v = z[i];
             if (e.bias) v += (float)static_cast<const T*>(e.bias)[s + i];
             if (e.pre) static_cast<T*>(e.pre)[r * e.pre_ld + s + i] = (T)v;
-            v = activation(v, e.act);
+            activate<1>(&v, e.act);
             if (e.res) v += (float)static_cast<const T*>(e.res)[r * e.res_rs + (s + i) * e.res_cs];
             static_cast<T*>(e.y)[r * e.y_ld + s + i] = (T)v;
         }
@@ -511,18 +509,69 @@ __global__ __launch_bounds__(256, SIDE == 256 ? 1 : SIDE == 128 ? 2 : 4) void k_
         auto at = [&](int row, int chunk) {
             return mine + (row * CHUNKS + (chunk ^ (row & (CHUNKS - 1)))) * 16;
         };
+        const int64_t s8 = st + lane % LANES * 8;
+        // a tile that lies inside the output, whole vectors: what a row needs of
+        // memory is asked for before its sums come back from LDS
+        bool inside = false;
+        float bias[8] = {};
+        if constexpr (EPI == MM_LINEAR) {
+            inside = p.e.vec && rt + COLS <= p.R && st + COLS <= p.S;
+            if (inside && p.e.bias) load8(static_cast<const TO*>(p.e.bias) + s8, bias);
+        }
 #pragma unroll 1
         for (int ph = 0; ph < F; ++ph) {
+            constexpr int PASSES = 16 * LANES / 64;
+            const int64_t r8 = rt + ph * 16 + lane / LANES;
+            float res[EPI == MM_LINEAR ? PASSES : 1][8];
+            if constexpr (EPI == MM_LINEAR)
+                if (inside && p.e.res)
+#pragma unroll
+                    for (int q = 0; q < PASSES; ++q)
+                        load8(static_cast<const TO*>(p.e.res) + (r8 + q * (64 / LANES)) * p.e.res_rs + s8, res[q]);
 #pragma unroll
             for (int i = 0; i < F; ++i)
                 if (i == ph)
 #pragma unroll
                     for (int j = 0; j < F; ++j)
                         *(f32x4*)at(lane & 15, j * 4 + (lane >> 4)) = acc[i][j];
+            if constexpr (EPI == MM_LINEAR)
+                if (inside) {
+                    float v[PASSES][8];
+#pragma unroll
+                    for (int q = 0; q < PASSES; ++q) {
+                        const int row = lane / LANES + q * (64 / LANES);
+                        *(f32x4*)v[q] = *(const f32x4*)at(row, lane % LANES * 2);
+                        *(f32x4*)(v[q] + 4) = *(const f32x4*)at(row, lane % LANES * 2 + 1);
+                    }
+#pragma unroll
+                    for (int q = 0; q < PASSES; ++q) {
+                        const int64_t r = r8 + q * (64 / LANES);
+                        if constexpr (sizeof(TO) == 4)
+#pragma unroll 1
+                            for (int e = 0; e < 8; ++e) {
+                                float x = 0.0f;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) x = i == e ? v[q][i] : x;
+                                if (!(fabsf(x) < __builtin_inff())) fix(v[q], e, whole_sum(p, bt, r, s8 + e));
+                            }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[q][e] += bias[e];
+                        if (p.e.pre) store8(static_cast<TO*>(p.e.pre) + r * p.e.pre_ld + s8, v[q]);
+                    }
+                    activate<8 * PASSES>(v[0], p.e.act);
+#pragma unroll
+                    for (int q = 0; q < PASSES; ++q) {
+                        if (p.e.res)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[q][e] += res[q][e];
+                        store8(static_cast<TO*>(p.e.y) + (r8 + q * (64 / LANES)) * p.e.y_ld + s8, v[q]);
+                    }
+                    continue;
+                }
             const int64_t rp = rt + ph * 16;
-#pragma unroll 2
+#pragma unroll 1
             for (int row = lane / LANES; row < 16; row += 64 / LANES) {
-                const int64_t r = rp + row, s = st + lane % LANES * 8;
+                const int64_t r = rp + row, s = s8;
                 float v[8];
                 *(f32x4*)v = *(const f32x4*)at(row, lane % LANES * 2);
                 *(f32x4*)(v + 4) = *(const f32x4*)at(row, lane % LANES * 2 + 1);
