@@ -748,7 +748,7 @@ int mag_stream_push_host(mag_stream* handle, const double* t_host, const float* 
 /* Largest extent of a matrix, and of the two that are a layer's features (in,
    out, the sides of an update). */
 #define MAG_MAX_EXTENT (1LL << 30)
-#define MAG_MAX_FEATURES (1LL << 22)
+#define MAG_MAX_FEATURES (1LL << 21)
 
 /* A matrix on the device.  Element (i, j) is data[i * row_stride + j *
    col_stride].  Inputs may have any strides >= 0 (0: one row or column read

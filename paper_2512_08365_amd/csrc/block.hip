@@ -95,7 +95,8 @@ bool same_shape(const mag_matrix& m, int64_t rows, int64_t cols)
 
 constexpr int64_t MOST_LD = 1LL << 22;  // 256 rows of it stay within 31 bits of bytes
 int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
-int parts(int dtype) { return dtype == MAG_F32 ? 3 : 1; }
+// elements of an operand's packed row of n
+int64_t packed_ld(int64_t n, int dtype) { return dtype == MAG_F32 ? (n + 31) / 32 * 96 : up8(n); }
 
 // How a product reads a matrix: where it lies, or as rows packed into the
 // workspace (fp32, which is cut into parts, and strides, alignments and widths
@@ -123,10 +124,9 @@ Operand operand(const mag_matrix& m, int dtype, bool along)
         }
     }
     o.packed = true;
-    o.op.ld = up8(m.cols);
-    o.op.plane = m.rows * o.op.ld;
+    o.op.ld = packed_ld(m.cols, dtype);
     o.op.mc = !along;
-    o.bytes = (size_t)(o.op.plane * 2 * parts(dtype));
+    o.bytes = (size_t)(m.rows * o.op.ld * 2);
     return o;
 }
 
@@ -140,18 +140,8 @@ int pack(const Operand& o, const mag_matrix& m, int dtype, hipStream_t stream)
     p.cols = m.cols;
     p.dst = const_cast<void*>(o.op.p);
     p.ld = o.op.ld;
-    p.plane = o.op.plane;
     TRY_HIP(mag::launch_pack(p, dtype, stream), "pack launch");
     return MAG_OK;
-}
-
-// the products of parts that fp32 operands take, smallest first: (0,2) (2,0)
-// (1,1) (0,1) (1,0) (0,0); of halves: (0,1) (1,0) (0,0)
-void set_products(mag::Mm& p, int n)
-{
-    p.products = n;
-    p.parts_a = n == 6 ? 0x010120 : n == 3 ? 0x010 : 0;
-    p.parts_b = n == 6 ? 0x001102 : n == 3 ? 0x001 : 0;
 }
 
 // Tile and splits of R x S x K.
@@ -160,25 +150,31 @@ struct Shape {
     int splits;
 };
 
-Shape choose(int64_t R, int64_t S, int64_t K, int products, int64_t batch, bool may_split)
+// kind: MM_BF16 ...
+Shape choose(int64_t R, int64_t S, int64_t K, int kind, int64_t batch, bool symmetric)
 {
     auto tiles = [&](int t) {
-        const int64_t side = mag::TILE_SIDE[t];
-        return (R + side - 1) / side * ((S + side - 1) / side) * batch;
+        const int64_t side = mag::TILE_SIDE[t], tr = (R + side - 1) / side;
+        return std::max<int64_t>(1, (symmetric ? tr * (tr + 1) / 2 : tr * ((S + side - 1) / side)) * batch);
     };
-    const int64_t steps = std::max<int64_t>(1, (K + 63) / 64) * products;
-    if (tiles(mag::TILE_256) >= 224) return {mag::TILE_256, 1};
+    const int64_t step = kind == mag::MM_F32 || kind == mag::MM_HALVES ? 32 : 64;
+    const int64_t steps = std::max<int64_t>(1, (K + step - 1) / step);
+    if (kind != mag::MM_F32 && tiles(mag::TILE_256) >= 224) return {mag::TILE_256, 1};
     if (tiles(mag::TILE_128) >= 224) return {mag::TILE_128, 1};
-    const int64_t n = std::max<int64_t>(1, tiles(mag::TILE_64));
-    if (!may_split || n >= 256) return {mag::TILE_64, 1};
+    const int64_t n = tiles(mag::TILE_64);
+    if (n >= 256) return {mag::TILE_64, 1};
     return {mag::TILE_64, (int)std::max<int64_t>(1, std::min<int64_t>({512 / n, steps / 4, 64}))};
+}
+
+int kind_of(int dtype)
+{
+    return dtype == MAG_F32 ? mag::MM_F32 : dtype == MAG_F16 ? mag::MM_F16 : mag::MM_BF16;
 }
 
 int launch_linear(const mag::Mm& p, int dtype, int tile, hipStream_t stream)
 {
     if (p.splits > 1) {
-        TRY_HIP(mag::launch_mm_partial(p, dtype == MAG_F16 ? MAG_F16 : MAG_BF16, tile, stream),
-                "product launch");
+        TRY_HIP(mag::launch_mm_partial(p, kind_of(dtype), tile, stream), "product launch");
         TRY_HIP(mag::launch_mm_join(p, dtype, stream), "join launch");
         return MAG_OK;
     }
@@ -189,9 +185,20 @@ int launch_linear(const mag::Mm& p, int dtype, int tile, hipStream_t stream)
     return MAG_OK;
 }
 
-size_t partial_bytes(int64_t R, int64_t S, const Shape& s)
+int launch_orth(const mag::Mm& p, int tile, hipStream_t stream)
 {
-    return s.splits > 1 ? (size_t)(s.splits * R * up8(S) * 4) : 0;
+    if (p.splits > 1) {
+        TRY_HIP(mag::launch_mm_partial(p, mag::MM_HALVES, tile, stream), "product launch");
+        TRY_HIP(mag::launch_orth_join(p, stream), "join launch");
+        return MAG_OK;
+    }
+    TRY_HIP(mag::launch_mm_orth(p, tile, stream), "product launch");
+    return MAG_OK;
+}
+
+size_t partial_bytes(int64_t R, int64_t S, const Shape& s, int64_t batch = 1)
+{
+    return s.splits > 1 ? (size_t)(batch * s.splits * R * up8(S) * 4) : 0;
 }
 
 // whether the rows of a matrix start at multiples of 16 bytes
@@ -225,8 +232,7 @@ size_t plan_linear(const mag_linear_args* a, void* ws, LinearPlan& pl)
 {
     pl.x = operand(a->x, a->dtype, true);
     pl.w = operand(a->weight, a->dtype, true);
-    const int products = a->dtype == MAG_F32 ? 6 : 1;
-    pl.shape = choose(a->x.rows, a->weight.rows, a->x.cols, products, 1, true);
+    pl.shape = choose(a->x.rows, a->weight.rows, a->x.cols, kind_of(a->dtype), 1, false);
     Carve c{static_cast<char*>(ws)};
     for (Operand* o : {&pl.x, &pl.w})
         if (o->packed) o->op.p = c.take(o->bytes);
@@ -248,7 +254,7 @@ struct BackwardPlan {
 size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& pl)
 {
     const int64_t M = a->x.rows, N = a->weight.rows, K = a->x.cols;
-    const int products = a->dtype == MAG_F32 ? 6 : 1;
+    const int kind = kind_of(a->dtype);
     // x and weight are both read across the reduction of the product they enter
     pl.x = operand(a->x, a->dtype, false);
     pl.w = operand(a->weight, a->dtype, false);
@@ -257,17 +263,16 @@ size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& 
     pl.own_dz = a->activation != MAG_ACT_NONE || pl.dy.packed || !a->dy.data;
     if (pl.own_dz) {
         pl.dz = mag::MmOperand{};
-        pl.dz.ld = up8(N);
-        pl.dz.plane = M * pl.dz.ld;
+        pl.dz.ld = packed_ld(N, a->dtype);
     } else {
         pl.dz = pl.dy.op;
     }
-    pl.dx = choose(M, K, N, products, 1, true);
-    pl.dw = choose(N, K, M, products, 1, true);
+    pl.dx = choose(M, K, N, kind, 1, false);
+    pl.dw = choose(N, K, M, kind, 1, false);
     Carve c{static_cast<char*>(ws)};
     for (Operand* o : {&pl.x, &pl.w})
         if (o->packed) o->op.p = c.take(o->bytes);
-    void* dz = c.take((size_t)(M * up8(N) * 2 * parts(a->dtype)));
+    void* dz = c.take((size_t)(M * packed_ld(N, a->dtype) * 2));
     if (pl.own_dz) pl.dz.p = dz;
     pl.column_part = c.take<float>((size_t)(mag::slope_chunks(M, N) * N * 4));
     pl.partial = c.take<float>(std::max(partial_bytes(M, K, pl.dx), partial_bytes(N, K, pl.dw)));
@@ -311,7 +316,9 @@ size_t norm_bytes(const mag_norm_args* a)
 // g's orientation is kept: X is g or its transpose, read either way
 struct OrthPlan {
     int64_t m, n;       // sides of X, m <= n
-    int64_t ld, lda;    // of g's rows and of A's and B's
+    int64_t ld, lda;    // of g's rows and of A's and B's, two parts each
+    Shape gram, square, whole;  // of A = X X^T, A A and B X
+    float* partial;
     int chunks;         // sums of squares of a matrix
     double* part;
     mag::f16* X[2];
@@ -323,17 +330,23 @@ size_t plan_orth(const mag_orthogonalize_args* a, void* ws, OrthPlan& pl)
 {
     pl.m = std::min(a->g.rows, a->g.cols);
     pl.n = std::max(a->g.rows, a->g.cols);
-    pl.ld = up8(a->g.cols);
-    pl.lda = up8(pl.m);
+    pl.ld = (a->g.cols + 31) / 32 * 64;
+    pl.lda = (pl.m + 31) / 32 * 64;
+    pl.gram = choose(pl.m, pl.m, pl.n, mag::MM_HALVES, a->batch, true);
+    pl.square = choose(pl.m, pl.m, pl.m, mag::MM_HALVES, a->batch, true);
+    pl.whole = choose(a->g.rows, a->g.cols, pl.m, mag::MM_HALVES, a->batch, false);
     Carve c{static_cast<char*>(ws)};
     // (8,192 elements each, 1,024 in all the batch: a few rounds of the device)
     const int64_t most = std::max<int64_t>(1, 1024 / std::max<int64_t>(a->batch, 1));
     pl.chunks = (int)std::min<int64_t>(most, (a->g.rows * a->g.cols + 8191) / 8192);
     pl.chunks = std::max(pl.chunks, 1);
     pl.part = c.take<double>((size_t)(a->batch * pl.chunks * 8));
-    for (auto& x : pl.X) x = c.take<mag::f16>((size_t)(a->batch * a->g.rows * pl.ld * 4));
-    pl.A = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 4));
-    pl.B = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 4));
+    for (auto& x : pl.X) x = c.take<mag::f16>((size_t)(a->batch * a->g.rows * pl.ld * 2));
+    pl.A = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 2));
+    pl.B = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 2));
+    pl.partial = c.take<float>(std::max({partial_bytes(pl.m, pl.m, pl.gram, a->batch),
+                                         partial_bytes(pl.m, pl.m, pl.square, a->batch),
+                                         partial_bytes(a->g.rows, a->g.cols, pl.whole, a->batch)}));
     return c.off;
 }
 
@@ -417,7 +430,6 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     p.S = N;
     p.K = K;
     p.batch = 1;
-    set_products(p, a->dtype == MAG_F32 ? 6 : 1);
     p.splits = pl.shape.splits;
     p.partial = pl.partial;
     p.partial_ld = up8(N);
@@ -491,14 +503,12 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         s.act = a->activation;
         s.dz = pl.own_dz && (a->dx.data || a->dweight.data) ? const_cast<void*>(pl.dz.p) : nullptr;
         s.ldz = pl.dz.ld;
-        s.plane = pl.dz.plane;
         s.dbias = a->dbias;
         s.part = pl.column_part;
         TRY_HIP(mag::launch_slope(s, a->dtype, stream), "linear_backward launch");
     }
     mag::Mm p{};
     p.batch = 1;
-    set_products(p, a->dtype == MAG_F32 ? 6 : 1);
     p.partial = pl.partial;
     p.S = K;
     p.partial_ld = up8(K);
@@ -651,8 +661,8 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
     plan_orth(a, workspace, pl);
     const bool tall = a->g.rows > a->g.cols;
     const int64_t m = pl.m, n = pl.n;
-    const int64_t x_batch = a->g.rows * pl.ld, x_plane = a->batch * x_batch;
-    const int64_t a_batch = m * pl.lda, a_plane = a->batch * a_batch;
+    const int64_t x_batch = a->g.rows * pl.ld;
+    const int64_t a_batch = m * pl.lda;
     // halves hold a value times a power of two that takes its bound near 2^15
     auto scale_for = [](double bound) { return ldexp(1.0, 15 - ilogb(bound) - 1); };
 
@@ -672,7 +682,6 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         o.scale = (float)sx;
         o.z = pl.X[0];
         o.z_ld = pl.ld;
-        o.z_plane = x_plane;
         o.z_batch = x_batch;
     } else {
         o.scale = 1.0f;
@@ -681,21 +690,20 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         o.out_batch = a->out_batch_stride;
     }
     TRY_HIP(mag::launch_orth_begin(o, a->dtype, stream), "orthogonalize launch");
-    const Shape side = choose(m, m, n, 3, a->batch, false);
-    const Shape whole = choose(a->g.rows, a->g.cols, m, 3, a->batch, false);
     for (int i = 0; i < a->steps; ++i) {
         const double u2 = most[i] * most[i];
         const double sa = scale_for(1.01 * u2);
         const double sb = scale_for(1.01 * (fabs(a->b) * u2 + fabs(a->c) * u2 * u2) + 0x1p-100);
         const double next = scale_for(most[i + 1] + 0x1p-100);
-        const mag::MmOperand X{pl.X[i & 1], pl.ld, x_plane, x_batch, 0};
-        const mag::MmOperand A{pl.A, pl.lda, a_plane, a_batch, 0};
-        const mag::MmOperand B{pl.B, pl.lda, a_plane, a_batch, 0};
+        const mag::MmOperand X{pl.X[i & 1], pl.ld, x_batch, 0};
+        const mag::MmOperand A{pl.A, pl.lda, a_batch, 0};
+        const mag::MmOperand B{pl.B, pl.lda, a_batch, 0};
         // A = X X^T
         mag::Mm p{};
         p.batch = (int)a->batch;
-        p.splits = 1;
-        set_products(p, 3);
+        p.partial = pl.partial;
+        p.partial_ld = up8(m);
+        p.splits = pl.gram.splits;
         p.a = p.b = X;
         p.a.mc = p.b.mc = tall;
         p.R = p.S = m;
@@ -704,9 +712,8 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         p.o.scale = (float)(sa / (sx * sx));
         p.o.z = pl.A;
         p.o.z_ld = pl.lda;
-        p.o.z_plane = a_plane;
         p.o.z_batch = a_batch;
-        TRY_HIP(mag::launch_mm_orth(p, side.tile, stream), "orthogonalize launch");
+        TRY(launch_orth(p, pl.gram.tile, stream));
         // B = b A + c A A
         p.a = p.b = A;
         p.K = m;
@@ -714,10 +721,10 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         p.o.mix = (float)(a->b * sb / sa);
         p.o.m = pl.A;
         p.o.m_ld = pl.lda;
-        p.o.m_plane = a_plane;
         p.o.m_batch = a_batch;
         p.o.z = pl.B;
-        TRY_HIP(mag::launch_mm_orth(p, side.tile, stream), "orthogonalize launch");
+        p.splits = pl.square.splits;
+        TRY(launch_orth(p, pl.square.tile, stream));
         // X <- a X + B X, or its transpose <- a X^T + X^T B (B symmetric)
         p.symmetric = 0;
         p.a = tall ? X : B;
@@ -731,17 +738,17 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         p.o.mix = (float)(a->a * out / sx);
         p.o.m = pl.X[i & 1];
         p.o.m_ld = pl.ld;
-        p.o.m_plane = x_plane;
         p.o.m_batch = x_batch;
         p.o.z = last ? nullptr : pl.X[(i + 1) & 1];
         p.o.z_ld = pl.ld;
-        p.o.z_plane = x_plane;
         p.o.z_batch = x_batch;
         p.o.out = a->out.data;
         p.o.out_ld = a->out.row_stride;
         p.o.out_batch = a->out_batch_stride;
         p.o.dtype = a->dtype;
-        TRY_HIP(mag::launch_mm_orth(p, whole.tile, stream), "orthogonalize launch");
+        p.splits = pl.whole.splits;
+        p.partial_ld = up8(a->g.cols);
+        TRY(launch_orth(p, pl.whole.tile, stream));
         sx = next;
     }
     return MAG_OK;

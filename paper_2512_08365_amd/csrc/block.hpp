@@ -16,12 +16,12 @@ using f16 = _Float16;
 
 // An operand of a product: element (row, k) at row * ld + k, or with mc at k *
 // ld + row (elements of two bytes; data and rows at multiples of 16 bytes, and
-// the run that is contiguous zero-padded to, or a multiple of, 8).  An fp32
-// operand is three such planes (bfloat16 parts), an update's two.
+// the run that is contiguous a multiple of 8 or zero-padded to one).  In P = 2 or
+// 3 parts, that run has 32 elements' first parts, then their second ones, and so
+// on, zero-padded to whole 32s, and ld counts all of them.
 struct MmOperand {
     const void* p;
     int64_t ld;
-    int64_t plane;  // elements from one part to the next
     int64_t batch;  // elements from one matrix of a batch to the next
     int32_t mc;
 };
@@ -39,26 +39,23 @@ struct Epilogue {
     int32_t vec;          // 16 bytes of a row can be moved at once everywhere
 };
 
-// z = scale sum + mix M, as two halves (planes) or, for the result, one number
+// z = scale sum + mix M, as two halves or, for the result, one number
 struct OrthStore {
     float scale, mix;
-    const f16* m;         // or NULL: its planes
-    int64_t m_ld, m_plane, m_batch;
-    f16* z;               // the planes, or NULL
-    int64_t z_ld, z_plane, z_batch;
+    const f16* m;         // or NULL: two parts, as an operand's
+    int64_t m_ld, m_batch;
+    f16* z;               // two parts, as an operand's, or NULL
+    int64_t z_ld, z_batch;
     void* out;            // the result (z NULL)
     int64_t out_ld, out_batch;
     int32_t dtype;        // of out
 };
 
-// out[r][s] = sum over k of a(r, k) b(s, k); with several parts an operand, the
-// sum over `products` pairs of parts (part i of the pairs: nibble i)
+// out[r][s] = sum over k of a(r, k) b(s, k)
 struct Mm {
     MmOperand a, b;
     int64_t R, S, K;
     int32_t batch;
-    int32_t products;
-    uint32_t parts_a, parts_b;
     int32_t splits;       // of the reduction, each with its own sums in `partial`
     int32_t symmetric;    // tiles on and above the diagonal only, mirrored (R = S)
     float* partial;       // [batch][splits][R][partial_ld]
@@ -69,28 +66,32 @@ struct Mm {
 enum { MM_LINEAR, MM_PARTIAL, MM_ORTH };
 enum { TILE_64, TILE_128, TILE_256, TILES };
 constexpr int64_t TILE_SIDE[TILES] = {64, 128, 256};
-// type: of the operands' elements (MAG_BF16 or MAG_F16); tile: TILE_*
-hipError_t launch_mm_bf16(const Mm& p, int tile, hipStream_t stream);  // y bfloat16
-hipError_t launch_mm_f16(const Mm& p, int tile, hipStream_t stream);   // y half
-hipError_t launch_mm_f32(const Mm& p, int tile, hipStream_t stream);   // three parts, y float
-hipError_t launch_mm_partial(const Mm& p, int type, int tile, hipStream_t stream);
+// what a product is made of: operands and result of bfloat16 or half; fp32
+// operands in three bfloat16 parts; an update's in two half parts
+enum { MM_BF16, MM_F16, MM_F32, MM_HALVES };
+// tile: TILE_*
+hipError_t launch_mm_bf16(const Mm& p, int tile, hipStream_t stream);
+hipError_t launch_mm_f16(const Mm& p, int tile, hipStream_t stream);
+hipError_t launch_mm_f32(const Mm& p, int tile, hipStream_t stream);   // (no 256 tile)
+// kind: MM_BF16 ... (no 256 tile)
+hipError_t launch_mm_partial(const Mm& p, int kind, int tile, hipStream_t stream);
 hipError_t launch_mm_orth(const Mm& p, int tile, hipStream_t stream);
-// the partial sums of a split product added up and stored
+// the partial sums of a split product added up and stored (dtype: of y)
 hipError_t launch_mm_join(const Mm& p, int dtype, hipStream_t stream);
+hipError_t launch_orth_join(const Mm& p, hipStream_t stream);
 
-// rows x cols values of any strides as rows of ld elements (a multiple of 8,
-// zeros after the last column): two-byte types as they are, fp32 as three
-// bfloat16 planes
+// rows x cols values of any strides as an operand's rows of ld elements: two-byte
+// types as they are, fp32 in three bfloat16 parts
 struct PackParams {
     const void* src;
     int64_t rs, cs;
     int64_t rows, cols;
     void* dst;
-    int64_t ld, plane;
+    int64_t ld;
 };
 hipError_t launch_pack(const PackParams& p, int dtype, hipStream_t stream);
 
-// dz = dy act'(pre) (T, row stride ldz), and dbias = the column sums of dz
+// dz = dy act'(pre), and dbias = the column sums of dz
 struct SlopeParams {
     const void* dy;
     int64_t dy_rs, dy_cs;
@@ -98,8 +99,8 @@ struct SlopeParams {
     int64_t pre_rs, pre_cs;
     int64_t M, N;
     int32_t act;
-    void* dz;        // NULL: not wanted; fp32: three bfloat16 planes
-    int64_t ldz, plane;
+    void* dz;        // NULL: not wanted; an operand's rows (fp32: three parts)
+    int64_t ldz;
     void* dbias;     // NULL: not wanted
     float* part;     // [slope_chunks(M)][N] column sums of the chunks of rows
 };
@@ -129,8 +130,8 @@ hipError_t launch_norm_backward(const NormParams& p, int dtype, int weight_dtype
                                 hipStream_t stream);
 
 // `batch` updates of rows x cols: their norms (part: [batch][chunks] sums of
-// squares), and scale g / (|g| + eps) as two halves (planes) or, with
-// out, as the result
+// squares), and scale g / (|g| + eps) as an operand of two halves or, with out,
+// as the result
 struct OrthParams {
     const void* g;
     int64_t g_batch, g_rs, g_cs;
@@ -140,7 +141,7 @@ struct OrthParams {
     int32_t chunks;
     float scale;
     f16* z;
-    int64_t z_ld, z_plane, z_batch;
+    int64_t z_ld, z_batch;
     void* out;
     int64_t out_ld, out_batch;
 };

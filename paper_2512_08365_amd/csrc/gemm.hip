@@ -33,9 +33,9 @@ __device__ __forceinline__ void three_parts(float v, short& a, short& b, short& 
     c = bits((bf16)(r - (float)m));
 }
 
-// eight neighbours of a row into dst (fp32: three planes)
+// eight neighbours of a row, from element j of it, into an operand's row
 template <class T>
-__device__ __forceinline__ void put8(const float* v, short* dst, int64_t plane)
+__device__ __forceinline__ void put8(const float* v, short* row, int64_t j)
 {
     h8 o;
     if constexpr (sizeof(T) == 4) {
@@ -48,25 +48,34 @@ __device__ __forceinline__ void put8(const float* v, short* dst, int64_t plane)
             m[i] = b;
             l[i] = c;
         }
-        *(h8*)(dst + plane) = m;
-        *(h8*)(dst + 2 * plane) = l;
+        short* d = row + place<3>(j);
+        *(h8*)d = o;
+        *(h8*)(d + 32) = m;
+        *(h8*)(d + 64) = l;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = __builtin_bit_cast(short, (T)v[i]);
+        *(h8*)(row + j) = o;
     }
-    *(h8*)dst = o;
+}
+
+// elements of an operand's row of n, without the parts
+template <class T>
+__host__ __device__ int64_t width_of(int64_t n)
+{
+    return sizeof(T) == 4 ? (n + 31) / 32 * 32 : (n + 7) / 8 * 8;
 }
 
 // Bandwidth bound: each thread moves 8 neighbours of a row.
 template <class T>
 __global__ __launch_bounds__(256) void k_pack(PackParams p)
 {
-    const int64_t per_row = p.ld / 8, n = p.rows * per_row;
+    const int64_t per_row = width_of<T>(p.cols) / 8, n = p.rows * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / per_row, j = i % per_row * 8;
         float v[8];
         get8(static_cast<const T*>(p.src) + r * p.rs, p.cs, j, p.cols, v);
-        put8<T>(v, static_cast<short*>(p.dst) + r * p.ld + j, p.plane);
+        put8<T>(v, static_cast<short*>(p.dst) + r * p.ld, j);
     }
 }
 
@@ -82,7 +91,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
     const int64_t j = (int64_t)blockIdx.x * SLOPE_COLS + lane * 8;
     const int64_t i0 = (int64_t)blockIdx.y * chunk, i1 = min(i0 + chunk, p.M);
     float sum[8] = {};
-    if (j < p.N)
+    if (j < width_of<T>(p.N))
         for (int64_t i = i0 + wave; i < i1; i += 4) {
             float d[8];
             get8(static_cast<const T*>(p.dy) + i * p.dy_rs, p.dy_cs, j, p.N, d);
@@ -95,7 +104,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += d[e];
-            if (p.dz) put8<T>(d, static_cast<short*>(p.dz) + i * p.ldz + j, p.plane);
+            if (p.dz) put8<T>(d, static_cast<short*>(p.dz) + i * p.ldz, j);
         }
     if (!p.dbias) return;
 #pragma unroll
@@ -155,7 +164,7 @@ unsigned blocks_for(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 
 
 hipError_t launch_pack(const PackParams& p, int dtype, hipStream_t stream)
 {
-    const int64_t n = p.rows * (p.ld / 8);
+    const int64_t n = p.rows * ((p.cols + 7) / 8);
     if (n == 0) return hipSuccess;
     const dim3 grid(blocks_for(n)), block(256);
     if (dtype == MAG_F32)

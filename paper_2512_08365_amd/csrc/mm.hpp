@@ -1,6 +1,8 @@
 // mm.hpp -- the matrix-core tile product of the feed-forward block's operators.
 #pragma once
 
+#include <type_traits>
+
 #include "activation.hpp"
 #include "block.hpp"
 
@@ -37,36 +39,55 @@ __device__ __forceinline__ void mfma_in_place(s16x8 a, s16x8 b, f32x4& c)
 }
 
 // ------------------------------------------------------------------- operands
-// A tile of an operand is 64 steps of the reduction by ROWS rows of the output,
-// in LDS as 16-byte chunks of 8 elements, filled by loads that go from memory
-// to LDS without registers.  Such a load writes 64 chunks one after another, so
-// a permutation against bank conflicts is made in what each lane reads.
-//   along k (MC false): element (row, k) at row * ld + k.  LDS row of 8 chunks;
-//     chunk c of row r sits at c ^ (r & 7), so 8 rows' chunks of one k cover
-//     all banks.  Read as they are: 8 consecutive k of a row a lane.
-//   along rows (MC true): element at k * ld + row.  LDS row (one k) of ROWS / 8
-//     chunks; chunk c of step k sits at c ^ mc_swizzle(k).  Read through the
-//     transposing LDS load: 16 lanes hand in 4 steps of 16 rows and get 4
-//     consecutive k of a row each.
-constexpr int STEP = 64;                     // reduction per tile
+// A tile of an operand is a step of the reduction (64 k; of operands in P = 2 or
+// 3 parts, which lie 32 k of each part after another in memory, 32) by ROWS rows
+// of the output, in LDS as 16-byte chunks of 8 elements, filled by loads that go
+// from memory to LDS without registers.  Such a load writes 64 chunks one after
+// another, so a permutation against bank conflicts is made in what each lane
+// reads.
+//   along k (MC false): element (row, k) at row * ld + k.  An LDS row has the 8 or
+//     12 chunks of a row; chunk c of row r sits at c ^ (r & 7), of 12 at c ^
+//     (r / 2 & 3), so that 8 rows' chunks of one k cover all banks.  Read as they
+//     are: 8 consecutive k of a row a lane.
+//   along rows (MC true): element at k * ld + row.  An LDS row is one k; chunk c
+//     of it sits at c ^ mc_swizzle(k).  Read through the transposing LDS load: 16
+//     lanes hand in 4 steps of 16 rows and get 4 consecutive k of a row each.
 constexpr uint32_t NOWHERE = 0x80000000u;    // a buffer offset past every extent: reads zeros
 
+constexpr int step_of(int P) { return P == 1 ? 64 : 32; }
+
 // what chunk c of step k is XORed with: 16 lanes read 4 steps' 32 bytes each, 32
-// lanes those of 8 steps further on too
-template <int ROWS>
+// lanes those of 8 steps further on too (CH: chunks of an LDS row)
+template <int CH>
 __device__ __forceinline__ int mc_swizzle(int k)
 {
-    return 2 * ((k & 3) | (ROWS >= 128 ? k >> 1 & 4 : 0));
+    return 2 * ((k & 3) | (CH % 16 == 0 ? k >> 1 & 4 : 0));
 }
 
-template <int ROWS, bool MC, int THREADS>
+template <int ROWS, bool MC, int P, int THREADS>
 struct Tile {
-    static constexpr int BYTES = ROWS * STEP * 2;
-    static constexpr int LOADS = BYTES / 16 / THREADS;  // chunks a thread
-    static constexpr int CH = MC ? ROWS / 8 : 8;        // chunks an LDS row
+    static constexpr int STEP = step_of(P);
+    static constexpr int BYTES = ROWS * STEP * P * 2;
+    static constexpr int LOADS = BYTES / 16 / THREADS;        // chunks a thread
+    static constexpr int CH = (MC ? ROWS : STEP) * P / 8;     // chunks an LDS row
+
+    // whether the thread's chunks lie alike in their lines
+    static constexpr bool ALIKE = THREADS % CH == 0;
 
     uint32_t off[LOADS];  // byte offset of the thread's chunks in a tile of the operand
-    int first;            // k of the first one (along k: of all)
+    int k0[ALIKE ? 1 : LOADS];  // their first k (of the first chunk, if alike)
+
+    // the first k of the thread's i-th chunk
+    static __device__ __forceinline__ int first(int i)
+    {
+        const int f = i * THREADS + (int)threadIdx.x, line = f / CH;
+        return MC ? line : source(line, f % CH) * 8 % STEP;
+    }
+    // the chunk that lies at `pos` of a line
+    static __device__ __forceinline__ int source(int line, int pos)
+    {
+        return pos ^ (MC ? mc_swizzle<CH>(line) : P == 3 ? line >> 1 & 3 : line & 7);
+    }
 
     // rows of the operand from this tile's first one on; ld in elements
     __device__ __forceinline__ void init(int64_t ld, int64_t rows_left)
@@ -74,20 +95,23 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int f = i * THREADS + (int)threadIdx.x;
-            const int line = f / CH, pos = f % CH;
+            const int line = f / CH;
+            int c = source(line, f % CH);
+            if (i < (ALIKE ? 1 : LOADS)) k0[i] = first(i);
+            // (rows past the last one: any others, nothing of theirs is stored)
             if constexpr (MC) {
-                int c = pos ^ mc_swizzle<ROWS>(line);
-                // (rows past the last one: any others, nothing of theirs is stored)
-                if ((int64_t)c * 8 >= rows_left) c = 0;
-                if (i == 0) first = line;
+                if ((int64_t)c * 8 >= padded(rows_left)) c = 0;
                 off[i] = (uint32_t)(line * ld * 2 + c * 16);
             } else {
-                const int c = pos ^ (line & 7);
                 const int64_t r = line < rows_left ? line : rows_left - 1;
-                if (i == 0) first = c * 8;
                 off[i] = (uint32_t)(r * ld * 2 + c * 16);
             }
         }
+    }
+    // elements that n rows take in a line
+    static __device__ __forceinline__ int64_t padded(int64_t n)
+    {
+        return P == 1 ? n : (n + 31) / 32 * (32 * P);
     }
 
     // The thread's i-th chunk.  base: the operand at this tile's first row and
@@ -99,58 +123,82 @@ struct Tile {
             __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0x7fffffff, 0x00020000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
             rs, (__attribute__((address_space(3))) void*)(lds + (i * THREADS + wave * 64) * 16), 16,
-            first + (MC ? i * (THREADS / CH) : 0) < k_left ? off[i] : NOWHERE, 0, 0, 0);
+            (ALIKE ? k0[0] < k_left - (MC ? i * (THREADS / CH) : 0) : k0[i] < k_left) ? off[i] : NOWHERE, 0, 0, 0);
     }
 };
 
 // Fragments of a wave's part of a tile: 16 rows, 32 k; row lane % 16, k 8 (lane /
 // 16) on.  What depends on the lane is worked out once, the rest is the load's
 // own constant offset.
-template <int ROWS, bool MC>
+template <int ROWS, bool MC, int P>
 struct Reader {
-    static constexpr int KEPT = MC ? (ROWS >= 256 ? 8 : ROWS >= 128 ? 4 : 2) : 2;
-    uint32_t at[KEPT];
+    static constexpr int LINE = (MC ? ROWS : step_of(P)) * P * 2;  // bytes of an LDS row
+    // along rows: what repeats from 16 rows to 16 rows (the swizzle XORs up to 16
+    // chunks: 128 rows, or 32 P-part ones a 64-byte part)
+    static constexpr int CYCLE = P == 1 ? 8 : P == 2 ? 4 : 8;
+    static constexpr int KEPT_I = ROWS / 32 < CYCLE ? ROWS / 32 : CYCLE;
+    static constexpr int KEPT = MC ? KEPT_I * (P == 1 ? 1 : P) : P == 3 ? 1 : 2;
+    int at[KEPT];
+
+    // The compiler takes the places for new: it would otherwise work the address
+    // of every read that lies too far on for a constant offset out before the
+    // loop, and hold a register for each.
+    __device__ __forceinline__ void renew()
+    {
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) asm volatile("" : "+v"(at[i]));
+    }
 
     __device__ __forceinline__ void init(int row)
     {
         const int lane = (int)threadIdx.x & 63, q = lane & 15;
         if constexpr (MC) {
-            const int k = (lane >> 4) * 8 + (q >> 2);
+            const int k = (lane >> 4) * 8 + (q >> 2), b = (q & 3) >> 1;
 #pragma unroll
-            for (int i = 0; i < KEPT; ++i) {
-                const int c = (row >> 3) + 2 * i + ((q & 3) >> 1);
-                // (k + 4 and k + 32 have the same place in their rows)
-                at[i] = (uint32_t)(k * (ROWS * 2) + ((c ^ mc_swizzle<ROWS>(k)) << 4) + ((q & 1) << 3));
-            }
+            for (int i = 0; i < KEPT_I; ++i)
+#pragma unroll
+                for (int s = 0; s < (P == 1 ? 1 : P); ++s) {
+                    const int n = row + 16 * i;
+                    const int c = (P == 1 ? n / 8 : n / 32 * (4 * P) + s * 4 + n % 32 / 8) + b;
+                    // (k + 4 and, of one part, k + 32 have the same place in their rows)
+                    at[i * (P == 1 ? 1 : P) + s] =
+                        k * LINE + ((c ^ mc_swizzle<LINE / 16>(k)) << 4) + ((q & 1) << 3);
+                }
+        } else if constexpr (P == 3) {
+            at[0] = (row + q) * LINE + (((lane >> 4) ^ (q >> 1 & 3)) << 4);
         } else {
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-                at[s] = (uint32_t)((row + q) * 128 + (((s * 4 + (lane >> 4)) ^ (q & 7)) << 4));
+                at[s] = (row + q) * LINE + (((s * 4 + (lane >> 4)) ^ (q & 7)) << 4);
         }
     }
 
-    // rows 16 i on, half s of the step
+    // rows 16 i on; s: half of a step, or part
     __device__ __forceinline__ s16x8 get(const char* lds, int i, int s) const
     {
         if constexpr (MC) {
-            const char* p = lds + at[i % KEPT] + (i / KEPT * KEPT * 32 + s * 32 * ROWS * 2);
+            const char* p = lds + at[i % KEPT_I * (P == 1 ? 1 : P) + (P == 1 ? 0 : s)] +
+                            (i / KEPT_I * KEPT_I * 32 * P + (P == 1 ? s * 32 * LINE : 0));
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                 (__attribute__((address_space(3))) s16x4*)p);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) s16x4*)(p + 4 * ROWS * 2));
+                (__attribute__((address_space(3))) s16x4*)(p + 4 * LINE));
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else if constexpr (P == 3) {
+            return *(const s16x8*)(lds + at[0] + i * 16 * LINE + s * 64);
         } else {
-            return *(const s16x8*)(lds + at[s] + i * 2048);
+            return *(const s16x8*)(lds + at[s] + i * 16 * LINE);
         }
     }
 };
 
 // ------------------------------------------------------------------ epilogues
 
-template <class T>
-__device__ __forceinline__ float part_sum(const T* h, int64_t plane, int64_t i)
+// element j of a row of P parts: the place of its first part (the next ones follow 32 on)
+template <int P>
+__device__ __forceinline__ int64_t place(int64_t j)
 {
-    return (float)h[i] + ((float)h[i + plane] + (float)h[i + 2 * plane]);
+    return P == 1 ? j : j / 32 * (32 * P) + j % 32;
 }
 
 // A sum of products of three-part fp32 operands that is not finite, taken again
@@ -160,14 +208,14 @@ __device__ __forceinline__ float part_sum(const T* h, int64_t plane, int64_t i)
 // exactly; an infinite or NaN one is its first part.
 __device__ __forceinline__ float whole_sum(const Mm& p, int64_t bt, int64_t r, int64_t s)
 {
-    const bf16* A = static_cast<const bf16*>(p.a.p) + bt * p.a.batch;
-    const bf16* B = static_cast<const bf16*>(p.b.p) + bt * p.b.batch;
-    const int64_t as = p.a.mc ? p.a.ld : 1, bs = p.b.mc ? p.b.ld : 1;
-    int64_t a = p.a.mc ? r : r * p.a.ld, b = p.b.mc ? s : s * p.b.ld;
+    auto value = [](const MmOperand& o, int64_t bt, int64_t row, int64_t k) {
+        const bf16* h = static_cast<const bf16*>(o.p) + bt * o.batch +
+                        (o.mc ? k * o.ld + place<3>(row) : row * o.ld + place<3>(k));
+        return (float)h[0] + ((float)h[32] + (float)h[64]);
+    };
     float sum = 0.0f;
 #pragma unroll 1
-    for (int64_t k = 0; k < p.K; ++k, a += as, b += bs)
-        sum = fmaf(part_sum(A, p.a.plane, a), part_sum(B, p.b.plane, b), sum);
+    for (int64_t k = 0; k < p.K; ++k) sum = fmaf(value(p.a, bt, r, k), value(p.b, bt, s, k), sum);
     return sum;
 }
 
@@ -266,7 +314,7 @@ __device__ __forceinline__ void two_halves(float v, f16& hi, f16& lo)
 }
 
 // z = scale v + mix m for n <= 8 neighbours of a row (the rest of an
-// iteration's planes' padding: zeros)
+// iteration's padding: zeros)
 static __device__ __forceinline__ void store_orth(const Mm& p, int64_t bt, int64_t r, int64_t s,
                                                   int n, const float* sum)
 {
@@ -275,10 +323,10 @@ static __device__ __forceinline__ void store_orth(const Mm& p, int64_t bt, int64
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = o.scale * sum[i];
     if (o.m) {
-        const f16* m = o.m + bt * o.m_batch + r * o.m_ld + s;
+        const f16* m = o.m + bt * o.m_batch + r * o.m_ld + place<2>(s);
         float hi[8], lo[8];
         load8(m, hi);
-        load8(m + o.m_plane, lo);
+        load8(m + 32, lo);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(o.mix, hi[i] + lo[i], v[i]);
     }
@@ -291,9 +339,9 @@ static __device__ __forceinline__ void store_orth(const Mm& p, int64_t bt, int64
             hi[i] = __builtin_bit_cast(short, h);
             lo[i] = __builtin_bit_cast(short, l);
         }
-        f16* z = o.z + bt * o.z_batch + r * o.z_ld + s;
+        f16* z = o.z + bt * o.z_batch + r * o.z_ld + place<2>(s);
         *(s16x8*)z = hi;
-        *(s16x8*)(z + o.z_plane) = lo;
+        *(s16x8*)(z + 32) = lo;
     } else {
         const int64_t at = bt * o.out_batch + r * o.out_ld + s;
 #pragma unroll
@@ -336,81 +384,81 @@ __device__ __forceinline__ void tile_above(uint32_t b, uint32_t& ti, uint32_t& t
     ti = b - tj * (tj + 1) / 2;
 }
 
-// Workgroups that the device holds at once, by tile.
-constexpr int wgs_per_cu(int side) { return side == 256 ? 1 : side == 128 ? 2 : 4; }
+// Tiles of operands in LDS at a time, and workgroups that a CU holds: a large tile
+// hides the way from memory behind one step's products, a small one needs more
+// steps ahead.
+constexpr int stages_of(int side, int P) { return side == 64 && P < 3 ? 4 : 2; }
+constexpr int wgs_per_cu(int side, int P) { return side == 256 ? 1 : side == 128 && P == 3 ? 1 : 2; }
 
 // Workgroups (as many as fit) walk the tiles.  Four waves hold a quarter of a
-// tile's sums each.  Two steps' operands are in LDS; a step's 64 k are taken as
-// two halves, and the fragments of a half are read from LDS, a few at a time,
-// while the products of the half before it run, as are the loads of the step
-// after the next issued: one barrier a step, where everybody is done reading one
-// step and has the next.  The next tile's first steps are loaded before the
-// present one's sums are stored, through LDS of their own.
-template <class T, class TO, int EPI, int SIDE, bool AMC, bool BMC>
-__global__ __launch_bounds__(256, SIDE == 256 ? 1 : SIDE == 128 ? 2 : 4) void k_mm(Mm p)
+// tile's sums each.  Fragments are read from LDS a few at a time while the
+// products of the ones before run, and the loads of the step that takes the
+// present one's place in LDS are issued between products too: one barrier a
+// step, where everybody is done reading one step and has the next.  The next
+// tile's first steps are loaded before the present one's sums are stored,
+// through LDS of their own.
+//   one part:    the halves of a step, 0 0 | 1 1
+//   two parts:   high high | low high | high low
+//   three parts: 1 1 | 1 2, 2 1, 2 2 | 3 1, 1 3 (the products below 2^-24 left out)
+template <class T, class TO, int EPI, int SIDE, int P, bool AMC, bool BMC>
+__global__ __launch_bounds__(256, wgs_per_cu(SIDE, P)) void k_mm(Mm p)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int THREADS = 256, W = 2;          // 2 x 2 waves
     constexpr int COLS = SIDE / W, F = COLS / 16;  // a wave's rows and columns, in 16s
+    constexpr int STAGES = stages_of(SIDE, P), STEP = step_of(P);
     constexpr bool IN_PLACE = F >= 8;
-    using TA = Tile<SIDE, AMC, THREADS>;
-    using TB = Tile<SIDE, BMC, THREADS>;
-    // two tiles of each operand, as separate arrays: what one is read from is
-    // not what is being filled
+    using TA = Tile<SIDE, AMC, P, THREADS>;
+    using TB = Tile<SIDE, BMC, P, THREADS>;
+    constexpr int L = TA::LOADS;
+    static_assert(TA::LOADS == TB::LOADS, "");
+    // each tile an array of its own: what one is read from is not what is being
+    // filled
     __shared__ __attribute__((aligned(1024))) char la0[TA::BYTES], lb0[TB::BYTES];
     __shared__ __attribute__((aligned(1024))) char la1[TA::BYTES], lb1[TB::BYTES];
+    __shared__ __attribute__((aligned(1024))) char la2[STAGES > 2 ? TA::BYTES : 16], lb2[STAGES > 2 ? TB::BYTES : 16];
+    __shared__ __attribute__((aligned(1024))) char la3[STAGES > 2 ? TA::BYTES : 16], lb3[STAGES > 2 ? TB::BYTES : 16];
     __shared__ __attribute__((aligned(1024))) char lo[4 * 16 * COLS * 4];
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const int lane = (int)threadIdx.x & 63;
     const int wr = wave / W * COLS, ws = wave % W * COLS;
     const uint32_t tr = (uint32_t)((p.R + SIDE - 1) / SIDE), ts = (uint32_t)((p.S + SIDE - 1) / SIDE);
-    const uint32_t tiles = EPI == MM_ORTH && p.symmetric ? tr * (tr + 1) / 2 : tr * ts;
+    const uint32_t tiles = EPI != MM_LINEAR && p.symmetric ? tr * (tr + 1) / 2 : tr * ts;
     const int64_t bt = blockIdx.z;
-    // this workgroup's share of the steps: all products of parts, K each
-    const int per_product = max(1, (int)((p.K + STEP - 1) / STEP));
-    const int64_t steps = (int64_t)per_product * p.products;
+    // this workgroup's share of the steps
+    const int64_t steps = (p.K + STEP - 1) / STEP;
     const int64_t t0 = steps * blockIdx.y / p.splits, t1 = steps * (blockIdx.y + 1) / p.splits;
     const int count = (int)(t1 - t0);
-    const int64_t a_step = AMC ? STEP * p.a.ld * 2 : STEP * 2;
-    const int64_t b_step = BMC ? STEP * p.b.ld * 2 : STEP * 2;
+    const int64_t a_step = AMC ? STEP * p.a.ld * 2 : STEP * P * 2;
+    const int64_t b_step = BMC ? STEP * p.b.ld * 2 : STEP * P * 2;
 
     TA ta;
     TB tb;
-    Reader<SIDE, AMC> ra;
-    Reader<SIDE, BMC> rb;
+    Reader<SIDE, AMC, P> ra;
+    Reader<SIDE, BMC, P> rb;
     ra.init(wr);
     rb.init(ws);
     int64_t r0, s0;
     bool mirror;
-    const char *A, *B, *pa, *pb;
-    int product, k_left, steps_left;
-    auto begin_product = [&](int kstep) {
-        pa = A + 2 * (p.parts_a >> (4 * product) & 15) * p.a.plane + kstep * a_step;
-        pb = B + 2 * (p.parts_b >> (4 * product) & 15) * p.b.plane + kstep * b_step;
-        k_left = (int)(p.K - (int64_t)kstep * STEP);
-    };
+    const char *pa, *pb;
+    int k_left;  // none behind this workgroup's last step
     auto advance = [&] {
         pa += a_step;
         pb += b_step;
         k_left -= STEP;
-        --steps_left;
-        if (__builtin_expect(k_left <= 0, 0)) {
-            product = min(product + 1, p.products - 1);
-            begin_product(0);
-        }
     };
     auto load = [&](char* la, char* lb) {
-        const int have = steps_left > 0 ? k_left : 0;
 #pragma unroll
-        for (int i = 0; i < TA::LOADS; ++i) ta.load(pa, have, la, wave, i);
-#pragma unroll
-        for (int i = 0; i < TB::LOADS; ++i) tb.load(pb, have, lb, wave, i);
+        for (int i = 0; i < L; ++i) {
+            ta.load(pa, k_left, la, wave, i);
+            tb.load(pb, k_left, lb, wave, i);
+        }
         advance();
     };
     auto begin_tile = [&](uint32_t g) {
         uint32_t ti, tj;
-        if (EPI == MM_ORTH && p.symmetric)
+        if (EPI != MM_LINEAR && p.symmetric)
             tile_above(g, ti, tj);
         else
             tile_of(g, tiles, tr, ts, ti, tj);
@@ -419,84 +467,145 @@ __global__ __launch_bounds__(256, SIDE == 256 ? 1 : SIDE == 128 ? 2 : 4) void k_
         s0 = (int64_t)tj * SIDE;
         ta.init(p.a.ld, p.R - r0);
         tb.init(p.b.ld, p.S - s0);
-        A = static_cast<const char*>(p.a.p) + 2 * (bt * p.a.batch + (AMC ? r0 : r0 * p.a.ld));
-        B = static_cast<const char*>(p.b.p) + 2 * (bt * p.b.batch + (BMC ? s0 : s0 * p.b.ld));
-        product = (int)(t0 / per_product);
-        steps_left = count;
-        begin_product((int)(t0 % per_product));
+        pa = static_cast<const char*>(p.a.p) + 2 * (bt * p.a.batch + (AMC ? r0 * P : r0 * p.a.ld)) + t0 * a_step;
+        pb = static_cast<const char*>(p.b.p) + 2 * (bt * p.b.batch + (BMC ? s0 * P : s0 * p.b.ld)) + t0 * b_step;
+        k_left = (int)(min(p.K, t1 * STEP) - t0 * STEP);
         load(la0, lb0);
         load(la1, lb1);
+        if constexpr (STAGES > 2) {
+            load(la2, lb2);
+            load(la3, lb3);
+        }
     };
 
     f32x4 acc[F][F];
-    s16x8 a0[F], b0[F], a1[F], b1[F];  // fragments of a step's halves
-    auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    auto product_of = [&](s16x8 a, s16x8 b, f32x4& c) {
-        // (b first: a lane then holds four neighbours of one output row)
-        if constexpr (IN_PLACE)
-            mfma_in_place<T>(b, a, c);
-        else
-            c = mfma<T>(b, a, c);
+    // everybody is done with what was read before, and has all but the last
+    // `ahead` steps that were loaded
+    auto meet = [](auto ahead) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(ahead)::value * 2 * L) : "memory");
+    };
+    using None = std::integral_constant<int, 0>;
+    using Ahead = std::integral_constant<int, STAGES - 2>;
+    auto products = [&](const s16x8& a, const s16x8* b, int i) {
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+            // (b first: a lane then holds four neighbours of one output row)
+            if constexpr (IN_PLACE)
+                mfma_in_place<T>(b[j], a, acc[i][j]);
+            else
+                acc[i][j] = mfma<T>(b[j], a, acc[i][j]);
+        }
     };
     // what wrote the sums is done, whatever reads them comes later
     auto settle = [&] {
         if constexpr (IN_PLACE) {
-            auto hold = [&] {
-#pragma unroll
-                for (int i = 0; i < F; ++i)
-#pragma unroll
-                    for (int j = 0; j < F; ++j) asm volatile("" : "+a"(acc[i][j]));
-            };
             asm volatile("s_nop 15\n\ts_nop 15");
-            hold();
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int j = 0; j < F; ++j) asm volatile("" : "+a"(acc[i][j]));
         }
     };
-    // a step in la, lb, whose first half is in a0, b0; the next one's is left there
-    auto step = [&](char* la, char* lb, char* na, char* nb) {
+    // A step in la, lb, whose first fragments are in xa, xb; the next one's are left
+    // in za, with `xb` or `zb` (one part: za, zb are read first, and the next ones
+    // go where the present ones were).
+    s16x8 xa[F], xb[F], za[F], zb[F], ya[P == 3 ? F : 1], yb[P == 3 ? F : 1];
+    auto begin_next = [&](const char* na, const char* nb, char* la, char* lb, s16x8* fa, s16x8* fb,
+                          int i) __attribute__((always_inline)) {
+        fb[i] = rb.get(nb, i, 0);
+        fa[i] = ra.get(na, i, 0);
 #pragma unroll
-        for (int i = 0; i < F; ++i) {
-            b1[i] = rb.get(lb, i, 1);
-            a1[i] = ra.get(la, i, 1);
-#pragma unroll
-            for (int j = 0; j < F; ++j) product_of(a0[i], b0[j], acc[i][j]);
+        for (int l = i * L / F; l < (i + 1) * L / F; ++l) {
+            ta.load(pa, k_left, la, wave, l);
+            tb.load(pb, k_left, lb, wave, l);
         }
-        meet();
-        const int have = steps_left > 0 ? k_left : 0;
+    };
+    auto step = [&](char* la, char* lb, const char* na, const char* nb, s16x8* pxa, s16x8* pxb,
+                    s16x8* pza, s16x8* pzb) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < F; ++i) {
-            b0[i] = rb.get(nb, i, 0);
-            a0[i] = ra.get(na, i, 0);
+            pzb[i] = rb.get(lb, i, 1);
+            pza[i] = ra.get(la, i, 1);
+            products(pxa[i], pxb, i);
+        }
+        if constexpr (P == 1) {
+            meet(Ahead{});
 #pragma unroll
-            for (int l = i * TA::LOADS / F; l < (i + 1) * TA::LOADS / F; ++l) {
-                ta.load(pa, have, la, wave, l);
-                tb.load(pb, have, lb, wave, l);
+            for (int i = 0; i < F; ++i) {
+                begin_next(na, nb, la, lb, pxa, pxb, i);
+                products(pza[i], pzb, i);
             }
+        } else if constexpr (P == 2) {
 #pragma unroll
-            for (int j = 0; j < F; ++j) product_of(a1[i], b1[j], acc[i][j]);
+            for (int i = 0; i < F; ++i) products(pza[i], pxb, i);
+            meet(Ahead{});
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                begin_next(na, nb, la, lb, pza, pxb, i);
+                products(pxa[i], pzb, i);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                yb[i] = rb.get(lb, i, 2);
+                ya[i] = ra.get(la, i, 2);
+                products(pxa[i], pzb, i);
+                products(pza[i], pxb, i);
+                products(pza[i], pzb, i);
+            }
+            meet(Ahead{});
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                products(ya[i], pxb, i);
+                begin_next(na, nb, la, lb, pza, pzb, i);
+                products(pxa[i], yb, i);
+            }
         }
         advance();
+    };
+    // the steps of a round of stages: operands' registers change places from step
+    // to step
+    auto pair = [&](char* a0, char* b0, char* a1, char* b1, const char* a2, const char* b2) {
+        if constexpr (IN_PLACE) {
+            ra.renew();
+            rb.renew();
+        }
+        if constexpr (P == 1) {
+            step(a0, b0, a1, b1, xa, xb, za, zb);
+            step(a1, b1, a2, b2, xa, xb, za, zb);
+        } else if constexpr (P == 2) {
+            step(a0, b0, a1, b1, xa, xb, za, zb);
+            step(a1, b1, a2, b2, za, xb, xa, zb);
+        } else {
+            step(a0, b0, a1, b1, xa, xb, za, zb);
+            step(a1, b1, a2, b2, za, zb, xa, xb);
+        }
     };
 
     uint32_t g = blockIdx.x;
     begin_tile(g);
     while (true) {
-        meet();
+        meet(None{});
 #pragma unroll
         for (int i = 0; i < F; ++i) {
-            b0[i] = rb.get(lb0, i, 0);
-            a0[i] = ra.get(la0, i, 0);
+            xb[i] = rb.get(lb0, i, 0);
+            xa[i] = ra.get(la0, i, 0);
 #pragma unroll
             for (int j = 0; j < F; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
         settle();
-        // (steps are taken two by two: behind the last one come zeros)
-        for (int t = 0; t < count; t += 2) {
-            step(la0, lb0, la1, lb1);
-            step(la1, lb1, la0, lb0);
+        // (a round of the stages at a time: behind the last step come zeros)
+        for (int t = 0; t < count; t += STAGES) {
+            if constexpr (STAGES == 2) {
+                pair(la0, lb0, la1, lb1, la0, lb0);
+            } else {
+                pair(la0, lb0, la1, lb1, la2, lb2);
+                pair(la2, lb2, la3, lb3, la0, lb0);
+            }
         }
-        meet();
+        meet(None{});
         settle();
-        const int64_t rt = r0 + wr, st = s0 + ws;
+    const int64_t rt = r0 + wr, st = s0 + ws;
         const bool mirrored = mirror;
         g += gridDim.x;
         if (g < tiles) begin_tile(g);
@@ -575,7 +684,7 @@ __global__ __launch_bounds__(256, SIDE == 256 ? 1 : SIDE == 128 ? 2 : 4) void k_
                 float v[8];
                 *(f32x4*)v = *(const f32x4*)at(row, lane % LANES * 2);
                 *(f32x4*)(v + 4) = *(const f32x4*)at(row, lane % LANES * 2 + 1);
-                if (r >= p.R || s >= (EPI == MM_ORTH && p.o.z ? p.o.z_ld : p.S)) continue;
+                if (r >= p.R || s >= (EPI == MM_ORTH && p.o.z ? p.o.z_ld / 2 : p.S)) continue;
                 const int n = (int)max((int64_t)0, min((int64_t)8, p.S - s));
                 if constexpr (EPI == MM_PARTIAL) {
                     // (the rows of the partial sums are padded to 8)
@@ -612,25 +721,25 @@ __global__ __launch_bounds__(256, SIDE == 256 ? 1 : SIDE == 128 ? 2 : 4) void k_
 #endif
 }
 
-template <class T, class TO, int EPI, int SIDE>
+template <class T, class TO, int EPI, int SIDE, int P>
 hipError_t launch_mm_tile(const Mm& p, hipStream_t stream)
 {
     const int64_t tr = (p.R + SIDE - 1) / SIDE, ts = (p.S + SIDE - 1) / SIDE;
     const int64_t tiles = p.symmetric ? tr * (tr + 1) / 2 : tr * ts;
     if (tiles > 0x7fffffffLL || p.batch > 65535) return hipErrorInvalidConfiguration;
-    const int64_t fit = (int64_t)device_cu_count() * wgs_per_cu(SIDE);
+    const int64_t fit = (int64_t)device_cu_count() * wgs_per_cu(SIDE, P);
     const int64_t each = (fit + (int64_t)p.splits * p.batch - 1) / ((int64_t)p.splits * p.batch);
     const dim3 grid((unsigned)(tiles < each ? tiles : each), (unsigned)p.splits, (unsigned)p.batch);
     const dim3 block(256);
     if (p.a.mc)
         if (p.b.mc)
-            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, true, true>), grid, block, 0, stream, p);
+            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, true, true>), grid, block, 0, stream, p);
         else
-            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, true, false>), grid, block, 0, stream, p);
+            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, true, false>), grid, block, 0, stream, p);
     else if (p.b.mc)
-        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, false, true>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, false, true>), grid, block, 0, stream, p);
     else
-        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, false, false>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, false, false>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 

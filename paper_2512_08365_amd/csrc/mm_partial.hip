@@ -3,19 +3,20 @@
 
 namespace mag {
 
-hipError_t launch_mm_partial(const Mm& p, int type, int tile, hipStream_t stream)
+template <class T, int P>
+static hipError_t launch(const Mm& p, int tile, hipStream_t stream)
 {
-    if (type == MAG_F16) {
-        switch (tile) {
-        case TILE_256: return launch_mm_tile<f16, f16, MM_PARTIAL, 256>(p, stream);
-        case TILE_128: return launch_mm_tile<f16, f16, MM_PARTIAL, 128>(p, stream);
-        default: return launch_mm_tile<f16, f16, MM_PARTIAL, 64>(p, stream);
-        }
-    }
-    switch (tile) {
-    case TILE_256: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 256>(p, stream);
-    case TILE_128: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 128>(p, stream);
-    default: return launch_mm_tile<bf16, bf16, MM_PARTIAL, 64>(p, stream);
+    if (tile == TILE_128) return launch_mm_tile<T, T, MM_PARTIAL, 128, P>(p, stream);
+    return launch_mm_tile<T, T, MM_PARTIAL, 64, P>(p, stream);
+}
+
+hipError_t launch_mm_partial(const Mm& p, int kind, int tile, hipStream_t stream)
+{
+    switch (kind) {
+    case MM_BF16: return launch<bf16, 1>(p, tile, stream);
+    case MM_F16: return launch<f16, 1>(p, tile, stream);
+    case MM_F32: return launch<bf16, 3>(p, tile, stream);
+    default: return launch<f16, 2>(p, tile, stream);
     }
 }
 
