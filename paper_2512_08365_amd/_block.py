@@ -50,21 +50,26 @@ def _as_rows(x, name):
                                           f"{x.stride()} cannot be seen as one") from None
 
 
-def _matrix(x, like, name):
-    """The five fields of a mag_matrix; x: a tensor of like's type and device."""
-    if not isinstance(x, torch.Tensor) or x.device != like.device:
-        raise MagnetonError(N.MAG_E_NULL, f"{name} must be a tensor on {like.device}")
-    if x.dtype != like.dtype:
-        raise MagnetonError(N.MAG_E_SIZE, f"{name} must be {like.dtype}, got {x.dtype}")
-    x = _as_rows(x, name)
+def _refuse(x, dtype, index, name):
+    """why x is not what _matrix or _vector ask for"""
+    if not isinstance(x, torch.Tensor) or x.get_device() != index:
+        raise MagnetonError(N.MAG_E_NULL, f"{name} must be a tensor on GPU {index}")
+    raise MagnetonError(N.MAG_E_SIZE, f"{name} must be {dtype}, got {x.dtype}")
+
+
+# (a decode step calls these some ten times: few attribute reads, one check)
+def _matrix(x, dtype, index, name):
+    """The five fields of a mag_matrix; x: a tensor of that type and device."""
+    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.get_device() != index:
+        _refuse(x, dtype, index, name)
+    if x.dim() != 2:
+        x = _as_rows(x, name)
     return (x.data_ptr(), *x.shape, *x.stride())
 
 
-def _vector(x, dtype, like, width, name):
-    if not isinstance(x, torch.Tensor) or x.device != like.device:
-        raise MagnetonError(N.MAG_E_NULL, f"{name} must be a tensor on {like.device}")
-    if x.dtype != dtype:
-        raise MagnetonError(N.MAG_E_SIZE, f"{name} must be {dtype}, got {x.dtype}")
+def _vector(x, dtype, index, width, name):
+    if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.get_device() != index:
+        _refuse(x, dtype, index, name)
     if x.dim() != 1 or x.shape[0] != width or (width > 1 and x.stride(0) != 1):
         raise MagnetonError(N.MAG_E_SIZE, f"{name} must be {width} contiguous values")
     return x.data_ptr()
@@ -84,36 +89,44 @@ def _size(call, args) -> int:
 
 
 def _workspace(workspace, size, args, like):
-    """(pointer, bytes) of the workspace given, or of one allocated for the call
-    (its memory is reused in stream order)."""
+    """(tensor, pointer, bytes) of the workspace given, or of one allocated for the
+    call (its memory is reused in stream order)."""
     if workspace is None:
         bytes_ = _size(size, args)
-        workspace = torch.empty(max(bytes_, 1), dtype=torch.uint8, device=like.device)
-    elif (not isinstance(workspace, torch.Tensor) or workspace.device != like.device
+        if not bytes_:
+            return None, 0, 0
+        workspace = torch.empty(bytes_, dtype=torch.uint8, device=like.device)
+    elif (not isinstance(workspace, torch.Tensor) or workspace.get_device() != like.get_device()
           or not workspace.is_contiguous()):
         raise MagnetonError(N.MAG_E_WORKSPACE, f"workspace must be contiguous on {like.device}")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _launch(device, call):
-    """call(stream) with the tensors' device current"""
-    index = device.index
+# the handle of a device's current stream without a stream object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _launch(index, call, *args):
+    """call(*args, stream) with the tensors' device current"""
     if index == torch.cuda.current_device():
-        _check(call(torch.cuda.current_stream(device).cuda_stream))
-        return
-    with torch.cuda.device(index):
-        _check(call(torch.cuda.current_stream(device).cuda_stream))
+        rc = call(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = call(*args, _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
 def _linear_args(x, weight, bias, residual, act, pre, out):
-    dt = _dtype(x, "x")
-    mx = _matrix(x, x, "x")
-    mw = _matrix(weight, x, "weight")
+    dt, ty, dev = _dtype(x, "x"), x.dtype, x.get_device()
+    mw = _matrix(weight, ty, dev, "weight")
     return N.LINEAR_ARGS.pack(
-        dt, act, *mx, *mw, *(_NONE if residual is None else _matrix(residual, x, "residual")),
-        *(_NONE if pre is None else _matrix(pre, x, "pre")),
-        *(_NONE if out is None else _matrix(out, x, "out")),
-        0 if bias is None else _vector(bias, x.dtype, x, mw[1], "bias"))
+        dt, act, *_matrix(x, ty, dev, "x"), *mw,
+        *(_NONE if residual is None else _matrix(residual, ty, dev, "residual")),
+        *(_NONE if pre is None else _matrix(pre, ty, dev, "pre")),
+        *(_NONE if out is None else _matrix(out, ty, dev, "out")),
+        0 if bias is None else _vector(bias, ty, dev, mw[1], "bias"))
 
 
 def linear_workspace_size(x, weight) -> int:
@@ -144,19 +157,20 @@ def linear(x, weight, bias=None, residual=None, *, activation=None, pre=None, ou
             pre = torch.empty(shape, dtype=x.dtype, device=x.device)
     args = _linear_args(x, weight, bias, residual, act, pre, out)
     ws, p, n = _workspace(workspace, lib.mag_linear_workspace_size, args, x)
-    _launch(x.device, lambda s: lib.mag_linear(args, p, n, s))
+    _launch(x.get_device(), lib.mag_linear, args, p, n)
     return out if pre is None else (out, pre)
 
 
 def _linear_backward_args(x, weight, dy, pre, act, dx, dweight, dbias):
-    dt = _dtype(x, "x")
-    mw = _matrix(weight, x, "weight")
+    dt, ty, dev = _dtype(x, "x"), x.dtype, x.get_device()
+    mw = _matrix(weight, ty, dev, "weight")
     return N.LINEAR_BACKWARD_ARGS.pack(
-        dt, act, *_matrix(x, x, "x"), *mw, *(_NONE if pre is None else _matrix(pre, x, "pre")),
-        *(_NONE if dy is None else _matrix(dy, x, "dy")),
-        *(_NONE if dx is None else _matrix(dx, x, "dx")),
-        *(_NONE if dweight is None else _matrix(dweight, x, "dweight")),
-        0 if dbias is None else _vector(dbias, x.dtype, x, mw[1], "dbias"))
+        dt, act, *_matrix(x, ty, dev, "x"), *mw,
+        *(_NONE if pre is None else _matrix(pre, ty, dev, "pre")),
+        *(_NONE if dy is None else _matrix(dy, ty, dev, "dy")),
+        *(_NONE if dx is None else _matrix(dx, ty, dev, "dx")),
+        *(_NONE if dweight is None else _matrix(dweight, ty, dev, "dweight")),
+        0 if dbias is None else _vector(dbias, ty, dev, mw[1], "dbias"))
 
 
 def linear_backward_workspace_size(x, weight, dy=None) -> int:
@@ -184,31 +198,31 @@ def linear_backward(x, weight, dy, pre=None, *, activation=None, bias=True,
     dx, dweight, dbias = out
     args = _linear_backward_args(x, weight, dy, pre, act, dx, dweight, dbias)
     ws, p, n = _workspace(workspace, lib.mag_linear_backward_workspace_size, args, x)
-    _launch(x.device, lambda s: lib.mag_linear_backward(args, p, n, s))
+    _launch(x.get_device(), lib.mag_linear_backward, args, p, n)
     return dx, dweight, dbias
 
 
 def _norm_args(x, weight, bias, y, dy, dx, mean, rstd, dweight, dbias, eps):
-    dt = _dtype(x, "x")
-    mx = _matrix(x, x, "x")
-    rows, width = mx[1], mx[2]
-    some = next((v for v in (weight, bias, dweight, dbias) if v is not None), None)
-    wt = x.dtype if some is None else some.dtype
-    if some is not None:
-        _dtype(some, "weight")
-
-    def vec(v, name):
-        return 0 if v is None else _vector(v, wt, x, width, name)
-
-    def stat(v, name):
-        return 0 if v is None else _vector(v, torch.float32, x, rows, name)
-
+    dt, ty, dev = _dtype(x, "x"), x.dtype, x.get_device()
+    mx = _matrix(x, ty, dev, "x")
+    _, rows, width, _, _ = mx
+    wt = ty
+    for some in (weight, bias, dweight, dbias):
+        if some is not None:
+            _dtype(some, "weight")
+            wt = some.dtype
+            break
+    f32 = torch.float32
     return N.NORM_ARGS.pack(
-        dt, _DTYPES[wt], *mx, *(_NONE if y is None else _matrix(y, x, "out")),
-        *(_NONE if dy is None else _matrix(dy, x, "dy")),
-        *(_NONE if dx is None else _matrix(dx, x, "dx")), vec(weight, "weight"),
-        vec(bias, "bias"), stat(mean, "mean"), stat(rstd, "rstd"), vec(dweight, "dweight"),
-        vec(dbias, "dbias"), float(eps))
+        dt, _DTYPES[wt], *mx, *(_NONE if y is None else _matrix(y, ty, dev, "out")),
+        *(_NONE if dy is None else _matrix(dy, ty, dev, "dy")),
+        *(_NONE if dx is None else _matrix(dx, ty, dev, "dx")),
+        0 if weight is None else _vector(weight, wt, dev, width, "weight"),
+        0 if bias is None else _vector(bias, wt, dev, width, "bias"),
+        0 if mean is None else _vector(mean, f32, dev, rows, "mean"),
+        0 if rstd is None else _vector(rstd, f32, dev, rows, "rstd"),
+        0 if dweight is None else _vector(dweight, wt, dev, width, "dweight"),
+        0 if dbias is None else _vector(dbias, wt, dev, width, "dbias"), eps)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, *, statistics=None, out=None):
@@ -228,7 +242,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, *, statistics=None, out=None
     elif statistics is not None:
         mean, rstd = statistics
     args = _norm_args(x, weight, bias, out, None, None, mean, rstd, None, None, eps)
-    _launch(x.device, lambda s: lib.mag_layer_norm(args, s))
+    _launch(x.get_device(), lib.mag_layer_norm, args)
     return out if statistics is None else (out, mean, rstd)
 
 
@@ -254,7 +268,7 @@ def layer_norm_backward(x, dy, mean, rstd, weight=None, *, need=(True, True, Tru
     dx, dweight, dbias = out
     args = _norm_args(x, weight, None, None, dy, dx, mean, rstd, dweight, dbias, 0.0)
     ws, p, n = _workspace(workspace, lib.mag_layer_norm_backward_workspace_size, args, x)
-    _launch(x.device, lambda s: lib.mag_layer_norm_backward(args, p, n, s))
+    _launch(x.get_device(), lib.mag_layer_norm_backward, args, p, n)
     return dx, dweight, dbias
 
 
@@ -262,7 +276,7 @@ def _orthogonalize_args(g, steps, coefficients, eps, out):
     dt = _dtype(g, "g")
     if out is None:
         out = g
-    elif not isinstance(out, torch.Tensor) or out.device != g.device:
+    elif not isinstance(out, torch.Tensor) or out.get_device() != g.get_device():
         raise MagnetonError(N.MAG_E_NULL, f"out must be a tensor on {g.device}")
     if g.dim() not in (2, 3) or out.shape != g.shape:
         raise MagnetonError(N.MAG_E_SIZE, "g and out must be [rows, cols] or [batch, rows, cols]")
@@ -293,5 +307,5 @@ def orthogonalize(g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, 
         out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
     args = _orthogonalize_args(g, steps, coefficients, eps, out)
     ws, p, n = _workspace(workspace, lib.mag_orthogonalize_workspace_size, args, g)
-    _launch(g.device, lambda s: lib.mag_orthogonalize(args, p, n, s))
+    _launch(g.get_device(), lib.mag_orthogonalize, args, p, n)
     return out

@@ -223,6 +223,8 @@ int check_linear(const mag_linear_args* a)
 }
 
 struct LinearPlan {
+    bool skinny;       // few rows: operands as they lie, one launch, no workspace
+    bool across;       // the weight lies input by output
     Operand x, w;
     Shape shape;
     float* partial;
@@ -230,6 +232,11 @@ struct LinearPlan {
 
 size_t plan_linear(const mag_linear_args* a, void* ws, LinearPlan& pl)
 {
+    const bool along = a->weight.col_stride == 1 || a->weight.cols <= 1;
+    pl.across = !along;
+    pl.skinny = a->x.rows <= mag::SKINNY_ROWS && (a->x.col_stride == 1 || a->x.cols <= 1) &&
+                (along || a->weight.row_stride == 1 || a->weight.rows <= 1);
+    if (pl.skinny) return 0;
     pl.x = operand(a->x, a->dtype, true);
     pl.w = operand(a->weight, a->dtype, true);
     pl.shape = choose(a->x.rows, a->weight.rows, a->x.cols, kind_of(a->dtype), 1, false);
@@ -421,6 +428,30 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     TRY(check_workspace(workspace, workspace_bytes, plan_linear(a, nullptr, pl)));
     if (M == 0 || N == 0) return MAG_OK;
     plan_linear(a, workspace, pl);
+    mag::Epilogue e{};
+    e.bias = a->bias;
+    e.act = a->activation;
+    e.res = a->residual.data;
+    e.res_rs = a->residual.row_stride;
+    e.res_cs = a->residual.col_stride;
+    e.pre = a->pre.data;
+    e.pre_ld = a->pre.row_stride;
+    e.y = a->y.data;
+    e.y_ld = a->y.row_stride;
+    if (pl.skinny) {
+        mag::SkinnyParams s{};
+        s.x = a->x.data;
+        s.x_ld = a->x.row_stride;
+        s.w = a->weight.data;
+        s.w_ld = pl.across ? a->weight.col_stride : a->weight.row_stride;
+        s.across = pl.across;
+        s.M = M;
+        s.N = N;
+        s.K = K;
+        s.e = e;
+        TRY_HIP(mag::launch_skinny(s, a->dtype, stream), "linear launch");
+        return MAG_OK;
+    }
     if (pl.x.packed) TRY(pack(pl.x, a->x, a->dtype, stream));
     if (pl.w.packed) TRY(pack(pl.w, a->weight, a->dtype, stream));
     mag::Mm p{};
@@ -433,15 +464,7 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     p.splits = pl.shape.splits;
     p.partial = pl.partial;
     p.partial_ld = up8(N);
-    p.e.bias = a->bias;
-    p.e.act = a->activation;
-    p.e.res = a->residual.data;
-    p.e.res_rs = a->residual.row_stride;
-    p.e.res_cs = a->residual.col_stride;
-    p.e.pre = a->pre.data;
-    p.e.pre_ld = a->pre.row_stride;
-    p.e.y = a->y.data;
-    p.e.y_ld = a->y.row_stride;
+    p.e = e;
     p.e.vec = vec8(p.e.y, M, p.e.y_ld, a->dtype) && vec8(p.e.pre, M, p.e.pre_ld, a->dtype) &&
               vec8(p.e.bias, 1, 0, a->dtype) && vec8(p.e.res, M, p.e.res_rs, a->dtype) &&
               (!p.e.res || p.e.res_cs == 1);

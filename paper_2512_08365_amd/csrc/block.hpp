@@ -80,6 +80,20 @@ hipError_t launch_mm_orth(const Mm& p, int tile, hipStream_t stream);
 hipError_t launch_mm_join(const Mm& p, int dtype, hipStream_t stream);
 hipError_t launch_orth_join(const Mm& p, hipStream_t stream);
 
+// y of at most SKINNY_ROWS rows, operands as they lie: x row by row, weight along
+// the reduction or (across) input by output
+constexpr int64_t SKINNY_ROWS = 32;
+struct SkinnyParams {
+    const void* x;
+    int64_t x_ld;
+    const void* w;
+    int64_t w_ld;
+    int32_t across;
+    int64_t M, N, K;
+    Epilogue e;
+};
+hipError_t launch_skinny(const SkinnyParams& p, int dtype, hipStream_t stream);
+
 // rows x cols values of any strides as an operand's rows of ld elements: two-byte
 // types as they are, fp32 in three bfloat16 parts
 struct PackParams {
