@@ -150,20 +150,54 @@ struct Shape {
     int splits;
 };
 
-// kind: MM_BF16 ...
+// What a workgroup's step, its tile beside the steps, and the call cost, in us,
+// measured with 256 and 512 workgroups over reductions of 512 and 4,096: alone
+// on a CU, and with a second one (0: there is no room for one).
+struct TileCost {
+    double alone, shared, tile;
+};
+constexpr double CALL_COST = 2.5;
+constexpr double JOIN_COST = 3.5;           // a split product's second launch
+constexpr double PARTIAL_BYTES = 4.5e6;     // of partial sums a us, written or read
+const TileCost TILE_COST[4][mag::TILES] = {
+    // 64 (four steps in LDS), 128, 256
+    {{0.19, 0.35, 1.8}, {0.64, 0.80, 3.5}, {1.43, 0.0, 11.5}},   // bfloat16: 64 k a step
+    {{0.19, 0.35, 1.8}, {0.64, 0.80, 3.5}, {1.43, 0.0, 11.5}},   // half
+    {{0.35, 0.0, 3.6}, {1.30, 0.0, 10.5}, {0.0, 0.0, 0.0}},      // three parts: 32 k, six products
+    {{0.22, 0.36, 1.8}, {0.73, 1.19, 6.5}, {2.13, 0.0, 10.5}},   // two parts: 32 k, three products
+};
+
+// The tile and split of the reduction that these costs make fastest: large tiles
+// move the least data where there are enough of them for the 256 CUs, small ones
+// and splits fill the CUs otherwise (1,024 cubed in bfloat16: 8 us with 64, 13 us
+// with 128; 4,096 cubed: 109 us with 256, 120 us with 128).  kind: MM_BF16 ...
 Shape choose(int64_t R, int64_t S, int64_t K, int kind, int64_t batch, bool symmetric)
 {
-    auto tiles = [&](int t) {
-        const int64_t side = mag::TILE_SIDE[t], tr = (R + side - 1) / side;
-        return std::max<int64_t>(1, (symmetric ? tr * (tr + 1) / 2 : tr * ((S + side - 1) / side)) * batch);
-    };
+    constexpr int64_t CUS = 256;
     const int64_t step = kind == mag::MM_F32 || kind == mag::MM_HALVES ? 32 : 64;
     const int64_t steps = std::max<int64_t>(1, (K + step - 1) / step);
-    if (kind != mag::MM_F32 && tiles(mag::TILE_256) >= 224) return {mag::TILE_256, 1};
-    if (tiles(mag::TILE_128) >= 224) return {mag::TILE_128, 1};
-    const int64_t n = tiles(mag::TILE_64);
-    if (n >= 256) return {mag::TILE_64, 1};
-    return {mag::TILE_64, (int)std::max<int64_t>(1, std::min<int64_t>({512 / n, steps / 4, 64}))};
+    Shape best{mag::TILE_64, 1};
+    double least = 1e300;
+    for (int t = 0; t < mag::TILES; ++t) {
+        const TileCost& c = TILE_COST[kind][t];
+        if (c.alone == 0.0) continue;
+        const int64_t side = mag::TILE_SIDE[t], tr = (R + side - 1) / side;
+        const int64_t tiles = (symmetric ? tr * (tr + 1) / 2 : tr * ((S + side - 1) / side)) * batch;
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+            if (s > 1 && (t == mag::TILE_256 || steps < 2 * s)) break;
+            const int64_t wgs = tiles * s;
+            const bool shared = wgs > CUS && c.shared > 0.0;
+            const int64_t rounds = (wgs + (shared ? 2 : 1) * CUS - 1) / ((shared ? 2 : 1) * CUS);
+            double cost = CALL_COST + (double)rounds *
+                          ((double)((steps + s - 1) / s) * (shared ? c.shared : c.alone) + c.tile);
+            if (s > 1) cost += JOIN_COST + 2.0 * (double)s * (double)R * (double)S * (double)batch * 4.0 / PARTIAL_BYTES;
+            if (cost < least) {
+                least = cost;
+                best = Shape{t, s};
+            }
+        }
+    }
+    return best;
 }
 
 int kind_of(int dtype)

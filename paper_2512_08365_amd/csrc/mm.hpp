@@ -384,11 +384,11 @@ __device__ __forceinline__ void tile_above(uint32_t b, uint32_t& ti, uint32_t& t
     ti = b - tj * (tj + 1) / 2;
 }
 
-// Tiles of operands in LDS at a time, and workgroups that a CU holds: a large tile
-// hides the way from memory behind one step's products, a small one needs more
-// steps ahead.
-constexpr int stages_of(int side, int P) { return side == 64 && P < 3 ? 4 : 2; }
-constexpr int wgs_per_cu(int side, int P) { return side == 256 ? 1 : side == 128 && P == 3 ? 1 : 2; }
+// Workgroups that a CU holds, by its 160 KB of LDS and 512 registers a lane.
+constexpr int wgs_per_cu(int side, int P, int stages)
+{
+    return side == 256 || (side == 128 && (P == 3 || stages == 4)) || (P == 3 && stages == 4) ? 1 : 2;
+}
 
 // Workgroups (as many as fit) walk the tiles.  Four waves hold a quarter of a
 // tile's sums each.  Fragments are read from LDS a few at a time while the
@@ -400,13 +400,13 @@ constexpr int wgs_per_cu(int side, int P) { return side == 256 ? 1 : side == 128
 //   one part:    the halves of a step, 0 0 | 1 1
 //   two parts:   high high | low high | high low
 //   three parts: 1 1 | 1 2, 2 1, 2 2 | 3 1, 1 3 (the products below 2^-24 left out)
-template <class T, class TO, int EPI, int SIDE, int P, bool AMC, bool BMC>
-__global__ __launch_bounds__(256, wgs_per_cu(SIDE, P)) void k_mm(Mm p)
+template <class T, class TO, int EPI, int SIDE, int STAGES, int P, bool AMC, bool BMC>
+__global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int THREADS = 256, W = 2;          // 2 x 2 waves
     constexpr int COLS = SIDE / W, F = COLS / 16;  // a wave's rows and columns, in 16s
-    constexpr int STAGES = stages_of(SIDE, P), STEP = step_of(P);
+    constexpr int STEP = step_of(P);
     constexpr bool IN_PLACE = F >= 8;
     using TA = Tile<SIDE, AMC, P, THREADS>;
     using TB = Tile<SIDE, BMC, P, THREADS>;
@@ -721,25 +721,25 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P)) void k_mm(Mm p)
 #endif
 }
 
-template <class T, class TO, int EPI, int SIDE, int P>
+template <class T, class TO, int EPI, int SIDE, int STAGES, int P>
 hipError_t launch_mm_tile(const Mm& p, hipStream_t stream)
 {
     const int64_t tr = (p.R + SIDE - 1) / SIDE, ts = (p.S + SIDE - 1) / SIDE;
     const int64_t tiles = p.symmetric ? tr * (tr + 1) / 2 : tr * ts;
     if (tiles > 0x7fffffffLL || p.batch > 65535) return hipErrorInvalidConfiguration;
-    const int64_t fit = (int64_t)device_cu_count() * wgs_per_cu(SIDE, P);
+    const int64_t fit = (int64_t)device_cu_count() * wgs_per_cu(SIDE, P, STAGES);
     const int64_t each = (fit + (int64_t)p.splits * p.batch - 1) / ((int64_t)p.splits * p.batch);
     const dim3 grid((unsigned)(tiles < each ? tiles : each), (unsigned)p.splits, (unsigned)p.batch);
     const dim3 block(256);
     if (p.a.mc)
         if (p.b.mc)
-            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, true, true>), grid, block, 0, stream, p);
+            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, STAGES, P, true, true>), grid, block, 0, stream, p);
         else
-            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, true, false>), grid, block, 0, stream, p);
+            hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, STAGES, P, true, false>), grid, block, 0, stream, p);
     else if (p.b.mc)
-        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, false, true>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, STAGES, P, false, true>), grid, block, 0, stream, p);
     else
-        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, P, false, false>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_mm<T, TO, EPI, SIDE, STAGES, P, false, false>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 

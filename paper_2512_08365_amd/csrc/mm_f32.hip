@@ -5,8 +5,8 @@ namespace mag {
 
 hipError_t launch_mm_f32(const Mm& p, int tile, hipStream_t stream)
 {
-    if (tile == TILE_128) return launch_mm_tile<bf16, float, MM_LINEAR, 128, 3>(p, stream);
-    return launch_mm_tile<bf16, float, MM_LINEAR, 64, 3>(p, stream);
+    if (tile == TILE_128) return launch_mm_tile<bf16, float, MM_LINEAR, 128, 2, 3>(p, stream);
+    return launch_mm_tile<bf16, float, MM_LINEAR, 64, 4, 3>(p, stream);
 }
 
 }  // namespace mag

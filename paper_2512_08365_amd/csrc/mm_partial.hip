@@ -6,8 +6,8 @@ namespace mag {
 template <class T, int P>
 static hipError_t launch(const Mm& p, int tile, hipStream_t stream)
 {
-    if (tile == TILE_128) return launch_mm_tile<T, T, MM_PARTIAL, 128, P>(p, stream);
-    return launch_mm_tile<T, T, MM_PARTIAL, 64, P>(p, stream);
+    if (tile == TILE_128) return launch_mm_tile<T, T, MM_PARTIAL, 128, 2, P>(p, stream);
+    return launch_mm_tile<T, T, MM_PARTIAL, 64, 4, P>(p, stream);
 }
 
 hipError_t launch_mm_partial(const Mm& p, int kind, int tile, hipStream_t stream)
