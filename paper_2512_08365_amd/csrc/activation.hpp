@@ -14,6 +14,22 @@ __device__ __forceinline__ float logistic(float z)
 constexpr float GELU_2K = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float GELU_C = 0.044715f;
 
+// The normal distribution's Phi(z) and, times sqrt(2 pi), its density: Abramowitz
+// and Stegun's formula 7.1.26 for the error function (off by 1.5e-7 at most), as
+// the tail below 0, so that small tails keep their size.
+__device__ __forceinline__ float normal(float z, float& density)
+{
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    density = __expf(-0.5f * z * z);
+    float q = fmaf(1.061405429f, t, -1.453152027f);
+    q = fmaf(q, t, 1.421413741f);
+    q = fmaf(q, t, -0.284496736f);
+    q = fmaf(q, t, 0.254829592f);
+    const float tail = 0.5f * q * t * density;
+    return z > 0.0f ? 1.0f - tail : tail;
+}
+
 // one activation or slope of N values: the kind is looked at once
 template <int N, class F>
 __device__ __forceinline__ void each(float* z, F f)
@@ -28,7 +44,10 @@ __device__ __forceinline__ void activate(float* z, int act)
     switch (act) {
     case MAG_ACT_RELU: return each<N>(z, [](float v) { return v > 0.0f ? v : (v != v ? v : 0.0f); });
     case MAG_ACT_GELU:
-        return each<N>(z, [](float v) { return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f)); });
+        return each<N>(z, [](float v) {
+            float density;
+            return v * normal(v, density);
+        });
     case MAG_ACT_GELU_TANH:
         return each<N>(z, [](float v) { return v * logistic(GELU_2K * (v + GELU_C * v * v * v)); });
     case MAG_ACT_SILU: return each<N>(z, [](float v) { return v * logistic(v); });
@@ -44,8 +63,9 @@ __device__ __forceinline__ void slopes(float* z, int act)
     case MAG_ACT_RELU: return each<N>(z, [](float v) { return v > 0.0f ? 1.0f : 0.0f; });
     case MAG_ACT_GELU:
         return each<N>(z, [](float v) {
-            return 0.5f * (1.0f + erff(v * 0.70710678118654752f)) +
-                   v * __expf(-0.5f * v * v) * 0.39894228040143268f;
+            float density;
+            const float phi = normal(v, density);
+            return fmaf(v * density, 0.39894228040143268f, phi);
         });
     case MAG_ACT_GELU_TANH:
         return each<N>(z, [](float v) {

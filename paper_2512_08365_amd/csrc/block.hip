@@ -130,7 +130,7 @@ Operand operand(const mag_matrix& m, int dtype, bool along)
     return o;
 }
 
-int pack(const Operand& o, const mag_matrix& m, int dtype, hipStream_t stream)
+mag::PackParams packing(const Operand& o, const mag_matrix& m)
 {
     mag::PackParams p{};
     p.src = m.data;
@@ -140,8 +140,7 @@ int pack(const Operand& o, const mag_matrix& m, int dtype, hipStream_t stream)
     p.cols = m.cols;
     p.dst = const_cast<void*>(o.op.p);
     p.ld = o.op.ld;
-    TRY_HIP(mag::launch_pack(p, dtype, stream), "pack launch");
-    return MAG_OK;
+    return p;
 }
 
 // Tile and splits of R x S x K.
@@ -486,8 +485,10 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
         TRY_HIP(mag::launch_skinny(s, a->dtype, stream), "linear launch");
         return MAG_OK;
     }
-    if (pl.x.packed) TRY(pack(pl.x, a->x, a->dtype, stream));
-    if (pl.w.packed) TRY(pack(pl.w, a->weight, a->dtype, stream));
+    const mag::PackParams px = packing(pl.x, a->x), pw = packing(pl.w, a->weight);
+    TRY_HIP(mag::launch_prepare(pl.x.packed ? &px : nullptr, pl.w.packed ? &pw : nullptr, nullptr,
+                                a->dtype, stream),
+            "linear launch");
     mag::Mm p{};
     p.a = pl.x.op;
     p.b = pl.w.op;
@@ -564,14 +565,19 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         s.part = pl.column_part;
         TRY_HIP(mag::launch_slope(s, a->dtype, stream), "linear_backward launch");
     }
+    const bool dx = a->dx.data && M > 0 && K > 0, dw = a->dweight.data && N > 0 && K > 0;
+    const mag::PackParams px = packing(pl.x, a->x), pw = packing(pl.w, a->weight);
+    const mag::ColumnSums sums{pl.column_part, mag::slope_chunks(M, N), N, a->dbias};
+    TRY_HIP(mag::launch_prepare(dw && pl.x.packed ? &px : nullptr, dx && pl.w.packed ? &pw : nullptr,
+                                a->dbias ? &sums : nullptr, a->dtype, stream),
+            "linear_backward launch");
     mag::Mm p{};
     p.batch = 1;
     p.partial = pl.partial;
     p.S = K;
     p.partial_ld = up8(K);
     p.a = pl.dz;
-    if (a->dx.data && M > 0 && K > 0) {
-        if (pl.w.packed) TRY(pack(pl.w, a->weight, a->dtype, stream));
+    if (dx) {
         p.b = pl.w.op;
         p.R = M;
         p.K = N;
@@ -581,8 +587,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         p.e.vec = vec8(p.e.y, M, p.e.y_ld, a->dtype);
         TRY(launch_linear(p, a->dtype, pl.dx.tile, stream));
     }
-    if (a->dweight.data && N > 0 && K > 0) {
-        if (pl.x.packed) TRY(pack(pl.x, a->x, a->dtype, stream));
+    if (dw) {
         p.a.mc = !pl.dz.mc;
         p.b = pl.x.op;
         p.R = N;

@@ -103,9 +103,17 @@ struct PackParams {
     void* dst;
     int64_t ld;
 };
-hipError_t launch_pack(const PackParams& p, int dtype, hipStream_t stream);
+// column sums of `chunks` rows of sums
+struct ColumnSums {
+    const float* part;
+    int64_t chunks, N;
+    void* out;
+};
+// two matrices packed and column sums finished, any of them NULL: one launch
+hipError_t launch_prepare(const PackParams* a, const PackParams* b, const ColumnSums* c, int dtype,
+                          hipStream_t stream);
 
-// dz = dy act'(pre), and dbias = the column sums of dz
+// dz = dy act'(pre), and with dbias the column sums of dz by chunks of rows
 struct SlopeParams {
     const void* dy;
     int64_t dy_rs, dy_cs;

@@ -66,12 +66,12 @@ __host__ __device__ int64_t width_of(int64_t n)
     return sizeof(T) == 4 ? (n + 31) / 32 * 32 : (n + 7) / 8 * 8;
 }
 
-// Bandwidth bound: each thread moves 8 neighbours of a row.
+// One thread's 8 neighbours of a packed row.
 template <class T>
-__global__ __launch_bounds__(256) void k_pack(PackParams p)
+__device__ __forceinline__ void pack_some(const PackParams& p, int64_t block, int64_t blocks)
 {
     const int64_t per_row = width_of<T>(p.cols) / 8, n = p.rows * per_row;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = block * 256 + threadIdx.x; i < n; i += blocks * 256) {
         const int64_t r = i / per_row, j = i % per_row * 8;
         float v[8];
         get8(static_cast<const T*>(p.src) + r * p.rs, p.cs, j, p.cols, v);
@@ -80,9 +80,11 @@ __global__ __launch_bounds__(256) void k_pack(PackParams p)
 }
 
 constexpr int SLOPE_COLS = 512;  // columns of a workgroup: 64 lanes of 8
+constexpr int SLOPE_ROWS = 2;    // rows a wave has in flight (4: too many registers, 40 % slower)
 
 // dz and the column sums of one chunk of rows: four waves take its rows in
-// turn, 8 columns a lane, and add their sums up in LDS at the end.
+// turn, 8 columns a lane, and add their sums up in LDS at the end.  Bound by
+// memory (a prompt's 805 MB in 170 us).
 template <class T>
 __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
 {
@@ -90,21 +92,29 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t j = (int64_t)blockIdx.x * SLOPE_COLS + lane * 8;
     const int64_t i0 = (int64_t)blockIdx.y * chunk, i1 = min(i0 + chunk, p.M);
+    const bool acts = p.act != MAG_ACT_NONE;
     float sum[8] = {};
     if (j < width_of<T>(p.N))
-        for (int64_t i = i0 + wave; i < i1; i += 4) {
-            float d[8];
-            get8(static_cast<const T*>(p.dy) + i * p.dy_rs, p.dy_cs, j, p.N, d);
-            if (p.act != MAG_ACT_NONE) {
-                float z[8];
-                get8(static_cast<const T*>(p.pre) + i * p.pre_rs, p.pre_cs, j, p.N, z);
-                slopes<8>(z, p.act);
+        for (int64_t i = i0 + wave; i < i1; i += 4 * SLOPE_ROWS) {
+            float d[SLOPE_ROWS][8], z[SLOPE_ROWS][8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] *= z[e];
+            for (int u = 0; u < SLOPE_ROWS; ++u) {
+                const int64_t r = min(i + 4 * u, i1 - 1);
+                get8(static_cast<const T*>(p.dy) + r * p.dy_rs, p.dy_cs, j, p.N, d[u]);
+                if (acts) get8(static_cast<const T*>(p.pre) + r * p.pre_rs, p.pre_cs, j, p.N, z[u]);
+            }
+            if (acts) {
+                slopes<8 * SLOPE_ROWS>(z[0], p.act);
+#pragma unroll
+                for (int e = 0; e < 8 * SLOPE_ROWS; ++e) d[0][e] *= z[0][e];
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += d[e];
-            if (p.dz) put8<T>(d, static_cast<short*>(p.dz) + i * p.ldz, j);
+            for (int u = 0; u < SLOPE_ROWS; ++u) {
+                if (i + 4 * u >= i1) break;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += d[u][e];
+                if (p.dz) put8<T>(d[u], static_cast<short*>(p.dz) + (i + 4 * u) * p.ldz, j);
+            }
         }
     if (!p.dbias) return;
 #pragma unroll
@@ -118,20 +128,38 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
     }
 }
 
-// column sums of the chunks' sums: 4 waves a workgroup of 64 columns
+// 64 columns' sums of the chunks' sums
 template <class T>
-__global__ __launch_bounds__(256) void k_column_sums(const float* part, int64_t chunks, int64_t N,
-                                                     T* out)
+__device__ __forceinline__ void column_sums(const ColumnSums& p, int64_t block)
 {
     __shared__ float sums[4][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t j = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (j < N)
-        for (int64_t c = wave; c < chunks; c += 4) s += part[c * N + j];
-    sums[wave][lane] = s;
+    const int64_t j = block * 64 + lane;
+    float s[8] = {};
+    if (j < p.N)
+        for (int64_t c = wave; c < p.chunks; c += 32)
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (c + 4 * u < p.chunks) s[u] += p.part[(c + 4 * u) * p.N + j];
+    sums[wave][lane] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
     __syncthreads();
-    if (wave == 0 && j < N) out[j] = (T)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
+    if (wave == 0 && j < p.N)
+        static_cast<T*>(p.out)[j] =
+            (T)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
+}
+
+// What a layer's products need beforehand, side by side in one launch (each is
+// a few us of latency): up to two matrices packed and the column sums finished.
+template <class T>
+__global__ __launch_bounds__(256) void k_prepare(PackParams a, PackParams b, ColumnSums c,
+                                                 uint32_t blocks_a, uint32_t blocks_b)
+{
+    if (blockIdx.x < blocks_a)
+        pack_some<T>(a, blockIdx.x, blocks_a);
+    else if (blockIdx.x < blocks_a + blocks_b)
+        pack_some<T>(b, blockIdx.x - blocks_a, blocks_b);
+    else
+        column_sums<T>(c, blockIdx.x - blocks_a - blocks_b);
 }
 
 template <class TO>
@@ -162,17 +190,26 @@ unsigned blocks_for(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 
 
 }  // namespace
 
-hipError_t launch_pack(const PackParams& p, int dtype, hipStream_t stream)
+hipError_t launch_prepare(const PackParams* a, const PackParams* b, const ColumnSums* c, int dtype,
+                          hipStream_t stream)
 {
-    const int64_t n = p.rows * ((p.cols + 7) / 8);
-    if (n == 0) return hipSuccess;
-    const dim3 grid(blocks_for(n)), block(256);
+    auto blocks = [](const PackParams* p) {
+        return p ? blocks_for(p->rows * ((p->cols + 7) / 8)) : 0u;
+    };
+    const unsigned na = blocks(a), nb = blocks(b), nc = c ? (unsigned)((c->N + 63) / 64) : 0u;
+    if (na + nb + nc == 0) return hipSuccess;
+    const PackParams none{};
+    const ColumnSums no{};
+    const dim3 grid(na + nb + nc), block(256);
     if (dtype == MAG_F32)
-        hipLaunchKernelGGL(k_pack<float>, grid, block, 0, stream, p);
+        hipLaunchKernelGGL(k_prepare<float>, grid, block, 0, stream, a ? *a : none, b ? *b : none,
+                           c ? *c : no, na, nb);
     else if (dtype == MAG_F16)
-        hipLaunchKernelGGL(k_pack<f16>, grid, block, 0, stream, p);
+        hipLaunchKernelGGL(k_prepare<f16>, grid, block, 0, stream, a ? *a : none, b ? *b : none,
+                           c ? *c : no, na, nb);
     else
-        hipLaunchKernelGGL(k_pack<bf16>, grid, block, 0, stream, p);
+        hipLaunchKernelGGL(k_prepare<bf16>, grid, block, 0, stream, a ? *a : none, b ? *b : none,
+                           c ? *c : no, na, nb);
     return hipGetLastError();
 }
 
@@ -189,24 +226,12 @@ hipError_t launch_slope(const SlopeParams& p, int dtype, hipStream_t stream)
     if (p.N == 0) return hipSuccess;
     const int64_t chunks = slope_chunks(p.M, p.N), chunk = (p.M + chunks - 1) / chunks;
     const dim3 grid((unsigned)((p.N + SLOPE_COLS - 1) / SLOPE_COLS), (unsigned)chunks), block(256);
-    const dim3 sums((unsigned)((p.N + 63) / 64));
     if (dtype == MAG_F32)
         hipLaunchKernelGGL(k_slope<float>, grid, block, 0, stream, p, chunk);
     else if (dtype == MAG_F16)
         hipLaunchKernelGGL(k_slope<f16>, grid, block, 0, stream, p, chunk);
     else
         hipLaunchKernelGGL(k_slope<bf16>, grid, block, 0, stream, p, chunk);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !p.dbias) return e;
-    if (dtype == MAG_F32)
-        hipLaunchKernelGGL(k_column_sums<float>, sums, block, 0, stream, p.part, chunks, p.N,
-                           static_cast<float*>(p.dbias));
-    else if (dtype == MAG_F16)
-        hipLaunchKernelGGL(k_column_sums<f16>, sums, block, 0, stream, p.part, chunks, p.N,
-                           static_cast<f16*>(p.dbias));
-    else
-        hipLaunchKernelGGL(k_column_sums<bf16>, sums, block, 0, stream, p.part, chunks, p.N,
-                           static_cast<bf16*>(p.dbias));
     return hipGetLastError();
 }
 

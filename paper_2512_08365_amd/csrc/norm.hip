@@ -263,23 +263,27 @@ __global__ __launch_bounds__(THREADS) void k_norm_back(NormParams p)
     }
 }
 
-// the workgroups' sums added up: 16 waves of 64 columns
+// the workgroups' sums added up: 16 columns a workgroup, 64 threads each that
+// have all of their loads in flight
 template <class W>
 __global__ __launch_bounds__(1024) void k_norm_columns(const float* part, int parts, int64_t n,
                                                        W* dweight, W* dbias)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t j = (int64_t)blockIdx.x * 64 + lane;
-    float s = 0.0f;
+    __shared__ float sums[64][17];
+    const int col = threadIdx.x % 16, row = threadIdx.x / 16;
+    const int64_t j = (int64_t)blockIdx.x * 16 + col;
+    float t[8] = {};
     if (j < 2 * n)
-        for (int k = wave; k < parts; k += 16) s += part[(int64_t)k * 2 * n + j];
-    sums[wave][lane] = s;
-    __syncthreads();
-    if (wave || j >= 2 * n) return;
-    s = 0.0f;
+        for (int k = row; k < parts; k += 512)
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += sums[k][lane];
+            for (int u = 0; u < 8; ++u)
+                if (k + 64 * u < parts) t[u] += part[(int64_t)(k + 64 * u) * 2 * n + j];
+    sums[row][col] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+    __syncthreads();
+    if (threadIdx.x >= 16 || j >= 2 * n) return;
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 64; ++k) s += sums[k][col];
     if (j < n && dweight) dweight[j] = (W)s;
     if (j >= n && dbias) dbias[j - n] = (W)s;
 }
@@ -393,7 +397,7 @@ hipError_t backward(const NormParams& p, hipStream_t stream)
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (sums) {
-        hipLaunchKernelGGL(k_norm_columns<W>, dim3((unsigned)((2 * p.N + 63) / 64)), dim3(1024), 0,
+        hipLaunchKernelGGL(k_norm_columns<W>, dim3((unsigned)((2 * p.N + 15) / 16)), dim3(1024), 0,
                            stream, p.part, parts, p.N, static_cast<W*>(p.dweight),
                            static_cast<W*>(p.dbias));
         e = hipGetLastError();
@@ -408,9 +412,10 @@ hipError_t backward(const NormParams& p, hipStream_t stream)
 
 int norm_parts(int64_t M, int64_t N)
 {
-    const int rows = back_rows(N);
-    return (int)std::max<int64_t>(1, std::min<int64_t>((M + rows - 1) / rows,
-                                                       rows == 1 ? BACK_WGS : 2 * BACK_WGS));
+    // the rows spread evenly over the workgroups
+    const int64_t rows = back_rows(N), most = rows == 1 ? BACK_WGS : 2 * BACK_WGS;
+    const int64_t groups = std::max<int64_t>(1, (M + rows - 1) / rows), rounds = (groups + most - 1) / most;
+    return (int)((groups + rounds - 1) / rounds);
 }
 
 hipError_t launch_norm(const NormParams& p, int dtype, int weight_dtype, hipStream_t stream)
