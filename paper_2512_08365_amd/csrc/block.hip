@@ -234,12 +234,6 @@ size_t partial_bytes(int64_t R, int64_t S, const Shape& s, int64_t batch = 1)
     return s.splits > 1 ? (size_t)(batch * s.splits * R * up8(S) * 4) : 0;
 }
 
-// whether the rows of a matrix start at multiples of 16 bytes
-bool vec8(const void* p, int64_t rows, int64_t row_stride, int dtype)
-{
-    return !p || ((rows <= 1 || row_stride * (int64_t)element(dtype) % 16 == 0) && aligned(p, 16));
-}
-
 // ------------------------------------------------------------------- linear
 
 int check_linear(const mag_linear_args* a)
@@ -500,9 +494,7 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     p.partial = pl.partial;
     p.partial_ld = up8(N);
     p.e = e;
-    p.e.vec = vec8(p.e.y, M, p.e.y_ld, a->dtype) && vec8(p.e.pre, M, p.e.pre_ld, a->dtype) &&
-              vec8(p.e.bias, 1, 0, a->dtype) && vec8(p.e.res, M, p.e.res_rs, a->dtype) &&
-              (!p.e.res || p.e.res_cs == 1);
+    p.e.vec = !e.res || e.res_cs == 1;
     return launch_linear(p, a->dtype, pl.shape.tile, stream);
 }
 
@@ -584,7 +576,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         p.splits = pl.dx.splits;
         p.e.y = a->dx.data;
         p.e.y_ld = a->dx.row_stride;
-        p.e.vec = vec8(p.e.y, M, p.e.y_ld, a->dtype);
+        p.e.vec = 1;
         TRY(launch_linear(p, a->dtype, pl.dx.tile, stream));
     }
     if (dw) {
@@ -595,7 +587,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         p.splits = pl.dw.splits;
         p.e.y = a->dweight.data;
         p.e.y_ld = a->dweight.row_stride;
-        p.e.vec = vec8(p.e.y, N, p.e.y_ld, a->dtype);
+        p.e.vec = 1;
         TRY(launch_linear(p, a->dtype, pl.dw.tile, stream));
     }
     return MAG_OK;

@@ -36,7 +36,7 @@ struct Epilogue {
     void* y;
     int64_t y_ld;
     int32_t act;
-    int32_t vec;          // 16 bytes of a row can be moved at once everywhere
+    int32_t vec;          // neighbours of a row are neighbours in memory everywhere
 };
 
 // z = scale sum + mix M, as two halves or, for the result, one number

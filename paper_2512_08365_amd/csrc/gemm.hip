@@ -178,10 +178,7 @@ __global__ __launch_bounds__(256) void k_mm_join(Mm p)
             for (int e = 0; e < 8; ++e) v[e] += w[e];
         }
         const int m = (int)min((int64_t)8, p.S - s);
-        if constexpr (sizeof(TO) == 4)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < m && !(fabsf(v[e]) < __builtin_inff())) v[e] = whole_sum(p, 0, r, s + e);
+        if constexpr (sizeof(TO) == 4) make_whole(p, 0, r, s, m, v);
         store_linear<TO>(p.e, r, s, m, v);
     }
 }

@@ -219,10 +219,52 @@ __device__ __forceinline__ float whole_sum(const Mm& p, int64_t bt, int64_t r, i
     return sum;
 }
 
-__device__ __forceinline__ void fix(float* v, int e, float x)
+// ... of 8 neighbours of a row, from column s on (n of them)
+__device__ __forceinline__ void make_whole(const Mm& p, int64_t bt, int64_t r, int64_t s, int n, float* v)
 {
+    bool all = true;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i == e ? x : v[i];
+    for (int i = 0; i < 8; ++i) all = all && fabsf(v[i]) < __builtin_inff();
+    if (__builtin_expect(all, 1)) return;
+#pragma unroll 1
+    for (int e = 0; e < n; ++e) {
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x = i == e ? v[i] : x;
+        if (fabsf(x) < __builtin_inff()) continue;
+        x = whole_sum(p, bt, r, s + e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i == e ? x : v[i];
+    }
+}
+
+// eight neighbours of a row, at any element (the hardware takes vector loads and
+// stores at every alignment)
+template <class T>
+__device__ __forceinline__ void load8(const T* p, float* v)
+{
+    constexpr int PER = 16 / sizeof(T);
+    typedef T Piece __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+#pragma unroll
+    for (int h = 0; h < 8 / PER; ++h) {
+        const Piece t = *(const Piece*)(p + h * PER);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[h * PER + i] = (float)t[i];
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void store8(T* p, const float* v)
+{
+    constexpr int PER = 16 / sizeof(T);
+    typedef T Piece __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+#pragma unroll
+    for (int h = 0; h < 8 / PER; ++h) {
+        Piece t;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) t[i] = (T)v[h * PER + i];
+        *(Piece*)(p + h * PER) = t;
+    }
 }
 
 // eight neighbours from column j on (zeros from column `cols` on); neighbours in
@@ -231,45 +273,10 @@ template <class T>
 __device__ __forceinline__ void get8(const T* p, int64_t cs, int64_t j, int64_t cols, float* v)
 {
     if (cs == 1 && j + 8 <= cols) {
-        T t[8];
-        __builtin_memcpy(t, p + j, sizeof(t));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)t[i];
+        load8(p + j, v);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = j + i < cols ? (float)p[(j + i) * cs] : 0.0f;
-    }
-}
-
-// eight neighbours of a row, two bytes or four each
-template <class T>
-__device__ __forceinline__ void load8(const T* p, float* v)
-{
-    if constexpr (sizeof(T) == 4) {
-        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = a[i];
-            v[4 + i] = b[i];
-        }
-    } else {
-        const s16x8 a = *(const s16x8*)p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)__builtin_bit_cast(T, (short)a[i]);
-    }
-}
-
-template <class T>
-__device__ __forceinline__ void store8(T* p, const float* v)
-{
-    if constexpr (sizeof(T) == 4) {
-        *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-        *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-        s16x8 a;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = __builtin_bit_cast(short, (T)v[i]);
-        *(s16x8*)p = a;
     }
 }
 
@@ -655,14 +662,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
 #pragma unroll
                     for (int q = 0; q < PASSES; ++q) {
                         const int64_t r = r8 + q * (64 / LANES);
-                        if constexpr (sizeof(TO) == 4)
-#pragma unroll 1
-                            for (int e = 0; e < 8; ++e) {
-                                float x = 0.0f;
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) x = i == e ? v[q][i] : x;
-                                if (!(fabsf(x) < __builtin_inff())) fix(v[q], e, whole_sum(p, bt, r, s8 + e));
-                            }
+                        if constexpr (sizeof(TO) == 4) make_whole(p, bt, r, s8, 8, v[q]);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[q][e] += bias[e];
                         if (p.e.pre) store8(static_cast<TO*>(p.e.pre) + r * p.e.pre_ld + s8, v[q]);
@@ -692,11 +692,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
                     *(f32x4*)q = *(f32x4*)v;
                     *(f32x4*)(q + 4) = *(f32x4*)(v + 4);
                 } else if constexpr (EPI == MM_LINEAR) {
-                    if constexpr (sizeof(TO) == 4)
-#pragma unroll 1
-                        for (int e = 0; e < n; ++e)
-                            if (!(fabsf(*(const float*)(at(row, lane % LANES * 2 + e / 4) + e % 4 * 4)) < __builtin_inff()))
-                                fix(v, e, whole_sum(p, bt, r, s + e));
+                    if constexpr (sizeof(TO) == 4) make_whole(p, bt, r, s, n, v);
                     store_linear<TO>(p.e, r, s, n, v);
                 } else {
                     store_orth(p, bt, r, s, n, v);
