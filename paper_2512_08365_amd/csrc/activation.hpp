@@ -5,14 +5,22 @@
 
 namespace mag {
 
-// (the hardware's reciprocal, off by one unit of the last place; 1 / inf = 0)
-__device__ __forceinline__ float logistic(float z)
-{
-    return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-}
-
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr float GELU_2K = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float GELU_C = 0.044715f;
+
+// 1 / (1 + 2^y), the logistic function of -y ln 2 (the hardware's exponential
+// and reciprocal, off by a unit of the last place each; 1 / inf = 0)
+__device__ __forceinline__ float logistic2(float y)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y));
+}
+__device__ __forceinline__ float logistic(float z) { return logistic2(-LOG2E * z); }
+// of 2 sqrt(2/pi) (z + 0.044715 z^3)
+__device__ __forceinline__ float gelu_logistic(float z)
+{
+    return logistic2(z * fmaf(-LOG2E * GELU_2K * GELU_C * z, z, -LOG2E * GELU_2K));
+}
 
 // The normal distribution's Phi(z) and, times sqrt(2 pi), its density: Abramowitz
 // and Stegun's formula 7.1.26 for the error function (off by 1.5e-7 at most), as
@@ -49,7 +57,7 @@ __device__ __forceinline__ void activate(float* z, int act)
             return v * normal(v, density);
         });
     case MAG_ACT_GELU_TANH:
-        return each<N>(z, [](float v) { return v * logistic(GELU_2K * (v + GELU_C * v * v * v)); });
+        return each<N>(z, [](float v) { return v * gelu_logistic(v); });
     case MAG_ACT_SILU: return each<N>(z, [](float v) { return v * logistic(v); });
     default: return;
     }
@@ -69,7 +77,7 @@ __device__ __forceinline__ void slopes(float* z, int act)
         });
     case MAG_ACT_GELU_TANH:
         return each<N>(z, [](float v) {
-            const float s = logistic(GELU_2K * (v + GELU_C * v * v * v));
+            const float s = gelu_logistic(v);
             return s + v * s * (1.0f - s) * GELU_2K * (1.0f + 3.0f * GELU_C * v * v);
         });
     case MAG_ACT_SILU:

@@ -342,7 +342,7 @@ int check_norm(const mag_norm_args* a)
 
 size_t norm_bytes(const mag_norm_args* a)
 {
-    return (size_t)mag::norm_parts(a->x.rows, a->x.cols) * 2 * (size_t)a->x.cols * 4;
+    return (size_t)mag::norm_parts(a->x.rows, a->x.cols, a->dtype) * 2 * (size_t)a->x.cols * 4;
 }
 
 // ------------------------------------------------------------- orthogonalize

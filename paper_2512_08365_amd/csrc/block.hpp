@@ -143,10 +143,10 @@ struct NormParams {
     float* rstd;
     void* dweight;
     void* dbias;
-    float* part;     // backward: [norm_parts(M, N)][2][N] sums over rows
+    float* part;     // backward: [norm_parts(...)][2][N] sums over rows
     float eps;
 };
-int norm_parts(int64_t M, int64_t N);
+int norm_parts(int64_t M, int64_t N, int dtype);
 hipError_t launch_norm(const NormParams& p, int dtype, int weight_dtype, hipStream_t stream);
 hipError_t launch_norm_backward(const NormParams& p, int dtype, int weight_dtype,
                                 hipStream_t stream);

@@ -72,7 +72,7 @@ __device__ __forceinline__ void pack_some(const PackParams& p, int64_t block, in
 {
     const int64_t per_row = width_of<T>(p.cols) / 8, n = p.rows * per_row;
     for (int64_t i = block * 256 + threadIdx.x; i < n; i += blocks * 256) {
-        const int64_t r = i / per_row, j = i % per_row * 8;
+        const int64_t r = quotient(i, per_row), j = (i - r * per_row) * 8;
         float v[8];
         get8(static_cast<const T*>(p.src) + r * p.rs, p.cs, j, p.cols, v);
         put8<T>(v, static_cast<short*>(p.dst) + r * p.ld, j);
@@ -128,24 +128,28 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
     }
 }
 
-// 64 columns' sums of the chunks' sums
+// 16 columns' sums of the chunks' sums, 16 threads each with all of their loads
+// in flight
+constexpr int SUM_COLS = 16;
 template <class T>
 __device__ __forceinline__ void column_sums(const ColumnSums& p, int64_t block)
 {
-    __shared__ float sums[4][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t j = block * 64 + lane;
+    __shared__ float sums[16][SUM_COLS + 1];
+    const int col = threadIdx.x % SUM_COLS, row = threadIdx.x / SUM_COLS;
+    const int64_t j = block * SUM_COLS + col;
     float s[8] = {};
     if (j < p.N)
-        for (int64_t c = wave; c < p.chunks; c += 32)
+        for (int64_t c = row; c < p.chunks; c += 128)
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-                if (c + 4 * u < p.chunks) s[u] += p.part[(c + 4 * u) * p.N + j];
-    sums[wave][lane] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+                if (c + 16 * u < p.chunks) s[u] += p.part[(c + 16 * u) * p.N + j];
+    sums[row][col] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
     __syncthreads();
-    if (wave == 0 && j < p.N)
-        static_cast<T*>(p.out)[j] =
-            (T)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
+    if (row || j >= p.N) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += sums[k][col];
+    static_cast<T*>(p.out)[j] = (T)sum;
 }
 
 // What a layer's products need beforehand, side by side in one launch (each is
@@ -168,7 +172,7 @@ __global__ __launch_bounds__(256) void k_mm_join(Mm p)
     const int64_t per_row = p.partial_ld / 8, n = p.R * per_row;
     const int64_t plane = p.R * p.partial_ld;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per_row, s = i % per_row * 8;
+        const int64_t r = quotient(i, per_row), s = (i - r * per_row) * 8;
         const float* q = p.partial + r * p.partial_ld + s;
         float v[8], w[8];
         load8(q, v);
@@ -193,7 +197,7 @@ hipError_t launch_prepare(const PackParams* a, const PackParams* b, const Column
     auto blocks = [](const PackParams* p) {
         return p ? blocks_for(p->rows * ((p->cols + 7) / 8)) : 0u;
     };
-    const unsigned na = blocks(a), nb = blocks(b), nc = c ? (unsigned)((c->N + 63) / 64) : 0u;
+    const unsigned na = blocks(a), nb = blocks(b), nc = c ? (unsigned)((c->N + SUM_COLS - 1) / SUM_COLS) : 0u;
     if (na + nb + nc == 0) return hipSuccess;
     const PackParams none{};
     const ColumnSums no{};
@@ -215,7 +219,7 @@ int64_t slope_chunks(int64_t M, int64_t N)
 {
     const int64_t across = (N + SLOPE_COLS - 1) / SLOPE_COLS;
     const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(across, 1));
-    return std::max<int64_t>(1, std::min<int64_t>(want, (M + 15) / 16));
+    return std::max<int64_t>(1, std::min<int64_t>(want, (M + 4 * SLOPE_ROWS - 1) / (4 * SLOPE_ROWS)));
 }
 
 hipError_t launch_slope(const SlopeParams& p, int dtype, hipStream_t stream)

@@ -313,6 +313,12 @@ __device__ __forceinline__ void store_linear(const Epilogue& e, int64_t r, int64
     }
 }
 
+// a / b of numbers >= 0: the 64-bit division takes some hundred instructions
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)
+{
+    return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 // v as the sum of two halves
 __device__ __forceinline__ void two_halves(float v, f16& hi, f16& lo)
 {

@@ -21,8 +21,8 @@ namespace {
 
 constexpr int HELD = 16;          // elements a thread
 constexpr int64_t MOST_HELD = 1024 * HELD;  // width of a row that 1,024 threads hold
-constexpr int BACK_WGS = 256;     // workgroups of 1,024 threads (half as many: twice this) of the
-                                  // backward pass, each with its own sums over rows
+constexpr int BACK_WGS = 256;     // workgroups of the backward pass, each with its own sums over
+                                  // rows (twice as many where a CU's registers hold two)
 
 // The G threads of a row hold V neighbours each, G V further on the next V, and
 // so on: 8 where the width is a multiple of 8 (the hardware takes vector loads
@@ -384,7 +384,7 @@ hipError_t backward(const NormParams& p, hipStream_t stream)
 {
     const bool sums = p.dweight || p.dbias;
     const bool wide = p.N > MOST_HELD || p.x_cs != 1 || p.dy_cs != 1;
-    const int parts = norm_parts(p.M, p.N);
+    const int parts = norm_parts(p.M, p.N, sizeof(T) == 4 ? MAG_F32 : MAG_BF16);
     if (wide && sums)
         hipLaunchKernelGGL(k_norm_back_wide_columns<T>, dim3((unsigned)((p.N + 255) / 256), parts),
                            dim3(256), 0, stream, p);
@@ -410,10 +410,11 @@ hipError_t backward(const NormParams& p, hipStream_t stream)
 
 }  // namespace
 
-int norm_parts(int64_t M, int64_t N)
+int norm_parts(int64_t M, int64_t N, int dtype)
 {
     // the rows spread evenly over the workgroups
-    const int64_t rows = back_rows(N), most = rows == 1 ? BACK_WGS : 2 * BACK_WGS;
+    const int64_t rows = back_rows(N);
+    const int64_t most = dtype != MAG_F32 && N % 8 == 0 && rows > 1 ? 2 * BACK_WGS : BACK_WGS;
     const int64_t groups = std::max<int64_t>(1, (M + rows - 1) / rows), rounds = (groups + most - 1) / most;
     return (int)((groups + rounds - 1) / rounds);
 }

@@ -20,7 +20,8 @@ __global__ __launch_bounds__(256) void k_orth_norm(OrthParams p)
     double s = 0.0;
     for (int64_t i = i0 + threadIdx.x; i < i1; i += 256) {
         float v[8];
-        get8(g + i / per_row * p.g_rs, p.g_cs, i % per_row * 8, p.cols, v);
+        const int64_t r = quotient(i, per_row);
+        get8(g + r * p.g_rs, p.g_cs, (i - r * per_row) * 8, p.cols, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s = fma((double)v[e], (double)v[e], s);
     }
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(256) void k_orth_scale(OrthParams p)
     const T* g = static_cast<const T*>(p.g) + bt * p.g_batch;
     const int64_t per_row = (p.cols + 31) / 32 * 4, n = p.rows * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per_row, j = i % per_row * 8;
+        const int64_t r = quotient(i, per_row), j = (i - r * per_row) * 8;
         h8 hi, lo;
         float x[8];
         get8(g + r * p.g_rs, p.g_cs, j, p.cols, x);
