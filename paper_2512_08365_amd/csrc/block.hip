@@ -95,12 +95,14 @@ bool same_shape(const mag_matrix& m, int64_t rows, int64_t cols)
 
 constexpr int64_t MOST_LD = 1LL << 22;  // 256 rows of it stay within 31 bits of bytes
 int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
-// elements of an operand's packed row of n
-int64_t packed_ld(int64_t n, int dtype) { return dtype == MAG_F32 ? (n + 31) / 32 * 96 : up8(n); }
+// bytes of an element of a product's operand (kind: MM_*), elements of a packed
+// row of n
+size_t part_size(int kind) { return kind == mag::MM_F32 ? 4 : 2; }
+int64_t packed_ld(int64_t n, int kind) { return kind == mag::MM_F32_PARTS ? (n + 31) / 32 * 96 : up8(n); }
 
 // How a product reads a matrix: where it lies, or as rows packed into the
-// workspace (fp32, which is cut into parts, and strides, alignments and widths
-// that the 16-byte loads do not take).
+// workspace (what is cut into parts, and strides, alignments and widths that the
+// 16-byte loads do not take).
 struct Operand {
     bool packed;
     size_t bytes;      // of the packed rows
@@ -108,14 +110,15 @@ struct Operand {
 };
 
 // along: the reduction runs along the matrix's columns (else along its rows)
-Operand operand(const mag_matrix& m, int dtype, bool along)
+Operand operand(const mag_matrix& m, int kind, bool along)
 {
     Operand o{};
-    if (dtype != MAG_F32 && aligned(m.data, 16)) {
-        const bool by_rows = (m.cols <= 1 || m.col_stride == 1) && m.cols % 8 == 0 &&
-                             (m.rows <= 1 || (m.row_stride % 8 == 0 && m.row_stride < MOST_LD));
-        const bool by_cols = m.row_stride == 1 && m.rows % 8 == 0 && m.rows > 1 &&
-                             (m.cols <= 1 || (m.col_stride % 8 == 0 && m.col_stride < MOST_LD));
+    if (kind != mag::MM_F32_PARTS && aligned(m.data, 16)) {
+        const int64_t per = 16 / (int64_t)part_size(kind);
+        const bool by_rows = (m.cols <= 1 || m.col_stride == 1) && m.cols % per == 0 &&
+                             (m.rows <= 1 || (m.row_stride % per == 0 && m.row_stride < MOST_LD));
+        const bool by_cols = m.row_stride == 1 && m.rows % per == 0 && m.rows > 1 &&
+                             (m.cols <= 1 || (m.col_stride % per == 0 && m.col_stride < MOST_LD));
         if (by_rows || by_cols) {
             o.op.p = m.data;
             o.op.ld = by_rows ? (m.rows <= 1 ? 0 : m.row_stride) : (m.cols <= 1 ? 0 : m.col_stride);
@@ -124,9 +127,9 @@ Operand operand(const mag_matrix& m, int dtype, bool along)
         }
     }
     o.packed = true;
-    o.op.ld = packed_ld(m.cols, dtype);
+    o.op.ld = packed_ld(m.cols, kind);
     o.op.mc = !along;
-    o.bytes = (size_t)(m.rows * o.op.ld * 2);
+    o.bytes = (size_t)(m.rows * o.op.ld) * part_size(kind);
     return o;
 }
 
@@ -147,6 +150,7 @@ mag::PackParams packing(const Operand& o, const mag_matrix& m)
 struct Shape {
     int tile;
     int splits;
+    double cost;   // estimated, in us
 };
 
 // What a workgroup's step, its tile beside the steps, and the call cost, in us,
@@ -158,11 +162,12 @@ struct TileCost {
 constexpr double CALL_COST = 2.5;
 constexpr double JOIN_COST = 3.5;           // a split product's second launch
 constexpr double PARTIAL_BYTES = 4.5e6;     // of partial sums a us, written or read
-const TileCost TILE_COST[4][mag::TILES] = {
+const TileCost TILE_COST[mag::MM_KINDS][mag::TILES] = {
     // 64 (four steps in LDS), 128, 256
     {{0.19, 0.35, 1.8}, {0.64, 0.80, 3.5}, {1.43, 0.0, 11.5}},   // bfloat16: 64 k a step
     {{0.19, 0.35, 1.8}, {0.64, 0.80, 3.5}, {1.43, 0.0, 11.5}},   // half
-    {{0.35, 0.0, 3.6}, {1.30, 0.0, 10.5}, {0.0, 0.0, 0.0}},      // three parts: 32 k, six products
+    {{0.53, 1.00, 1.8}, {0.0, 0.0, 0.0}, {0.0, 0.0, 0.0}},       // fp32: 32 k
+    {{0.35, 0.0, 3.6}, {1.20, 0.0, 10.5}, {0.0, 0.0, 0.0}},      // three parts: 32 k, six products
     {{0.22, 0.36, 1.8}, {0.73, 1.19, 6.5}, {2.13, 0.0, 10.5}},   // two parts: 32 k, three products
 };
 
@@ -173,10 +178,9 @@ const TileCost TILE_COST[4][mag::TILES] = {
 Shape choose(int64_t R, int64_t S, int64_t K, int kind, int64_t batch, bool symmetric)
 {
     constexpr int64_t CUS = 256;
-    const int64_t step = kind == mag::MM_F32 || kind == mag::MM_HALVES ? 32 : 64;
+    const int64_t step = kind == mag::MM_BF16 || kind == mag::MM_F16 ? 64 : 32;
     const int64_t steps = std::max<int64_t>(1, (K + step - 1) / step);
-    Shape best{mag::TILE_64, 1};
-    double least = 1e300;
+    Shape best{mag::TILE_64, 1, 1e300};
     for (int t = 0; t < mag::TILES; ++t) {
         const TileCost& c = TILE_COST[kind][t];
         if (c.alone == 0.0) continue;
@@ -185,35 +189,47 @@ Shape choose(int64_t R, int64_t S, int64_t K, int kind, int64_t batch, bool symm
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (s > 1 && (t == mag::TILE_256 || steps < 2 * s)) break;
             const int64_t wgs = tiles * s;
-            const bool shared = wgs > CUS && c.shared > 0.0;
-            const int64_t rounds = (wgs + (shared ? 2 : 1) * CUS - 1) / ((shared ? 2 : 1) * CUS);
-            double cost = CALL_COST + (double)rounds *
-                          ((double)((steps + s - 1) / s) * (shared ? c.shared : c.alone) + c.tile);
+            // rounds of two a CU where there is room; what is left has CUs of its own if
+            // the reduction is not split (of a split one, the same CUs' pairs go on)
+            const int64_t pairs = c.shared == 0.0 ? 0 : (wgs + (s > 1 && wgs > CUS ? 2 * CUS : CUS) - 1) / (2 * CUS);
+            const int64_t single = (std::max<int64_t>(wgs - pairs * 2 * CUS, 0) + CUS - 1) / CUS;
+            const double each = (double)((steps + s - 1) / s);
+            double cost = CALL_COST + (double)pairs * (each * c.shared + c.tile) +
+                          (double)single * (each * c.alone + c.tile);
             if (s > 1) cost += JOIN_COST + 2.0 * (double)s * (double)R * (double)S * (double)batch * 4.0 / PARTIAL_BYTES;
-            if (cost < least) {
-                least = cost;
-                best = Shape{t, s};
-            }
+            if (cost < best.cost) best = Shape{t, s, cost};
         }
     }
     return best;
 }
 
+// The products' kind without parts.
 int kind_of(int dtype)
 {
     return dtype == MAG_F32 ? mag::MM_F32 : dtype == MAG_F16 ? mag::MM_F16 : mag::MM_BF16;
 }
 
-int launch_linear(const mag::Mm& p, int dtype, int tile, hipStream_t stream)
+// What packing `n` elements costs, in us: a launch and its bytes (read, and
+// written whole or as three parts of two bytes).
+double packing_cost(int64_t n, int kind)
+{
+    if (n == 0) return 0.0;
+    return 3.0 + (double)n * (kind == mag::MM_F32_PARTS ? 10.0 : 8.0) / 6.5e6;
+}
+
+int launch_linear(const mag::Mm& p, int kind, int tile, hipStream_t stream)
 {
     if (p.splits > 1) {
-        TRY_HIP(mag::launch_mm_partial(p, kind_of(dtype), tile, stream), "product launch");
-        TRY_HIP(mag::launch_mm_join(p, dtype, stream), "join launch");
+        TRY_HIP(mag::launch_mm_partial(p, kind, tile, stream), "product launch");
+        TRY_HIP(mag::launch_mm_join(p, kind == mag::MM_F16 ? MAG_F16 : kind == mag::MM_BF16 ? MAG_BF16 : MAG_F32,
+                                    stream),
+                "join launch");
         return MAG_OK;
     }
-    TRY_HIP(dtype == MAG_F32 ? mag::launch_mm_f32(p, tile, stream)
-            : dtype == MAG_F16 ? mag::launch_mm_f16(p, tile, stream)
-                               : mag::launch_mm_bf16(p, tile, stream),
+    TRY_HIP(kind == mag::MM_F32_PARTS ? mag::launch_mm_f32_parts(p, tile, stream)
+            : kind == mag::MM_F32     ? mag::launch_mm_f32(p, stream)
+            : kind == mag::MM_F16     ? mag::launch_mm_f16(p, tile, stream)
+                                      : mag::launch_mm_bf16(p, tile, stream),
             "product launch");
     return MAG_OK;
 }
@@ -250,6 +266,7 @@ int check_linear(const mag_linear_args* a)
 }
 
 struct LinearPlan {
+    int kind;          // MM_*
     bool skinny;       // few rows: operands as they lie, one launch, no workspace
     bool across;       // the weight lies input by output
     Operand x, w;
@@ -264,9 +281,20 @@ size_t plan_linear(const mag_linear_args* a, void* ws, LinearPlan& pl)
     pl.skinny = a->x.rows <= mag::SKINNY_ROWS && (a->x.col_stride == 1 || a->x.cols <= 1) &&
                 (along || a->weight.row_stride == 1 || a->weight.rows <= 1);
     if (pl.skinny) return 0;
-    pl.x = operand(a->x, a->dtype, true);
-    pl.w = operand(a->weight, a->dtype, true);
-    pl.shape = choose(a->x.rows, a->weight.rows, a->x.cols, kind_of(a->dtype), 1, false);
+    double least = 1e300;
+    for (int kind : {kind_of(a->dtype), (int)mag::MM_F32_PARTS}) {
+        if (kind == mag::MM_F32_PARTS && a->dtype != MAG_F32) break;
+        const Operand x = operand(a->x, kind, true), w = operand(a->weight, kind, true);
+        const Shape s = choose(a->x.rows, a->weight.rows, a->x.cols, kind, 1, false);
+        const double cost = s.cost + packing_cost((x.packed ? a->x.rows * a->x.cols : 0) +
+                                                  (w.packed ? a->weight.rows * a->weight.cols : 0), kind);
+        if (cost >= least) break;
+        least = cost;
+        pl.kind = kind;
+        pl.x = x;
+        pl.w = w;
+        pl.shape = s;
+    }
     Carve c{static_cast<char*>(ws)};
     for (Operand* o : {&pl.x, &pl.w})
         if (o->packed) o->op.p = c.take(o->bytes);
@@ -277,6 +305,7 @@ size_t plan_linear(const mag_linear_args* a, void* ws, LinearPlan& pl)
 // ------------------------------------------------------------------ backward
 
 struct BackwardPlan {
+    int kind;         // MM_*
     Operand x, w, dy;
     bool own_dz;      // dz in the workspace (else dy is dz)
     mag::MmOperand dz;
@@ -288,25 +317,34 @@ struct BackwardPlan {
 size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& pl)
 {
     const int64_t M = a->x.rows, N = a->weight.rows, K = a->x.cols;
-    const int kind = kind_of(a->dtype);
-    // x and weight are both read across the reduction of the product they enter
-    pl.x = operand(a->x, a->dtype, false);
-    pl.w = operand(a->weight, a->dtype, false);
-    pl.dy = operand(a->dy, a->dtype, true);
+    double least = 1e300;
+    for (int kind : {kind_of(a->dtype), (int)mag::MM_F32_PARTS}) {
+        if (kind == mag::MM_F32_PARTS && a->dtype != MAG_F32) break;
+        // x and weight are both read across the reduction of the product they enter
+        const Operand x = operand(a->x, kind, false), w = operand(a->weight, kind, false);
+        const Shape dx = choose(M, K, N, kind, 1, false), dw = choose(N, K, M, kind, 1, false);
+        const double cost = dx.cost + dw.cost + packing_cost((x.packed ? M * K : 0) + (w.packed ? N * K : 0), kind);
+        if (cost >= least) break;
+        least = cost;
+        pl.kind = kind;
+        pl.x = x;
+        pl.w = w;
+        pl.dx = dx;
+        pl.dw = dw;
+    }
+    pl.dy = operand(a->dy, pl.kind, true);
     // (as for the sizes: room for dz whether or not dy can stand in for it)
     pl.own_dz = a->activation != MAG_ACT_NONE || pl.dy.packed || !a->dy.data;
     if (pl.own_dz) {
         pl.dz = mag::MmOperand{};
-        pl.dz.ld = packed_ld(N, a->dtype);
+        pl.dz.ld = packed_ld(N, pl.kind);
     } else {
         pl.dz = pl.dy.op;
     }
-    pl.dx = choose(M, K, N, kind, 1, false);
-    pl.dw = choose(N, K, M, kind, 1, false);
     Carve c{static_cast<char*>(ws)};
     for (Operand* o : {&pl.x, &pl.w})
         if (o->packed) o->op.p = c.take(o->bytes);
-    void* dz = c.take((size_t)(M * packed_ld(N, a->dtype) * 2));
+    void* dz = c.take((size_t)(M * packed_ld(N, pl.kind)) * part_size(pl.kind));
     if (pl.own_dz) pl.dz.p = dz;
     pl.column_part = c.take<float>((size_t)(mag::slope_chunks(M, N) * N * 4));
     pl.partial = c.take<float>(std::max(partial_bytes(M, K, pl.dx), partial_bytes(N, K, pl.dw)));
@@ -481,9 +519,10 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     }
     const mag::PackParams px = packing(pl.x, a->x), pw = packing(pl.w, a->weight);
     TRY_HIP(mag::launch_prepare(pl.x.packed ? &px : nullptr, pl.w.packed ? &pw : nullptr, nullptr,
-                                a->dtype, stream),
+                                pl.kind, stream),
             "linear launch");
     mag::Mm p{};
+    p.in_parts = pl.kind == mag::MM_F32_PARTS;
     p.a = pl.x.op;
     p.b = pl.w.op;
     p.R = M;
@@ -495,7 +534,7 @@ int mag_linear(const mag_linear_args* a, void* workspace, size_t workspace_bytes
     p.partial_ld = up8(N);
     p.e = e;
     p.e.vec = !e.res || e.res_cs == 1;
-    return launch_linear(p, a->dtype, pl.shape.tile, stream);
+    return launch_linear(p, pl.kind, pl.shape.tile, stream);
 }
 
 int mag_linear_backward_workspace_size(const mag_linear_backward_args* args, size_t* bytes)
@@ -555,15 +594,16 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         s.ldz = pl.dz.ld;
         s.dbias = a->dbias;
         s.part = pl.column_part;
-        TRY_HIP(mag::launch_slope(s, a->dtype, stream), "linear_backward launch");
+        TRY_HIP(mag::launch_slope(s, pl.kind, stream), "linear_backward launch");
     }
     const bool dx = a->dx.data && M > 0 && K > 0, dw = a->dweight.data && N > 0 && K > 0;
     const mag::PackParams px = packing(pl.x, a->x), pw = packing(pl.w, a->weight);
     const mag::ColumnSums sums{pl.column_part, mag::slope_chunks(M, N), N, a->dbias};
     TRY_HIP(mag::launch_prepare(dw && pl.x.packed ? &px : nullptr, dx && pl.w.packed ? &pw : nullptr,
-                                a->dbias ? &sums : nullptr, a->dtype, stream),
+                                a->dbias ? &sums : nullptr, pl.kind, stream),
             "linear_backward launch");
     mag::Mm p{};
+    p.in_parts = pl.kind == mag::MM_F32_PARTS;
     p.batch = 1;
     p.partial = pl.partial;
     p.S = K;
@@ -577,7 +617,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         p.e.y = a->dx.data;
         p.e.y_ld = a->dx.row_stride;
         p.e.vec = 1;
-        TRY(launch_linear(p, a->dtype, pl.dx.tile, stream));
+        TRY(launch_linear(p, pl.kind, pl.dx.tile, stream));
     }
     if (dw) {
         p.a.mc = !pl.dz.mc;
@@ -588,7 +628,7 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         p.e.y = a->dweight.data;
         p.e.y_ld = a->dweight.row_stride;
         p.e.vec = 1;
-        TRY(launch_linear(p, a->dtype, pl.dw.tile, stream));
+        TRY(launch_linear(p, pl.kind, pl.dw.tile, stream));
     }
     return MAG_OK;
 }

@@ -15,8 +15,8 @@ using bf16 = __bf16;
 using f16 = _Float16;
 
 // An operand of a product: element (row, k) at row * ld + k, or with mc at k *
-// ld + row (elements of two bytes; data and rows at multiples of 16 bytes, and
-// the run that is contiguous a multiple of 8 or zero-padded to one).  In P = 2 or
+// ld + row (data and rows at multiples of 16 bytes, and the run that is
+// contiguous a multiple of 16 bytes or zero-padded to one).  In P = 2 or
 // 3 parts, that run has 32 elements' first parts, then their second ones, and so
 // on, zero-padded to whole 32s, and ld counts all of them.
 struct MmOperand {
@@ -57,6 +57,7 @@ struct Mm {
     int64_t R, S, K;
     int32_t batch;
     int32_t splits;       // of the reduction, each with its own sums in `partial`
+    int32_t in_parts;     // fp32 operands in three parts: sums that are not finite are retaken
     int32_t symmetric;    // tiles on and above the diagonal only, mirrored (R = S)
     float* partial;       // [batch][splits][R][partial_ld]
     int64_t partial_ld;
@@ -66,14 +67,15 @@ struct Mm {
 enum { MM_LINEAR, MM_PARTIAL, MM_ORTH };
 enum { TILE_64, TILE_128, TILE_256, TILES };
 constexpr int64_t TILE_SIDE[TILES] = {64, 128, 256};
-// what a product is made of: operands and result of bfloat16 or half; fp32
+// what a product is made of: operands and result of bfloat16, half or fp32; fp32
 // operands in three bfloat16 parts; an update's in two half parts
-enum { MM_BF16, MM_F16, MM_F32, MM_HALVES };
+enum { MM_BF16, MM_F16, MM_F32, MM_F32_PARTS, MM_HALVES, MM_KINDS };
 // tile: TILE_*
 hipError_t launch_mm_bf16(const Mm& p, int tile, hipStream_t stream);
 hipError_t launch_mm_f16(const Mm& p, int tile, hipStream_t stream);
-hipError_t launch_mm_f32(const Mm& p, int tile, hipStream_t stream);   // (no 256 tile)
-// kind: MM_BF16 ... (no 256 tile)
+hipError_t launch_mm_f32(const Mm& p, hipStream_t stream);                   // (64 alone)
+hipError_t launch_mm_f32_parts(const Mm& p, int tile, hipStream_t stream);   // (no 256 tile)
+// kind: MM_BF16 ... (tiles as above, no 256)
 hipError_t launch_mm_partial(const Mm& p, int kind, int tile, hipStream_t stream);
 hipError_t launch_mm_orth(const Mm& p, int tile, hipStream_t stream);
 // the partial sums of a split product added up and stored (dtype: of y)
@@ -94,8 +96,8 @@ struct SkinnyParams {
 };
 hipError_t launch_skinny(const SkinnyParams& p, int dtype, hipStream_t stream);
 
-// rows x cols values of any strides as an operand's rows of ld elements: two-byte
-// types as they are, fp32 in three bfloat16 parts
+// rows x cols values of any strides as an operand's rows of ld elements: as they
+// are, or fp32 in three bfloat16 parts
 struct PackParams {
     const void* src;
     int64_t rs, cs;
@@ -110,7 +112,8 @@ struct ColumnSums {
     void* out;
 };
 // two matrices packed and column sums finished, any of them NULL: one launch
-hipError_t launch_prepare(const PackParams* a, const PackParams* b, const ColumnSums* c, int dtype,
+// (kind: MM_*, of the products that follow)
+hipError_t launch_prepare(const PackParams* a, const PackParams* b, const ColumnSums* c, int kind,
                           hipStream_t stream);
 
 // dz = dy act'(pre), and with dbias the column sums of dz by chunks of rows
@@ -121,13 +124,13 @@ struct SlopeParams {
     int64_t pre_rs, pre_cs;
     int64_t M, N;
     int32_t act;
-    void* dz;        // NULL: not wanted; an operand's rows (fp32: three parts)
+    void* dz;        // NULL: not wanted; an operand's rows
     int64_t ldz;
     void* dbias;     // NULL: not wanted
     float* part;     // [slope_chunks(M)][N] column sums of the chunks of rows
 };
 int64_t slope_chunks(int64_t M, int64_t N);
-hipError_t launch_slope(const SlopeParams& p, int dtype, hipStream_t stream);
+hipError_t launch_slope(const SlopeParams& p, int kind, hipStream_t stream);
 
 struct NormParams {
     const void* x;

@@ -33,12 +33,13 @@ __device__ __forceinline__ void three_parts(float v, short& a, short& b, short& 
     c = bits((bf16)(r - (float)m));
 }
 
-// eight neighbours of a row, from element j of it, into an operand's row
-template <class T>
-__device__ __forceinline__ void put8(const float* v, short* row, int64_t j)
+// eight neighbours of row r, from element j of it, into an operand's rows (PARTS:
+// in three parts)
+template <class T, bool PARTS>
+__device__ __forceinline__ void put8(const float* v, void* rows, int64_t ld, int64_t r, int64_t j)
 {
     h8 o;
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (PARTS) {
         h8 m, l;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -48,34 +49,32 @@ __device__ __forceinline__ void put8(const float* v, short* row, int64_t j)
             m[i] = b;
             l[i] = c;
         }
-        short* d = row + place<3>(j);
+        short* d = static_cast<short*>(rows) + r * ld + place<3>(j);
         *(h8*)d = o;
         *(h8*)(d + 32) = m;
         *(h8*)(d + 64) = l;
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = __builtin_bit_cast(short, (T)v[i]);
-        *(h8*)(row + j) = o;
+        store8(static_cast<T*>(rows) + r * ld + j, v);
     }
 }
 
 // elements of an operand's row of n, without the parts
-template <class T>
+template <bool PARTS>
 __host__ __device__ int64_t width_of(int64_t n)
 {
-    return sizeof(T) == 4 ? (n + 31) / 32 * 32 : (n + 7) / 8 * 8;
+    return PARTS ? (n + 31) / 32 * 32 : (n + 7) / 8 * 8;
 }
 
 // One thread's 8 neighbours of a packed row.
-template <class T>
+template <class T, bool PARTS>
 __device__ __forceinline__ void pack_some(const PackParams& p, int64_t block, int64_t blocks)
 {
-    const int64_t per_row = width_of<T>(p.cols) / 8, n = p.rows * per_row;
+    const int64_t per_row = width_of<PARTS>(p.cols) / 8, n = p.rows * per_row;
     for (int64_t i = block * 256 + threadIdx.x; i < n; i += blocks * 256) {
         const int64_t r = quotient(i, per_row), j = (i - r * per_row) * 8;
         float v[8];
         get8(static_cast<const T*>(p.src) + r * p.rs, p.cs, j, p.cols, v);
-        put8<T>(v, static_cast<short*>(p.dst) + r * p.ld, j);
+        put8<T, PARTS>(v, p.dst, p.ld, r, j);
     }
 }
 
@@ -85,7 +84,7 @@ constexpr int SLOPE_ROWS = 2;    // rows a wave has in flight (4: too many regis
 // dz and the column sums of one chunk of rows: four waves take its rows in
 // turn, 8 columns a lane, and add their sums up in LDS at the end.  Bound by
 // memory (a prompt's 805 MB in 170 us).
-template <class T>
+template <class T, bool PARTS>
 __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
 {
     __shared__ float sums[4][SLOPE_COLS + 4];
@@ -94,7 +93,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
     const int64_t i0 = (int64_t)blockIdx.y * chunk, i1 = min(i0 + chunk, p.M);
     const bool acts = p.act != MAG_ACT_NONE;
     float sum[8] = {};
-    if (j < width_of<T>(p.N))
+    if (j < width_of<PARTS>(p.N))
         for (int64_t i = i0 + wave; i < i1; i += 4 * SLOPE_ROWS) {
             float d[SLOPE_ROWS][8], z[SLOPE_ROWS][8];
 #pragma unroll
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
                 if (i + 4 * u >= i1) break;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += d[u][e];
-                if (p.dz) put8<T>(d[u], static_cast<short*>(p.dz) + (i + 4 * u) * p.ldz, j);
+                if (p.dz) put8<T, PARTS>(d[u], p.dz, p.ldz, i + 4 * u, j);
             }
         }
     if (!p.dbias) return;
@@ -154,14 +153,14 @@ __device__ __forceinline__ void column_sums(const ColumnSums& p, int64_t block)
 
 // What a layer's products need beforehand, side by side in one launch (each is
 // a few us of latency): up to two matrices packed and the column sums finished.
-template <class T>
+template <class T, bool PARTS>
 __global__ __launch_bounds__(256) void k_prepare(PackParams a, PackParams b, ColumnSums c,
                                                  uint32_t blocks_a, uint32_t blocks_b)
 {
     if (blockIdx.x < blocks_a)
-        pack_some<T>(a, blockIdx.x, blocks_a);
+        pack_some<T, PARTS>(a, blockIdx.x, blocks_a);
     else if (blockIdx.x < blocks_a + blocks_b)
-        pack_some<T>(b, blockIdx.x - blocks_a, blocks_b);
+        pack_some<T, PARTS>(b, blockIdx.x - blocks_a, blocks_b);
     else
         column_sums<T>(c, blockIdx.x - blocks_a - blocks_b);
 }
@@ -182,7 +181,8 @@ __global__ __launch_bounds__(256) void k_mm_join(Mm p)
             for (int e = 0; e < 8; ++e) v[e] += w[e];
         }
         const int m = (int)min((int64_t)8, p.S - s);
-        if constexpr (sizeof(TO) == 4) make_whole(p, 0, r, s, m, v);
+        if constexpr (sizeof(TO) == 4)
+            if (p.in_parts) make_whole(p, 0, r, s, m, v);
         store_linear<TO>(p.e, r, s, m, v);
     }
 }
@@ -191,7 +191,7 @@ unsigned blocks_for(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 
 
 }  // namespace
 
-hipError_t launch_prepare(const PackParams* a, const PackParams* b, const ColumnSums* c, int dtype,
+hipError_t launch_prepare(const PackParams* a, const PackParams* b, const ColumnSums* c, int kind,
                           hipStream_t stream)
 {
     auto blocks = [](const PackParams* p) {
@@ -202,15 +202,15 @@ hipError_t launch_prepare(const PackParams* a, const PackParams* b, const Column
     const PackParams none{};
     const ColumnSums no{};
     const dim3 grid(na + nb + nc), block(256);
-    if (dtype == MAG_F32)
-        hipLaunchKernelGGL(k_prepare<float>, grid, block, 0, stream, a ? *a : none, b ? *b : none,
-                           c ? *c : no, na, nb);
-    else if (dtype == MAG_F16)
-        hipLaunchKernelGGL(k_prepare<f16>, grid, block, 0, stream, a ? *a : none, b ? *b : none,
-                           c ? *c : no, na, nb);
-    else
-        hipLaunchKernelGGL(k_prepare<bf16>, grid, block, 0, stream, a ? *a : none, b ? *b : none,
-                           c ? *c : no, na, nb);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, stream, a ? *a : none, b ? *b : none, c ? *c : no, na, nb);
+    };
+    switch (kind) {
+    case MM_F32: launch(k_prepare<float, false>); break;
+    case MM_F32_PARTS: launch(k_prepare<float, true>); break;
+    case MM_F16: launch(k_prepare<f16, false>); break;
+    default: launch(k_prepare<bf16, false>); break;
+    }
     return hipGetLastError();
 }
 
@@ -222,17 +222,18 @@ int64_t slope_chunks(int64_t M, int64_t N)
     return std::max<int64_t>(1, std::min<int64_t>(want, (M + 4 * SLOPE_ROWS - 1) / (4 * SLOPE_ROWS)));
 }
 
-hipError_t launch_slope(const SlopeParams& p, int dtype, hipStream_t stream)
+hipError_t launch_slope(const SlopeParams& p, int kind, hipStream_t stream)
 {
     if (p.N == 0) return hipSuccess;
     const int64_t chunks = slope_chunks(p.M, p.N), chunk = (p.M + chunks - 1) / chunks;
     const dim3 grid((unsigned)((p.N + SLOPE_COLS - 1) / SLOPE_COLS), (unsigned)chunks), block(256);
-    if (dtype == MAG_F32)
-        hipLaunchKernelGGL(k_slope<float>, grid, block, 0, stream, p, chunk);
-    else if (dtype == MAG_F16)
-        hipLaunchKernelGGL(k_slope<f16>, grid, block, 0, stream, p, chunk);
-    else
-        hipLaunchKernelGGL(k_slope<bf16>, grid, block, 0, stream, p, chunk);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, chunk); };
+    switch (kind) {
+    case MM_F32: launch(k_slope<float, false>); break;
+    case MM_F32_PARTS: launch(k_slope<float, true>); break;
+    case MM_F16: launch(k_slope<f16, false>); break;
+    default: launch(k_slope<bf16, false>); break;
+    }
     return hipGetLastError();
 }
 

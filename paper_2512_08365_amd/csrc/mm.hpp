@@ -17,7 +17,7 @@ typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 template <class T>
 __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c)
 {
-    if constexpr (sizeof(T) == 2 && __is_same(T, bf16))
+    if constexpr (__is_same(T, bf16))
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                        __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     else
@@ -39,10 +39,11 @@ __device__ __forceinline__ void mfma_in_place(s16x8 a, s16x8 b, f32x4& c)
 }
 
 // ------------------------------------------------------------------- operands
-// A tile of an operand is a step of the reduction (64 k; of operands in P = 2 or
-// 3 parts, which lie 32 k of each part after another in memory, 32) by ROWS rows
-// of the output, in LDS as 16-byte chunks of 8 elements, filled by loads that go
-// from memory to LDS without registers.  Such a load writes 64 chunks one after
+// A tile of an operand is a step of the reduction (128 bytes, 64 k of two bytes;
+// of operands in P = 2 or 3 parts, which lie 32 k of each part after another in
+// memory, 32 k) by ROWS rows of the output, in LDS as 16-byte chunks of 8
+// elements (fp32: 4), filled by loads that go from memory to LDS without
+// registers.  Such a load writes 64 chunks one after
 // another, so a permutation against bank conflicts is made in what each lane
 // reads.
 //   along k (MC false): element (row, k) at row * ld + k.  An LDS row has the 8 or
@@ -51,25 +52,30 @@ __device__ __forceinline__ void mfma_in_place(s16x8 a, s16x8 b, f32x4& c)
 //     are: 8 consecutive k of a row a lane.
 //   along rows (MC true): element at k * ld + row.  An LDS row is one k; chunk c
 //     of it sits at c ^ mc_swizzle(k).  Read through the transposing LDS load: 16
-//     lanes hand in 4 steps of 16 rows and get 4 consecutive k of a row each.
+//     lanes hand in 4 steps of 16 rows and get 4 consecutive k of a row each (fp32:
+//     one number at a time, the chunks of lanes 16 apart in other banks).
 constexpr uint32_t NOWHERE = 0x80000000u;    // a buffer offset past every extent: reads zeros
 
-constexpr int step_of(int P) { return P == 1 ? 64 : 32; }
+template <class T>
+constexpr int step_of(int P) { return P == 1 ? 128 / (int)sizeof(T) : 32; }
 
 // what chunk c of step k is XORed with: 16 lanes read 4 steps' 32 bytes each, 32
-// lanes those of 8 steps further on too (CH: chunks of an LDS row)
-template <int CH>
+// lanes those of 8 steps further on too (CH: chunks of an LDS row); of fp32, 64
+// lanes read 4 steps' 64 bytes, 4 steps apart
+template <class T, int CH>
 __device__ __forceinline__ int mc_swizzle(int k)
 {
+    if constexpr (sizeof(T) == 4) return k & 12;
     return 2 * ((k & 3) | (CH % 16 == 0 ? k >> 1 & 4 : 0));
 }
 
-template <int ROWS, bool MC, int P, int THREADS>
+template <class T, int ROWS, bool MC, int P, int THREADS>
 struct Tile {
-    static constexpr int STEP = step_of(P);
-    static constexpr int BYTES = ROWS * STEP * P * 2;
+    static constexpr int STEP = step_of<T>(P);
+    static constexpr int SIZE = sizeof(T), PER = 16 / SIZE;   // elements a chunk
+    static constexpr int BYTES = ROWS * STEP * P * SIZE;
     static constexpr int LOADS = BYTES / 16 / THREADS;        // chunks a thread
-    static constexpr int CH = (MC ? ROWS : STEP) * P / 8;     // chunks an LDS row
+    static constexpr int CH = (MC ? ROWS : STEP) * P / PER;   // chunks an LDS row
 
     // whether the thread's chunks lie alike in their lines
     static constexpr bool ALIKE = THREADS % CH == 0;
@@ -81,12 +87,12 @@ struct Tile {
     static __device__ __forceinline__ int first(int i)
     {
         const int f = i * THREADS + (int)threadIdx.x, line = f / CH;
-        return MC ? line : source(line, f % CH) * 8 % STEP;
+        return MC ? line : source(line, f % CH) * PER % STEP;
     }
     // the chunk that lies at `pos` of a line
     static __device__ __forceinline__ int source(int line, int pos)
     {
-        return pos ^ (MC ? mc_swizzle<CH>(line) : P == 3 ? line >> 1 & 3 : line & 7);
+        return pos ^ (MC ? mc_swizzle<T, CH>(line) : P == 3 ? line >> 1 & 3 : line & 7);
     }
 
     // rows of the operand from this tile's first one on; ld in elements
@@ -100,11 +106,11 @@ struct Tile {
             if (i < (ALIKE ? 1 : LOADS)) k0[i] = first(i);
             // (rows past the last one: any others, nothing of theirs is stored)
             if constexpr (MC) {
-                if ((int64_t)c * 8 >= padded(rows_left)) c = 0;
-                off[i] = (uint32_t)(line * ld * 2 + c * 16);
+                if ((int64_t)c * PER >= padded(rows_left)) c = 0;
+                off[i] = (uint32_t)(line * ld * SIZE + c * 16);
             } else {
                 const int64_t r = line < rows_left ? line : rows_left - 1;
-                off[i] = (uint32_t)(r * ld * 2 + c * 16);
+                off[i] = (uint32_t)(r * ld * SIZE + c * 16);
             }
         }
     }
@@ -127,12 +133,12 @@ struct Tile {
     }
 };
 
-// Fragments of a wave's part of a tile: 16 rows, 32 k; row lane % 16, k 8 (lane /
-// 16) on.  What depends on the lane is worked out once, the rest is the load's
+// Fragments of a wave's part of a tile: 16 rows, 32 k (fp32: 16); row lane % 16, k
+// 8 (lane / 16) on (fp32: 4 (lane / 16)).  What depends on the lane is worked out once, the rest is the load's
 // own constant offset.
-template <int ROWS, bool MC, int P>
+template <class T, int ROWS, bool MC, int P>
 struct Reader {
-    static constexpr int LINE = (MC ? ROWS : step_of(P)) * P * 2;  // bytes of an LDS row
+    static constexpr int LINE = (MC ? ROWS : step_of<T>(P)) * P * (int)sizeof(T);  // bytes of an LDS row
     // along rows: what repeats from 16 rows to 16 rows (the swizzle XORs up to 16
     // chunks: 128 rows, or 32 P-part ones a 64-byte part)
     static constexpr int CYCLE = P == 1 ? 8 : P == 2 ? 4 : 8;
@@ -152,7 +158,14 @@ struct Reader {
     __device__ __forceinline__ void init(int row)
     {
         const int lane = (int)threadIdx.x & 63, q = lane & 15;
-        if constexpr (MC) {
+        if constexpr (MC && sizeof(T) == 4) {
+            const int k = (lane >> 4) * 4;
+#pragma unroll
+            for (int i = 0; i < KEPT_I; ++i) {
+                const int n = row + 16 * i + q;
+                at[i] = k * LINE + (((n >> 2) ^ mc_swizzle<T, LINE / 16>(k)) << 4) + (n & 3) * 4;
+            }
+        } else if constexpr (MC) {
             const int k = (lane >> 4) * 8 + (q >> 2), b = (q & 3) >> 1;
 #pragma unroll
             for (int i = 0; i < KEPT_I; ++i)
@@ -162,7 +175,7 @@ struct Reader {
                     const int c = (P == 1 ? n / 8 : n / 32 * (4 * P) + s * 4 + n % 32 / 8) + b;
                     // (k + 4 and, of one part, k + 32 have the same place in their rows)
                     at[i * (P == 1 ? 1 : P) + s] =
-                        k * LINE + ((c ^ mc_swizzle<LINE / 16>(k)) << 4) + ((q & 1) << 3);
+                        k * LINE + ((c ^ mc_swizzle<T, LINE / 16>(k)) << 4) + ((q & 1) << 3);
                 }
         } else if constexpr (P == 3) {
             at[0] = (row + q) * LINE + (((lane >> 4) ^ (q >> 1 & 3)) << 4);
@@ -176,7 +189,14 @@ struct Reader {
     // rows 16 i on; s: half of a step, or part
     __device__ __forceinline__ s16x8 get(const char* lds, int i, int s) const
     {
-        if constexpr (MC) {
+        if constexpr (MC && sizeof(T) == 4) {
+            static_assert(KEPT_I * 32 == ROWS, "");
+            const char* p = lds + at[i] + s * 16 * LINE;
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = *(const float*)(p + e * LINE);
+            return __builtin_bit_cast(s16x8, v);
+        } else if constexpr (MC) {
             const char* p = lds + at[i % KEPT_I * (P == 1 ? 1 : P) + (P == 1 ? 0 : s)] +
                             (i / KEPT_I * KEPT_I * 32 * P + (P == 1 ? s * 32 * LINE : 0));
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -419,10 +439,11 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int THREADS = 256, W = 2;          // 2 x 2 waves
     constexpr int COLS = SIDE / W, F = COLS / 16;  // a wave's rows and columns, in 16s
-    constexpr int STEP = step_of(P);
+    constexpr int STEP = step_of<T>(P);
+    constexpr int SIZE = sizeof(T);
     constexpr bool IN_PLACE = F >= 8;
-    using TA = Tile<SIDE, AMC, P, THREADS>;
-    using TB = Tile<SIDE, BMC, P, THREADS>;
+    using TA = Tile<T, SIDE, AMC, P, THREADS>;
+    using TB = Tile<T, SIDE, BMC, P, THREADS>;
     constexpr int L = TA::LOADS;
     static_assert(TA::LOADS == TB::LOADS, "");
     // each tile an array of its own: what one is read from is not what is being
@@ -443,13 +464,13 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
     const int64_t steps = (p.K + STEP - 1) / STEP;
     const int64_t t0 = steps * blockIdx.y / p.splits, t1 = steps * (blockIdx.y + 1) / p.splits;
     const int count = (int)(t1 - t0);
-    const int64_t a_step = AMC ? STEP * p.a.ld * 2 : STEP * P * 2;
-    const int64_t b_step = BMC ? STEP * p.b.ld * 2 : STEP * P * 2;
+    const int64_t a_step = AMC ? STEP * p.a.ld * SIZE : STEP * P * SIZE;
+    const int64_t b_step = BMC ? STEP * p.b.ld * SIZE : STEP * P * SIZE;
 
     TA ta;
     TB tb;
-    Reader<SIDE, AMC, P> ra;
-    Reader<SIDE, BMC, P> rb;
+    Reader<T, SIDE, AMC, P> ra;
+    Reader<T, SIDE, BMC, P> rb;
     ra.init(wr);
     rb.init(ws);
     int64_t r0, s0;
@@ -480,8 +501,8 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
         s0 = (int64_t)tj * SIDE;
         ta.init(p.a.ld, p.R - r0);
         tb.init(p.b.ld, p.S - s0);
-        pa = static_cast<const char*>(p.a.p) + 2 * (bt * p.a.batch + (AMC ? r0 * P : r0 * p.a.ld)) + t0 * a_step;
-        pb = static_cast<const char*>(p.b.p) + 2 * (bt * p.b.batch + (BMC ? s0 * P : s0 * p.b.ld)) + t0 * b_step;
+        pa = static_cast<const char*>(p.a.p) + SIZE * (bt * p.a.batch + (AMC ? r0 * P : r0 * p.a.ld)) + t0 * a_step;
+        pb = static_cast<const char*>(p.b.p) + SIZE * (bt * p.b.batch + (BMC ? s0 * P : s0 * p.b.ld)) + t0 * b_step;
         k_left = (int)(min(p.K, t1 * STEP) - t0 * STEP);
         load(la0, lb0);
         load(la1, lb1);
@@ -500,6 +521,16 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
     using None = std::integral_constant<int, 0>;
     using Ahead = std::integral_constant<int, STAGES - 2>;
     auto products = [&](const s16x8& a, const s16x8* b, int i) {
+        if constexpr (SIZE == 4) {
+            const f32x4 x = __builtin_bit_cast(f32x4, a);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < F; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, b[j])[k], x[k],
+                                                                     acc[i][j], 0, 0, 0);
+            return;
+        } else
 #pragma unroll
         for (int j = 0; j < F; ++j) {
             // (b first: a lane then holds four neighbours of one output row)
@@ -618,7 +649,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
         }
         meet(None{});
         settle();
-    const int64_t rt = r0 + wr, st = s0 + ws;
+        const int64_t rt = r0 + wr, st = s0 + ws;
         const bool mirrored = mirror;
         g += gridDim.x;
         if (g < tiles) begin_tile(g);
@@ -668,7 +699,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
 #pragma unroll
                     for (int q = 0; q < PASSES; ++q) {
                         const int64_t r = r8 + q * (64 / LANES);
-                        if constexpr (sizeof(TO) == 4) make_whole(p, bt, r, s8, 8, v[q]);
+                        if constexpr (P == 3) make_whole(p, bt, r, s8, 8, v[q]);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[q][e] += bias[e];
                         if (p.e.pre) store8(static_cast<TO*>(p.e.pre) + r * p.e.pre_ld + s8, v[q]);
@@ -698,7 +729,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
                     *(f32x4*)q = *(f32x4*)v;
                     *(f32x4*)(q + 4) = *(f32x4*)(v + 4);
                 } else if constexpr (EPI == MM_LINEAR) {
-                    if constexpr (sizeof(TO) == 4) make_whole(p, bt, r, s, n, v);
+                    if constexpr (P == 3) make_whole(p, bt, r, s, n, v);
                     store_linear<TO>(p.e, r, s, n, v);
                 } else {
                     store_orth(p, bt, r, s, n, v);

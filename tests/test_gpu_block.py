@@ -265,6 +265,48 @@ def test_linear_not_finite_values_stay_in_their_rows(rows, ty):
         assert bool(torch.isposinf(y[:, 2]).all())
 
 
+# fp32 products of many tiles, which are taken in parts: short and long reductions
+FLOAT_SIZES = [(1000, 2050, 777), (2048, 1024, 4096), (512, 8192, 1024)]
+
+
+@pytest.mark.parametrize("size", FLOAT_SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_linear_float_large_not_finite_values(size):
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    rows, inner, outer = size
+    g = _gen(16)
+    x = _normal(g, (rows, inner), 1.0, torch.float32)
+    w = _normal(g, (outer, inner), 0.1, torch.float32)
+    w[3, 7] = 0.0
+    w[5] = 0.5
+    ref = mag.linear(x, w)
+    bad = x.clone()
+    bad[0, 7] = float("inf")
+    bad[rows - 1, inner - 1] = float("nan")
+    y = mag.linear(bad, w)
+    want = torch.mm(bad[:1].double(), w.double().t().contiguous())
+    assert torch.equal(y[1:rows - 1], ref[1:rows - 1])
+    assert bool(torch.isnan(y[rows - 1]).all())
+    assert torch.equal(torch.isnan(y[:1]), torch.isnan(want))
+    assert torch.equal(y[:1][torch.isinf(want)].double(), want[torch.isinf(want)])
+    x.zero_()
+    x[:, 0] = 3.3e38
+    w.zero_()
+    w[:, 0] = 1.0
+    w[outer - 1, 0] = -1.0
+    w[2, 0] = 4.0
+    y = mag.linear(x, w)
+    assert bool((y[:, 0] == 3.3e38).all()) and bool((y[:, outer - 1] == -3.3e38).all())
+    assert bool(torch.isposinf(y[:, 2]).all())
+
+
+@pytest.mark.parametrize("layout", ["gap", "columns", "every2"])
+@pytest.mark.parametrize("size", FLOAT_SIZES[:2], ids=lambda s: "x".join(map(str, s)))
+def test_linear_float_large_layouts(size, layout):
+    check_linear(*size, "f32", act="relu", lx=layout, lw=LAYOUTS[5 - LAYOUTS.index(layout)])
+    check_linear_backward(*size, "f32", act="silu", lx=layout, lw="columns", ld=layout)
+
+
 @pytest.mark.parametrize("ty", TYPES)
 def test_linear_in_place_residual_another_stream_and_given_buffers(ty):
     torch = _torch()
