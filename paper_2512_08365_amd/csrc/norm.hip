@@ -25,8 +25,11 @@ constexpr int BACK_WGS = 256;     // workgroups of the backward pass, each with 
                                   // rows (twice as many where a CU's registers hold two)
 
 // The G threads of a row hold V neighbours each, G V further on the next V, and
-// so on: 8 where the width is a multiple of 8 (the hardware takes vector loads
-// at any element), single elements otherwise.
+// so on.  V is 8 (the hardware takes vector loads and stores at any element);
+// TAIL: the width is no multiple of 8, and one thread has elements of fewer.
+// fp32 rows of such widths go element by element, V = 1: 64 lanes' 4 bytes are
+// whole lines at once (13,399 x 791: 16 us, in vectors 20 us; bfloat16, 3,739 x
+// 11,918 backward: 94 us in vectors, 201 us by element).
 template <class T, int V>
 struct Held {
     T v[HELD];
@@ -38,22 +41,36 @@ __device__ __forceinline__ int column(int lane, int e)
     return (e / V * G + lane) * V + e % V;
 }
 
-template <int G, int V, class T>
+template <int G, int V, bool TAIL, class T>
 __device__ __forceinline__ void get(Held<T, V>& r, const T* row, int lane, int n)
 {
 #pragma unroll
     for (int c = 0; c < HELD / V; ++c) {
         const int j = (c * G + lane) * V;
-        if (j < n) {
-            __builtin_memcpy(r.v + c * V, row + j, V * sizeof(T));
+        T* to = r.v + c * V;
+        if (j + (TAIL ? V - 1 : 0) < n) {
+            // (at once: by memcpy, what else TAIL loads comes into the same registers by
+            // copies, ten too many for two workgroups of the backward pass a CU)
+            typedef T Piece __attribute__((ext_vector_type(TAIL ? V : 1), aligned(sizeof(T))));
+            if constexpr (TAIL) {
+                const Piece t = *(const Piece*)(row + j);
+#pragma unroll
+                for (int i = 0; i < V; ++i) to[i] = t[i];
+            } else {
+                __builtin_memcpy(to, row + j, V * sizeof(T));
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) r.v[c * V + i] = (T)0.0f;
+            for (int i = 0; i < V; ++i) to[i] = (T)0.0f;
+            if (TAIL && j < n)
+#pragma unroll
+                for (int i = 0; i < V - 1; ++i)
+                    if (j + i < n) to[i] = row[j + i];
         }
     }
 }
 
-template <int G, int V, class T>
+template <int G, int V, bool TAIL, class T>
 __device__ __forceinline__ void put(T* row, int lane, int n, const float* v)
 {
 #pragma unroll
@@ -62,7 +79,13 @@ __device__ __forceinline__ void put(T* row, int lane, int n, const float* v)
         T o[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] = (T)v[c * V + i];
-        if (j < n) __builtin_memcpy(row + j, o, V * sizeof(T));
+        if (j + (TAIL ? V - 1 : 0) < n) {
+            __builtin_memcpy(row + j, o, V * sizeof(T));
+        } else if (TAIL && j < n) {
+#pragma unroll
+            for (int i = 0; i < V - 1; ++i)
+                if (j + i < n) row[j + i] = o[i];
+        }
     }
 }
 
@@ -96,7 +119,7 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float2* lds)
     }
 }
 
-template <class T, class W, int G, int V, int THREADS>
+template <class T, class W, int G, int V, bool TAIL, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
 {
     constexpr int ROWS = THREADS / G;  // at a time
@@ -108,8 +131,8 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
     float w[HELD], b[HELD];
     {
         Held<W, V> a{}, d{};
-        if (p.weight) get<G, V>(a, static_cast<const W*>(p.weight), lane, n);
-        if (p.bias) get<G, V>(d, static_cast<const W*>(p.bias), lane, n);
+        if (p.weight) get<G, V, TAIL>(a, static_cast<const W*>(p.weight), lane, n);
+        if (p.bias) get<G, V, TAIL>(d, static_cast<const W*>(p.bias), lane, n);
 #pragma unroll
         for (int e = 0; e < HELD; ++e) {
             w[e] = p.weight ? (float)a.v[e] : 1.0f;
@@ -118,7 +141,7 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
     }
     Held<T, V> next{};
     const int64_t i0 = (int64_t)blockIdx.x * ROWS;
-    if (i0 + sub < p.M) get<G, V>(next, x + (i0 + sub) * p.x_rs, lane, n);
+    if (i0 + sub < p.M) get<G, V, TAIL>(next, x + (i0 + sub) * p.x_rs, lane, n);
     // (the workgroup's rows go together: its barriers are everybody's)
     for (int64_t base = i0; base < p.M; base += step) {
         const int64_t i = base + sub;
@@ -128,7 +151,7 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
             v[e] = (float)next.v[e];
             s += v[e];
         }
-        if (i + step < p.M) get<G, V>(next, x + (i + step) * p.x_rs, lane, n);
+        if (i + step < p.M) get<G, V, TAIL>(next, x + (i + step) * p.x_rs, lane, n);
         row_sums<G>(s, unused, lds[0]);
         const float mean = s / (float)n;
         s = 0.0f;
@@ -142,7 +165,7 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
         if (i >= p.M) continue;
 #pragma unroll
         for (int e = 0; e < HELD; ++e) v[e] = fmaf(v[e] * rstd, w[e], b[e]);
-        put<G, V>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, v);
+        put<G, V, TAIL>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, v);
         if (lane == 0) {
             if (p.mean) p.mean[i] = mean;
             if (p.rstd) p.rstd[i] = rstd;
@@ -183,7 +206,7 @@ __global__ __launch_bounds__(1024) void k_norm_wide(NormParams p)
 // over them of its columns in registers, adds up the threads of one column at
 // the end through LDS (one set of threads after another: a fixed order) and
 // leaves one row of sums for weight and bias each.
-template <class T, class W, int G, int V, int THREADS>
+template <class T, class W, int G, int V, bool TAIL, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm_back(NormParams p)
 {
     constexpr int ROWS = THREADS / G;
@@ -198,14 +221,14 @@ __global__ __launch_bounds__(THREADS) void k_norm_back(NormParams p)
     float w[HELD], dw[HELD] = {}, db[HELD] = {};
     {
         Held<W, V> a{};
-        if (p.weight) get<G, V>(a, static_cast<const W*>(p.weight), lane, n);
+        if (p.weight) get<G, V, TAIL>(a, static_cast<const W*>(p.weight), lane, n);
 #pragma unroll
         for (int e = 0; e < HELD; ++e) w[e] = p.weight ? (float)a.v[e] : 1.0f;
     }
     Held<T, V> nx{}, ny{};
     auto load = [&](int64_t i) {
-        get<G, V>(nx, x + i * p.x_rs, lane, n);
-        get<G, V>(ny, dy + i * p.dy_rs, lane, n);
+        get<G, V, TAIL>(nx, x + i * p.x_rs, lane, n);
+        get<G, V, TAIL>(ny, dy + i * p.dy_rs, lane, n);
     };
     const int64_t i0 = (int64_t)blockIdx.x * ROWS;
     if (AHEAD && i0 + sub < p.M) load(i0 + sub);
@@ -236,13 +259,13 @@ __global__ __launch_bounds__(THREADS) void k_norm_back(NormParams p)
         s2 /= (float)n;
 #pragma unroll
         for (int e = 0; e < HELD; ++e) h[e] = r * (h[e] - s1 - xh[e] * s2);
-        put<G, V>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, h);
+        put<G, V, TAIL>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, h);
     }
     if (!p.dweight && !p.dbias) return;
     float* part = p.part + (int64_t)blockIdx.x * 2 * n;
     if constexpr (ROWS == 1) {
-        put<G, V>(part, lane, n, dw);
-        put<G, V>(part + n, lane, n, db);
+        put<G, V, TAIL>(part, lane, n, dw);
+        put<G, V, TAIL>(part + n, lane, n, db);
     } else {
         for (int t = 0; t < ROWS; ++t) {
             if (sub == t)
@@ -337,7 +360,7 @@ int threads_of(int64_t n) { return n <= 64 * HELD ? 64 : n <= 256 * HELD ? 256 :
 // rows that a workgroup of the backward pass takes at a time
 int back_rows(int64_t n) { return n <= 64 * HELD ? 8 : n <= 256 * HELD ? 2 : 1; }
 
-template <class T, class W, int V>
+template <class T, class W, int V, bool TAIL>
 void forward_held(const NormParams& p, hipStream_t stream)
 {
     // as many workgroups as the device holds at once, the rows spread evenly
@@ -347,11 +370,11 @@ void forward_held(const NormParams& p, hipStream_t stream)
     const int64_t most = G == 1024 ? 512 : 2048, rounds = (groups + most - 1) / most;
     const dim3 grid((unsigned)((groups + rounds - 1) / rounds));
     if (G == 64)
-        hipLaunchKernelGGL((k_norm<T, W, 64, V, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_norm<T, W, 64, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 256)
-        hipLaunchKernelGGL((k_norm<T, W, 256, V, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_norm<T, W, 256, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else
-        hipLaunchKernelGGL((k_norm<T, W, 1024, V, 1024>), grid, dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_norm<T, W, 1024, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
 }
 
 template <class T, class W>
@@ -360,23 +383,23 @@ hipError_t forward(const NormParams& p, hipStream_t stream)
     if (p.N > MOST_HELD || p.x_cs != 1)
         hipLaunchKernelGGL((k_norm_wide<T, W>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
     else if (p.N % 8 == 0)
-        forward_held<T, W, 8>(p, stream);
+        forward_held<T, W, 8, false>(p, stream);
     else
-        forward_held<T, W, 1>(p, stream);
+        forward_held<T, W, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, stream);
     return hipGetLastError();
 }
 
-template <class T, class W, int V>
+template <class T, class W, int V, bool TAIL>
 void backward_held(const NormParams& p, int parts, hipStream_t stream)
 {
     const int G = threads_of(p.N);
     const dim3 grid(parts);
     if (G == 64)
-        hipLaunchKernelGGL((k_norm_back<T, W, 64, V, 512>), grid, dim3(512), 0, stream, p);
+        hipLaunchKernelGGL((k_norm_back<T, W, 64, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else if (G == 256)
-        hipLaunchKernelGGL((k_norm_back<T, W, 256, V, 512>), grid, dim3(512), 0, stream, p);
+        hipLaunchKernelGGL((k_norm_back<T, W, 256, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else
-        hipLaunchKernelGGL((k_norm_back<T, W, 1024, V, 1024>), grid, dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_norm_back<T, W, 1024, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
 }
 
 template <class T, class W>
@@ -390,9 +413,9 @@ hipError_t backward(const NormParams& p, hipStream_t stream)
                            dim3(256), 0, stream, p);
     else if (!wide && (p.y || sums)) {
         if (p.N % 8 == 0)
-            backward_held<T, W, 8>(p, parts, stream);
+            backward_held<T, W, 8, false>(p, parts, stream);
         else
-            backward_held<T, W, 1>(p, parts, stream);
+            backward_held<T, W, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, parts, stream);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -414,7 +437,7 @@ int norm_parts(int64_t M, int64_t N, int dtype)
 {
     // the rows spread evenly over the workgroups
     const int64_t rows = back_rows(N);
-    const int64_t most = dtype != MAG_F32 && N % 8 == 0 && rows > 1 ? 2 * BACK_WGS : BACK_WGS;
+    const int64_t most = dtype != MAG_F32 && rows > 1 ? 2 * BACK_WGS : BACK_WGS;
     const int64_t groups = std::max<int64_t>(1, (M + rows - 1) / rows), rounds = (groups + most - 1) / most;
     return (int)((groups + rounds - 1) / rounds);
 }
