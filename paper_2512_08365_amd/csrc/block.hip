@@ -105,6 +105,7 @@ int64_t packed_ld(int64_t n, int kind) { return kind == mag::MM_F32_PARTS ? (n +
 // 16-byte loads do not take).
 struct Operand {
     bool packed;
+    bool by_cols;      // packed: the matrix's columns are the rows
     size_t bytes;      // of the packed rows
     mag::MmOperand op; // p NULL while packed rows have no place yet
 };
@@ -126,10 +127,12 @@ Operand operand(const mag_matrix& m, int kind, bool along)
             return o;
         }
     }
+    // (packed as it lies: by columns if these are what is contiguous)
     o.packed = true;
-    o.op.ld = packed_ld(m.cols, kind);
-    o.op.mc = !along;
-    o.bytes = (size_t)(m.rows * o.op.ld) * part_size(kind);
+    o.by_cols = m.rows > 1 && m.row_stride == 1 && m.col_stride != 1;
+    o.op.ld = packed_ld(o.by_cols ? m.rows : m.cols, kind);
+    o.op.mc = o.by_cols == along;
+    o.bytes = (size_t)((o.by_cols ? m.cols : m.rows) * o.op.ld) * part_size(kind);
     return o;
 }
 
@@ -137,10 +140,10 @@ mag::PackParams packing(const Operand& o, const mag_matrix& m)
 {
     mag::PackParams p{};
     p.src = m.data;
-    p.rs = m.row_stride;
-    p.cs = m.col_stride;
-    p.rows = m.rows;
-    p.cols = m.cols;
+    p.rs = o.by_cols ? m.col_stride : m.row_stride;
+    p.cs = o.by_cols ? m.row_stride : m.col_stride;
+    p.rows = o.by_cols ? m.cols : m.rows;
+    p.cols = o.by_cols ? m.rows : m.cols;
     p.dst = const_cast<void*>(o.op.p);
     p.ld = o.op.ld;
     return p;
@@ -306,6 +309,8 @@ size_t plan_linear(const mag_linear_args* a, void* ws, LinearPlan& pl)
 
 struct BackwardPlan {
     int kind;         // MM_*
+    bool skinny;      // few rows: dx as a layer of few rows whose weight is the transpose
+    bool across;      // ... which lies row by row
     Operand x, w, dy;
     bool own_dz;      // dz in the workspace (else dy is dz)
     mag::MmOperand dz;
@@ -317,9 +322,11 @@ struct BackwardPlan {
 size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& pl)
 {
     const int64_t M = a->x.rows, N = a->weight.rows, K = a->x.cols;
+    pl.across = a->weight.row_stride != 1 && a->weight.rows > 1;
+    pl.skinny = M <= mag::SKINNY_ROWS && (!pl.across || a->weight.col_stride == 1 || K <= 1);
     double least = 1e300;
     for (int kind : {kind_of(a->dtype), (int)mag::MM_F32_PARTS}) {
-        if (kind == mag::MM_F32_PARTS && a->dtype != MAG_F32) break;
+        if (kind == mag::MM_F32_PARTS && (a->dtype != MAG_F32 || pl.skinny)) break;
         // x and weight are both read across the reduction of the product they enter
         const Operand x = operand(a->x, kind, false), w = operand(a->weight, kind, false);
         const Shape dx = choose(M, K, N, kind, 1, false), dw = choose(N, K, M, kind, 1, false);
@@ -334,7 +341,7 @@ size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& 
     }
     pl.dy = operand(a->dy, pl.kind, true);
     // (as for the sizes: room for dz whether or not dy can stand in for it)
-    pl.own_dz = a->activation != MAG_ACT_NONE || pl.dy.packed || !a->dy.data;
+    pl.own_dz = a->activation != MAG_ACT_NONE || pl.dy.packed || !a->dy.data || (pl.skinny && pl.dy.op.mc);
     if (pl.own_dz) {
         pl.dz = mag::MmOperand{};
         pl.dz.ld = packed_ld(N, pl.kind);
@@ -342,6 +349,10 @@ size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& 
         pl.dz = pl.dy.op;
     }
     Carve c{static_cast<char*>(ws)};
+    if (pl.skinny) {
+        pl.w.packed = false;
+        pl.dx.splits = 1;
+    }
     for (Operand* o : {&pl.x, &pl.w})
         if (o->packed) o->op.p = c.take(o->bytes);
     void* dz = c.take((size_t)(M * packed_ld(N, pl.kind)) * part_size(pl.kind));
@@ -609,7 +620,20 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
     p.S = K;
     p.partial_ld = up8(K);
     p.a = pl.dz;
-    if (dx) {
+    if (dx && pl.skinny) {
+        mag::SkinnyParams s{};
+        s.x = pl.dz.p;
+        s.x_ld = pl.dz.ld;
+        s.w = a->weight.data;
+        s.w_ld = pl.across ? a->weight.row_stride : a->weight.col_stride;
+        s.across = pl.across;
+        s.M = M;
+        s.N = K;
+        s.K = N;
+        s.e.y = a->dx.data;
+        s.e.y_ld = a->dx.row_stride;
+        TRY_HIP(mag::launch_skinny(s, a->dtype, stream), "linear_backward launch");
+    } else if (dx) {
         p.b = pl.w.op;
         p.R = M;
         p.K = N;

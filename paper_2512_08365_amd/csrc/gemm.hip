@@ -172,14 +172,8 @@ __global__ __launch_bounds__(256) void k_mm_join(Mm p)
     const int64_t plane = p.R * p.partial_ld;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = quotient(i, per_row), s = (i - r * per_row) * 8;
-        const float* q = p.partial + r * p.partial_ld + s;
-        float v[8], w[8];
-        load8(q, v);
-        for (int k = 1; k < p.splits; ++k) {
-            load8(q + k * plane, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += w[e];
-        }
+        float v[8] = {};
+        add_parts(p.partial + r * p.partial_ld + s, plane, p.splits, v);
         const int m = (int)min((int64_t)8, p.S - s);
         if constexpr (sizeof(TO) == 4)
             if (p.in_parts) make_whole(p, 0, r, s, m, v);
@@ -218,7 +212,8 @@ hipError_t launch_prepare(const PackParams* a, const PackParams* b, const Column
 int64_t slope_chunks(int64_t M, int64_t N)
 {
     const int64_t across = (N + SLOPE_COLS - 1) / SLOPE_COLS;
-    const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(across, 1));
+    // (256 at most: few columns' sums would be long in finishing them)
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(2048 / std::max<int64_t>(across, 1), 256));
     return std::max<int64_t>(1, std::min<int64_t>(want, (M + 4 * SLOPE_ROWS - 1) / (4 * SLOPE_ROWS)));
 }
 

@@ -287,6 +287,33 @@ __device__ __forceinline__ void store8(T* p, const float* v)
     }
 }
 
+// the sums of a split product's parts, one plane after another, N planes' loads
+// in flight
+template <int N>
+__device__ __forceinline__ void add_parts(const float* q, int64_t plane, int splits, float* v)
+{
+    for (int k = 0; k < splits; k += N) {
+        float w[N][8];
+#pragma unroll
+        for (int u = 0; u < N; ++u) load8(q + min(k + u, splits - 1) * plane, w[u]);
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            if (k + u < splits)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += w[u][e];
+    }
+}
+
+__device__ __forceinline__ void add_parts(const float* q, int64_t plane, int splits, float* v)
+{
+    if (splits <= 2)
+        add_parts<2>(q, plane, splits, v);
+    else if (splits <= 4)
+        add_parts<4>(q, plane, splits, v);
+    else
+        add_parts<8>(q, plane, splits, v);
+}
+
 // eight neighbours from column j on (zeros from column `cols` on); neighbours in
 // memory are loaded at once, whatever their alignment
 template <class T>

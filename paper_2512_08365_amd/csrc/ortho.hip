@@ -96,16 +96,10 @@ __global__ __launch_bounds__(256) void k_orth_join(Mm p)
         const int64_t r = r0 + i / 8, s = s0 + i % 8 * 8;
         if (r >= p.R || s >= across) continue;
         const int n = (int)max((int64_t)0, min((int64_t)8, p.S - s));
-        float v[8] = {}, w[8];
-        if (n > 0) {
-            const float* q = p.partial + ((int64_t)bt * p.splits * p.R + r) * p.partial_ld + s;
-            load8(q, v);
-            for (int k = 1; k < p.splits; ++k) {
-                load8(q + k * p.R * p.partial_ld, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += w[e];
-            }
-        }
+        float v[8] = {};
+        if (n > 0)
+            add_parts(p.partial + ((int64_t)bt * p.splits * p.R + r) * p.partial_ld + s, p.R * p.partial_ld,
+                      p.splits, v);
         if (mirror)
 #pragma unroll
             for (int e = 0; e < 8; ++e) block[i / 8][i % 8 * 8 + e] = v[e];

@@ -55,6 +55,27 @@ __device__ __forceinline__ Frag<T> fetch(const T* row, int64_t k, int64_t K)
     return f;
 }
 
+// fragments that end inside the row
+template <class T>
+__device__ __forceinline__ Frag<T> fetch_inside(const T* row, int64_t k)
+{
+    Frag<T> f;
+    __builtin_memcpy(f.v, row + k, 16);
+    return f;
+}
+
+// any fragments: their elements asked for before any is looked at
+template <class T>
+__device__ __forceinline__ Frag<T> fetch_last(const T* row, int64_t k, int64_t K)
+{
+    Frag<T> f;
+#pragma unroll
+    for (int i = 0; i < Frag<T>::KL; ++i) f.v[i] = row[min(k + i, K - 1)];
+#pragma unroll
+    for (int i = 0; i < Frag<T>::KL; ++i) f.v[i] = k + i < K ? f.v[i] : (T)0.0f;
+    return f;
+}
+
 // the sums of the waves added up and stored: G x 16 outputs of MF x 16 rows
 template <class T, int G, int MF, int WAVES>
 __device__ __forceinline__ void finish(const SkinnyParams& p, f32x4 (&acc)[G][MF], f32x4* lds, int64_t n0)
@@ -104,27 +125,40 @@ __global__ __launch_bounds__(WAVES * 64) void k_skinny_along(SkinnyParams p)
     for (int f = 0; f < MF; ++f)
         x[f] = static_cast<const T*>(p.x) + min((int64_t)f * 16 + lane % 16, p.M - 1) * p.x_ld;
     f32x4 acc[G][MF] = {};
-    for (int64_t k0 = (int64_t)wave * PIECE; k0 < p.K; k0 += (int64_t)WAVES * PIECE * AHEAD) {
-        Frag<T> fw[AHEAD][2][G], fx[AHEAD][2][MF];
+    Frag<T> fw[AHEAD][2][G], fx[AHEAD][2][MF];
+    auto load = [&](int a, int64_t k0, auto get) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) fw[a][s][g] = get(w[g], k0 + s * STEP + kl);
+#pragma unroll
+            for (int f = 0; f < MF; ++f) fx[a][s][f] = get(x[f], k0 + s * STEP + kl);
+        }
+    };
+    auto add = [&](int a) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int f = 0; f < MF; ++f) multiply(fw[a][s][g], fx[a][s][f], acc[g][f]);
+    };
+    // the whole pieces (which ones a wave has is the same for all of its lanes) ...
+    const int whole = (int)(p.K / PIECE);
+    for (int i = wave; i < whole; i += WAVES * AHEAD) {
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a)
+            if (i + a * WAVES < whole)
+                load(a, (int64_t)(i + a * WAVES) * PIECE, [](const T* row, int64_t k) { return fetch_inside(row, k); });
+            else
+                load(a, 0, [](const T*, int64_t) { return Frag<T>{}; });
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                // (pieces behind the end: zeros)
-                const int64_t k = k0 + (int64_t)a * WAVES * PIECE + s * STEP + kl;
-#pragma unroll
-                for (int g = 0; g < G; ++g) fw[a][s][g] = fetch(w[g], k, p.K);
-#pragma unroll
-                for (int f = 0; f < MF; ++f) fx[a][s][f] = fetch(x[f], k, p.K);
-            }
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a)
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-#pragma unroll
-                    for (int f = 0; f < MF; ++f) multiply(fw[a][s][g], fx[a][s][f], acc[g][f]);
+        for (int a = 0; a < AHEAD; ++a) add(a);
+    }
+    // ... and what is left, whose turn it is
+    if (p.K % PIECE && wave == whole % WAVES) {
+        load(0, (int64_t)whole * PIECE, [&](const T* row, int64_t k) { return fetch_last(row, k, p.K); });
+        add(0);
     }
     finish<T, G, MF, WAVES>(p, acc, lds, n0);
 }
@@ -211,9 +245,12 @@ hipError_t launch(const SkinnyParams& p, hipStream_t stream)
             hipLaunchKernelGGL((k_skinny_across<T, MF, 8>), grid, dim3(512), 0, stream, p);
         return hipGetLastError();
     }
-    // two groups of outputs where that leaves enough workgroups: the rows' own
-    // fragments, which come from L2, are then used twice
-    const bool two = p.N >= 16 * 1024;
+    // Two groups of outputs where that leaves enough workgroups: the rows' own
+    // fragments, which come from L2, are then used twice (4096 inputs: 32 rows by
+    // 8,192 outputs 20 us, one group 25 us; by 4,096 18 and 14 us; 16 rows by 16,384
+    // 32 and 35 us).  Of few rows these are nearly the same lines for all lanes (1
+    // row by 16,384: 33 and 24 us).
+    const bool two = MF == 2 ? p.N >= 8192 : p.M > 8 && p.N >= 16384;
     const dim3 grid((unsigned)((p.N + (two ? 31 : 15)) / (two ? 32 : 16)));
     if (two)
         hipLaunchKernelGGL((k_skinny_along<T, 2, MF, 8>), grid, dim3(512), 0, stream, p);

@@ -385,6 +385,15 @@ def test_linear_backward_layouts(lw, ld, ty):
 
 
 @pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("ld", LAYOUTS)
+@pytest.mark.parametrize("lw", LAYOUTS)
+def test_linear_backward_few_rows(lw, ld, ty):
+    check_linear_backward(1, 65, 1100, ty, lw=lw, ld=ld)
+    check_linear_backward(19, 272, 203, ty, act="silu", lx=ld, lw=lw, ld=ld)
+    check_linear_backward(32, 1300, 72, ty, lx=lw, lw=lw, ld=ld)
+
+
+@pytest.mark.parametrize("ty", TYPES)
 @pytest.mark.parametrize("size", [(4100, 264, 520), (2048, 1024, 1536), (1001, 2049, 1111),
                                   (20000, 64, 72)], ids=lambda s: "x".join(map(str, s)))
 def test_linear_backward_larger(size, ty):
