@@ -788,7 +788,8 @@ hipError_t launch_mm_tile(const Mm& p, hipStream_t stream)
     const int64_t tiles = p.symmetric ? tr * (tr + 1) / 2 : tr * ts;
     if (tiles > 0x7fffffffLL || p.batch > 65535) return hipErrorInvalidConfiguration;
     const int64_t fit = (int64_t)device_cu_count() * wgs_per_cu(SIDE, P, STAGES);
-    const int64_t each = (fit + (int64_t)p.splits * p.batch - 1) / ((int64_t)p.splits * p.batch);
+    // (no more than fit: the few that did not would have their tiles done alone)
+    const int64_t each = fit / ((int64_t)p.splits * p.batch) > 0 ? fit / ((int64_t)p.splits * p.batch) : 1;
     const dim3 grid((unsigned)(tiles < each ? tiles : each), (unsigned)p.splits, (unsigned)p.batch);
     const dim3 block(256);
     if (p.a.mc)

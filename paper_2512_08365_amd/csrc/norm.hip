@@ -2,7 +2,7 @@
 //
 // Both passes are bound by memory: every row is read once into registers, and
 // what a row needs of its neighbours is one reduction (the backward pass's two
-// sums go together).  A row belongs to 64, 256 or 1,024 threads, the fewest
+// sums go together).  A row belongs to 64, 256, 512 or 1,024 threads, the fewest
 // that hold it in 16 elements each: few enough registers that the rows'
 // weights stay in them from row to row (a 2-byte row's fp32 weight and bias are
 // four times its bytes, and would come from L2 each time), and so do the
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(1024) void k_norm_back_wide(NormParams p)
 }
 
 // threads of a row of width n
-int threads_of(int64_t n) { return n <= 64 * HELD ? 64 : n <= 256 * HELD ? 256 : 1024; }
+int threads_of(int64_t n) { return n <= 64 * HELD ? 64 : n <= 256 * HELD ? 256 : n <= 512 * HELD ? 512 : 1024; }
 // rows that a workgroup of the backward pass takes at a time
 int back_rows(int64_t n) { return n <= 64 * HELD ? 8 : n <= 256 * HELD ? 2 : 1; }
 
@@ -367,12 +367,14 @@ void forward_held(const NormParams& p, hipStream_t stream)
     // over them
     const int G = threads_of(p.N), rows = G == 64 ? 4 : 1;
     const int64_t groups = (p.M + rows - 1) / rows;
-    const int64_t most = G == 1024 ? 512 : 2048, rounds = (groups + most - 1) / most;
+    const int64_t most = G == 1024 ? 512 : G == 512 ? 1024 : 2048, rounds = (groups + most - 1) / most;
     const dim3 grid((unsigned)((groups + rounds - 1) / rounds));
     if (G == 64)
         hipLaunchKernelGGL((k_norm<T, W, 64, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 256)
         hipLaunchKernelGGL((k_norm<T, W, 256, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 512)
+        hipLaunchKernelGGL((k_norm<T, W, 512, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else
         hipLaunchKernelGGL((k_norm<T, W, 1024, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
 }
@@ -398,6 +400,8 @@ void backward_held(const NormParams& p, int parts, hipStream_t stream)
         hipLaunchKernelGGL((k_norm_back<T, W, 64, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else if (G == 256)
         hipLaunchKernelGGL((k_norm_back<T, W, 256, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
+    else if (G == 512)
+        hipLaunchKernelGGL((k_norm_back<T, W, 512, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else
         hipLaunchKernelGGL((k_norm_back<T, W, 1024, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
 }
