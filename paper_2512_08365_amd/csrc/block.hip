@@ -192,9 +192,8 @@ Shape choose(int64_t R, int64_t S, int64_t K, int kind, int64_t batch, bool symm
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
             if (s > 1 && (t == mag::TILE_256 || steps < 2 * s)) break;
             const int64_t wgs = tiles * s;
-            // rounds of two a CU where there is room; what is left has CUs of its own if
-            // the reduction is not split (of a split one, the same CUs' pairs go on)
-            const int64_t pairs = c.shared == 0.0 ? 0 : (wgs + (s > 1 && wgs > CUS ? 2 * CUS : CUS) - 1) / (2 * CUS);
+            // rounds of two a CU where there is room, then a last one of what is left
+            const int64_t pairs = c.shared == 0.0 ? 0 : (wgs + CUS - 1) / (2 * CUS);
             const int64_t single = (std::max<int64_t>(wgs - pairs * 2 * CUS, 0) + CUS - 1) / CUS;
             const double each = (double)((steps + s - 1) / s);
             double cost = CALL_COST + (double)pairs * (each * c.shared + c.tile) +
