@@ -404,8 +404,8 @@ struct OrthPlan {
     int chunks;         // sums of squares of a matrix
     double* part;
     mag::f16* X[2];
-    mag::f16* A;
-    mag::f16* B;
+    mag::f16* side[4];  // of m x m: A, and what the steps on that side need
+    bool grouped;       // several steps on that side are less work than one by one
 };
 
 size_t plan_orth(const mag_orthogonalize_args* a, void* ws, OrthPlan& pl)
@@ -424,8 +424,11 @@ size_t plan_orth(const mag_orthogonalize_args* a, void* ws, OrthPlan& pl)
     pl.chunks = std::max(pl.chunks, 1);
     pl.part = c.take<double>((size_t)(a->batch * pl.chunks * 8));
     for (auto& x : pl.X) x = c.take<mag::f16>((size_t)(a->batch * a->g.rows * pl.ld * 2));
-    pl.A = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 2));
-    pl.B = c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 2));
+    // (a step more on that side takes four products there, on its own one and the
+    // two long ones)
+    pl.grouped = a->dtype != MAG_F32 && pl.gram.cost + pl.whole.cost > 3.0 * pl.square.cost;
+    for (int i = 0; i < 4; ++i)
+        pl.side[i] = i < 2 || pl.grouped ? c.take<mag::f16>((size_t)(a->batch * pl.m * pl.lda * 2)) : nullptr;
     pl.partial = c.take<float>(std::max({partial_bytes(pl.m, pl.m, pl.gram, a->batch),
                                          partial_bytes(pl.m, pl.m, pl.square, a->batch),
                                          partial_bytes(a->g.rows, a->g.cols, pl.whole, a->batch)}));
@@ -459,6 +462,37 @@ double most_of_polynomial(double a, double b, double c, double u)
         for (double t : {q / (5.0 * c), a / q})
             if (t > 0.0 && t < u * u) top = std::max(top, f(sqrt(t)));
     return top;
+}
+
+// How many steps from step i on are done on the short side.  With Q the product of
+// their U = a I + b A + c A A, X <- Q X is all that is as long as X, and the next
+// A is U A U: of 2,048 x 8,192, three steps and two are 40 products of a side
+// cubed where five single ones are 65 (1,650 -> FIGURE us).  What an A so made
+// costs is accuracy: its rounding, 2^-21 of the largest eigenvalue, grows by the
+// slope of one step's map of eigenvalues, l (a + b l + c l l)^2, from step to step
+// and enters U times the slope of that.  A quarter of the result's own rounding is
+// let through (bfloat16: three steps by the usual coefficients, half: two; fp32
+// results go one by one).
+int orth_group(const mag_orthogonalize_args* a, const OrthPlan& pl, int i, const double* most)
+{
+    if (!pl.grouped) return 1;
+    const double allowed = a->dtype == MAG_BF16 ? 0x1p-11 : 0x1p-14;
+    double error = 0x1p-21, bound = 1.0;
+    int group = 1;
+    for (int j = i; j < a->steps; ++j) {
+        const double u2 = most[j] * most[j];
+        double slope = 0.0, growth = 1.0;
+        for (int k = 0; k <= 128; ++k) {
+            const double l = u2 * k / 128.0, q = a->a + l * (a->b + l * a->c), dq = a->b + 2.0 * a->c * l;
+            slope = std::max(slope, fabs(dq));
+            growth = std::max(growth, fabs(q * (q + 2.0 * l * dq)));
+        }
+        bound *= fabs(a->a) + fabs(a->b) * u2 + fabs(a->c) * u2 * u2;
+        if (j > i && (error * slope > allowed || bound > 0x1p40)) break;
+        group = j - i + 1;
+        error *= 1.05 * growth;
+    }
+    return group;
 }
 
 }  // namespace
@@ -807,65 +841,102 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         o.out_batch = a->out_batch_stride;
     }
     TRY_HIP(mag::launch_orth_begin(o, a->dtype, stream), "orthogonalize launch");
-    for (int i = 0; i < a->steps; ++i) {
-        const double u2 = most[i] * most[i];
-        const double sa = scale_for(1.01 * u2);
-        const double sb = scale_for(1.01 * (fabs(a->b) * u2 + fabs(a->c) * u2 * u2) + 0x1p-100);
-        const double next = scale_for(most[i + 1] + 0x1p-100);
-        const mag::MmOperand X{pl.X[i & 1], pl.ld, x_batch, 0};
-        const mag::MmOperand A{pl.A, pl.lda, a_batch, 0};
-        const mag::MmOperand B{pl.B, pl.lda, a_batch, 0};
-        // A = X X^T
-        mag::Mm p{};
-        p.batch = (int)a->batch;
-        p.partial = pl.partial;
-        p.partial_ld = up8(m);
-        p.splits = pl.gram.splits;
-        p.a = p.b = X;
-        p.a.mc = p.b.mc = tall;
+    const mag::MmOperand side[4] = {{pl.side[0], pl.lda, a_batch, 0}, {pl.side[1], pl.lda, a_batch, 0},
+                                    {pl.side[2], pl.lda, a_batch, 0}, {pl.side[3], pl.lda, a_batch, 0}};
+    mag::Mm p{};
+    p.batch = (int)a->batch;
+    p.partial = pl.partial;
+    auto symmetric = [&](const mag::MmOperand& x, const mag::MmOperand& y, int64_t k, double scale, int z,
+                         const Shape& shape) {
+        p.a = x;
+        p.b = y;
         p.R = p.S = m;
-        p.K = n;
+        p.K = k;
         p.symmetric = 1;
-        p.o.scale = (float)(sa / (sx * sx));
-        p.o.z = pl.A;
+        p.partial_ld = up8(m);
+        p.splits = shape.splits;
+        p.o.scale = (float)scale;
+        p.o.z = pl.side[z];
         p.o.z_ld = pl.lda;
         p.o.z_batch = a_batch;
-        TRY(launch_orth(p, pl.gram.tile, stream));
-        // B = b A + c A A
-        p.a = p.b = A;
-        p.K = m;
-        p.o.scale = (float)(a->c * sb / (sa * sa));
-        p.o.mix = (float)(a->b * sb / sa);
-        p.o.m = pl.A;
-        p.o.m_ld = pl.lda;
-        p.o.m_batch = a_batch;
-        p.o.z = pl.B;
-        p.splits = pl.square.splits;
-        TRY(launch_orth(p, pl.square.tile, stream));
-        // X <- a X + B X, or its transpose <- a X^T + X^T B (B symmetric)
+        const int rc = launch_orth(p, shape.tile, stream);
+        p.o.m = nullptr;
+        p.o.diagonal = 0.0f;
+        return rc;
+    };
+    auto mixed = [&](const mag::MmOperand& x, double mix) {
+        p.o.m = static_cast<const mag::f16*>(x.p);
+        p.o.m_ld = x.ld;
+        p.o.m_batch = x.batch;
+        p.o.mix = (float)mix;
+    };
+    constexpr int A = 0;
+    for (int i = 0, from = 0; i < a->steps; from ^= 1) {
+        const int group = orth_group(a, pl, i, most);
+        mag::MmOperand X{pl.X[from], pl.ld, x_batch, 0};
+        // A = X X^T
+        X.mc = tall;
+        double sa = scale_for(1.01 * most[i] * most[i]);
+        TRY(symmetric(X, X, n, sa / (sx * sx), A, pl.gram));
+        // Q: what X is multiplied by, without `rest` I
+        int q = 1;
+        double sq = 0.0, rest = a->a, bound = 1.0;
+        for (int j = i; j < i + group; ++j) {
+            const double u2 = most[j] * most[j];
+            const double of_u = fabs(a->b) * u2 + fabs(a->c) * u2 * u2 + (group > 1 ? fabs(a->a) : 0.0);
+            const double su = scale_for(1.01 * of_u + 0x1p-100);
+            // U = b A + c A A, of a group a I + b A + c A A
+            const int u = j == i ? 1 : q % 3 + 1;
+            mixed(side[A], a->b * su / sa);
+            if (group > 1) p.o.diagonal = (float)(a->a * su);
+            TRY(symmetric(side[A], side[A], m, a->c * su / (sa * sa), u, pl.square));
+            const int other = 6 - q - u;   // (of 1, 2 and 3, where q and u differ)
+            bound *= of_u;
+            if (j == i) {
+                sq = su;
+            } else {
+                // Q <- U Q
+                const double next = scale_for(1.01 * bound + 0x1p-100);
+                TRY(symmetric(side[u], side[q], m, next / (su * sq), other, pl.square));
+                sq = next;
+                q = other;
+            }
+            if (j + 1 < i + group) {
+                // A <- U A U
+                const int t = u == q ? u % 3 + 1 : 6 - q - u;
+                const double st = scale_for(1.01 * most[j] * most[j + 1] + 0x1p-100);
+                const double next = scale_for(1.01 * most[j + 1] * most[j + 1] + 0x1p-100);
+                TRY(symmetric(side[u], side[A], m, st / (su * sa), t, pl.square));
+                TRY(symmetric(side[u], side[t], m, next / (su * st), A, pl.square));
+                sa = next;
+            }
+        }
+        if (group > 1) rest = 0.0;
+        i += group;
+        // X <- rest X + Q X, or its transpose <- rest X^T + X^T Q (Q symmetric)
+        const bool last = i == a->steps;
+        const double next = scale_for(most[i] + 0x1p-100), out = last ? 1.0 : next;
+        X.mc = 0;
+        if (rest != 0.0) mixed(X, rest * out / sx);
         p.symmetric = 0;
-        p.a = tall ? X : B;
-        p.b = tall ? B : X;
+        p.a = tall ? X : side[q];
+        p.b = tall ? side[q] : X;
         p.b.mc = !tall;
         p.R = a->g.rows;
         p.S = a->g.cols;
-        const bool last = i + 1 == a->steps;
-        const double out = last ? 1.0 : next;
-        p.o.scale = (float)(out / (sb * sx));
-        p.o.mix = (float)(a->a * out / sx);
-        p.o.m = pl.X[i & 1];
-        p.o.m_ld = pl.ld;
-        p.o.m_batch = x_batch;
-        p.o.z = last ? nullptr : pl.X[(i + 1) & 1];
+        p.K = m;
+        p.partial_ld = up8(a->g.cols);
+        p.splits = pl.whole.splits;
+        p.o.scale = (float)(out / (sq * sx));
+        p.o.z = last ? nullptr : pl.X[from ^ 1];
         p.o.z_ld = pl.ld;
         p.o.z_batch = x_batch;
         p.o.out = a->out.data;
         p.o.out_ld = a->out.row_stride;
         p.o.out_batch = a->out_batch_stride;
         p.o.dtype = a->dtype;
-        p.splits = pl.whole.splits;
-        p.partial_ld = up8(a->g.cols);
         TRY(launch_orth(p, pl.whole.tile, stream));
+        p.o.m = nullptr;
         sx = next;
     }
     return MAG_OK;

@@ -39,9 +39,9 @@ struct Epilogue {
     int32_t vec;          // neighbours of a row are neighbours in memory everywhere
 };
 
-// z = scale sum + mix M, as two halves or, for the result, one number
+// z = scale sum + mix M + diagonal I, as two halves or, for the result, one number
 struct OrthStore {
-    float scale, mix;
+    float scale, mix, diagonal;
     const f16* m;         // or NULL: two parts, as an operand's
     int64_t m_ld, m_batch;
     f16* z;               // two parts, as an operand's, or NULL

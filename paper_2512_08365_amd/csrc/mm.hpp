@@ -373,8 +373,8 @@ __device__ __forceinline__ void two_halves(float v, f16& hi, f16& lo)
     lo = (f16)(v - (float)hi);
 }
 
-// z = scale v + mix m for n <= 8 neighbours of a row (the rest of an
-// iteration's padding: zeros)
+// z = scale v + mix m (and the diagonal) for n <= 8 neighbours of a row (the rest
+// of an iteration's padding: zeros)
 static __device__ __forceinline__ void store_orth(const Mm& p, int64_t bt, int64_t r, int64_t s,
                                                   int n, const float* sum)
 {
@@ -390,6 +390,9 @@ static __device__ __forceinline__ void store_orth(const Mm& p, int64_t bt, int64
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(o.mix, hi[i] + lo[i], v[i]);
     }
+    if (o.diagonal != 0.0f)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += s + i == r ? o.diagonal : 0.0f;
     if (o.z) {
         s16x8 hi, lo;
 #pragma unroll
