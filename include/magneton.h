@@ -781,10 +781,11 @@ typedef struct mag_linear_args {
  *   mag_linear_workspace_size: bytes for args->x and args->weight (type, sizes,
  *   strides and the 16-byte alignment of data count; the rest of args is not
  *   read).
- * fp32 operands are cut into three bfloat16 parts each, whose sum is the
- * operand exactly, and the six largest of the nine products are summed in fp32
- * (the rest is below 2^-24 of a product); a sum that is not finite is
- * taken again from the operands themselves.
+ * fp32 operands of small products are multiplied as they are.  Those of large
+ * ones (from some 10^10 operations on) are cut into three bfloat16
+ * parts each, whose sum is the operand exactly, and the six largest of the nine
+ * products are summed in fp32 (the rest is below 2^-24 of a product); a sum that
+ * is not finite is taken again from the operands themselves.
  * Errors: MAG_E_NULL, MAG_E_SIZE (types, sizes, strides), MAG_E_ALIGN,
  * MAG_E_WORKSPACE, MAG_E_HIP.
  */
@@ -809,7 +810,7 @@ typedef struct mag_linear_backward_args {
  * mag_linear_backward -- gradients of mag_linear: dz = dy act'(pre), dx = dz
  * weight, dweight = dz^T x, dbias = the sum of dz over the rows (the residual's
  * gradient is dy itself).  The products read dz rounded to the operands' type,
- * as x and weight are held (fp32: the parts of mag_linear); dbias sums it
+ * as x and weight are held (fp32: as mag_linear multiplies them); dbias sums it
  * unrounded.  rows = 0 gives dweight = 0 and dbias = 0.
  *   workspace_size: of args' sizes, strides and alignments of x, weight and dy.
  * Errors as mag_linear.
@@ -869,7 +870,9 @@ typedef struct mag_orthogonalize_args {
  * transpose where g is taller than wide.  mag_invariants of the result shows
  * its singular values.  Operands of the products are held as the sum of two
  * half-precision numbers (22 bits) under a power of two that follows from the
- * polynomial's bound, sums in fp32.  steps = 0 gives g / (|g| + eps).
+ * polynomial's bound, sums in fp32.  Results of two bytes may take up to three
+ * steps in one on the short side, as far as a quarter of their own rounding
+ * allows.  steps = 0 gives g / (|g| + eps).
  * Errors: MAG_E_NULL, MAG_E_SIZE (also a polynomial whose bound on X passes
  * 2^60), MAG_E_ALIGN, MAG_E_WORKSPACE, MAG_E_HIP.
  */

