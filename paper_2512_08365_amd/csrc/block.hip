@@ -96,9 +96,16 @@ bool same_shape(const mag_matrix& m, int64_t rows, int64_t cols)
 constexpr int64_t MOST_LD = 1LL << 22;  // 256 rows of it stay within 31 bits of bytes
 int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 // bytes of an element of a product's operand (kind: MM_*), elements of a packed
-// row of n
+// row of n: whole lines of 128 bytes, but for narrow ones (a step's 128 bytes of a
+// row are then one line in L2: gradients of 1,000 x 777 by 2,050 half 34.7 us with
+// rows of whole 16 bytes, 29.5 us so)
 size_t part_size(int kind) { return kind == mag::MM_F32 ? 4 : 2; }
-int64_t packed_ld(int64_t n, int kind) { return kind == mag::MM_F32_PARTS ? (n + 31) / 32 * 96 : up8(n); }
+int64_t packed_ld(int64_t n, int kind)
+{
+    if (kind == mag::MM_F32_PARTS) return n > 32 ? (n + 63) / 64 * 192 : 96;
+    const int64_t line = 128 / (int64_t)part_size(kind);
+    return n > line ? (n + line - 1) / line * line : up8(n);
+}
 
 // How a product reads a matrix: where it lies, or as rows packed into the
 // workspace (what is cut into parts, and strides, alignments and widths that the
@@ -205,6 +212,31 @@ Shape choose(int64_t R, int64_t S, int64_t K, int kind, int64_t batch, bool symm
             if (s > 1) cost += JOIN_COST + 2.0 * (double)s * (double)R * (double)S * (double)batch * 4.0 / PARTIAL_BYTES;
             if (cost < best.cost) best = Shape{t, s, cost};
         }
+    }
+    return best;
+}
+
+// Two products side by side in one launch, in 64 tiles: the workgroups that fit
+// are dealt to them so that the slower one is done as early as may be.
+struct Together {
+    int wgs_dx, wgs_dw;
+    double cost;
+};
+Together choose_two(int64_t M, int64_t N, int64_t K, int kind)
+{
+    const TileCost& c = TILE_COST[kind][mag::TILE_64];
+    const int64_t step = kind == mag::MM_BF16 || kind == mag::MM_F16 ? 64 : 32;
+    auto tiles = [](int64_t r, int64_t s) { return (double)((r + 63) / 64) * (double)((s + 63) / 64); };
+    const double dx = tiles(M, K), dw = tiles(N, K), slots = c.shared > 0.0 ? 512 : 256;
+    const double per_step = dx + dw > 256 && c.shared > 0.0 ? c.shared : c.alone;
+    const double one_dx = (double)((N + step - 1) / step) * per_step + c.tile;
+    const double one_dw = (double)((M + step - 1) / step) * per_step + c.tile;
+    Together best{0, 0, 1e300};
+    if (dx + dw <= slots) return Together{(int)dx, (int)dw, CALL_COST + std::max(one_dx, one_dw)};
+    for (int w = 8; w < slots; w += 8) {   // (in eights: an XCD keeps its run)
+        const double cost = CALL_COST + std::max(ceil(dx / w) * one_dx, ceil(dw / (slots - w)) * one_dw);
+        if (cost < best.cost)
+            best = Together{(int)std::min<double>(w, dx), (int)std::min<double>(slots - w, dw), cost};
     }
     return best;
 }
@@ -318,6 +350,7 @@ struct BackwardPlan {
     bool own_dz;      // dz in the workspace (else dy is dz)
     mag::MmOperand dz;
     Shape dx, dw;
+    Together two;     // both at once, if that costs less
     float* partial;
     float* column_part;
 };
@@ -333,7 +366,10 @@ size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& 
         // x and weight are both read across the reduction of the product they enter
         const Operand x = operand(a->x, kind, false), w = operand(a->weight, kind, false);
         const Shape dx = choose(M, K, N, kind, 1, false), dw = choose(N, K, M, kind, 1, false);
-        const double cost = dx.cost + dw.cost + packing_cost((x.packed ? M * K : 0) + (w.packed ? N * K : 0), kind);
+        Together two = choose_two(M, N, K, kind);
+        if (two.cost > dx.cost + dw.cost || pl.skinny || !x.op.mc || !w.op.mc) two.cost = 0.0;
+        const double cost = (two.cost > 0.0 ? two.cost : dx.cost + dw.cost) +
+                            packing_cost((x.packed ? M * K : 0) + (w.packed ? N * K : 0), kind);
         if (cost >= least) break;
         least = cost;
         pl.kind = kind;
@@ -341,6 +377,7 @@ size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& 
         pl.w = w;
         pl.dx = dx;
         pl.dw = dw;
+        pl.two = two;
     }
     pl.dy = operand(a->dy, pl.kind, true);
     // (as for the sizes: room for dz whether or not dy can stand in for it)
@@ -351,6 +388,7 @@ size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& 
     } else {
         pl.dz = pl.dy.op;
     }
+    if (pl.dz.mc) pl.two.cost = 0.0;
     Carve c{static_cast<char*>(ws)};
     if (pl.skinny) {
         pl.w.packed = false;
@@ -652,11 +690,29 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
             "linear_backward launch");
     mag::Mm p{};
     p.in_parts = pl.kind == mag::MM_F32_PARTS;
-    p.batch = 1;
+    p.batch = p.splits = 1;
     p.partial = pl.partial;
-    p.S = K;
     p.partial_ld = up8(K);
-    p.a = pl.dz;
+    p.S = K;
+    p.e.vec = 1;
+    mag::Mm q = p;
+    p.a = q.a = pl.dz;
+    q.a.mc = !pl.dz.mc;
+    p.b = pl.w.op;
+    p.R = M;
+    p.K = N;
+    p.e.y = a->dx.data;
+    p.e.y_ld = a->dx.row_stride;
+    q.b = pl.x.op;
+    q.R = N;
+    q.K = M;
+    q.e.y = a->dweight.data;
+    q.e.y_ld = a->dweight.row_stride;
+    if (dx && dw && pl.two.cost > 0.0) {
+        TRY_HIP(mag::launch_mm_two(p, q, pl.kind, pl.two.wgs_dx, pl.two.wgs_dw, stream),
+                "linear_backward launch");
+        return MAG_OK;
+    }
     if (dx && pl.skinny) {
         mag::SkinnyParams s{};
         s.x = pl.dz.p;
@@ -671,25 +727,12 @@ int mag_linear_backward(const mag_linear_backward_args* a, void* workspace, size
         s.e.y_ld = a->dx.row_stride;
         TRY_HIP(mag::launch_skinny(s, a->dtype, stream), "linear_backward launch");
     } else if (dx) {
-        p.b = pl.w.op;
-        p.R = M;
-        p.K = N;
         p.splits = pl.dx.splits;
-        p.e.y = a->dx.data;
-        p.e.y_ld = a->dx.row_stride;
-        p.e.vec = 1;
         TRY(launch_linear(p, pl.kind, pl.dx.tile, stream));
     }
     if (dw) {
-        p.a.mc = !pl.dz.mc;
-        p.b = pl.x.op;
-        p.R = N;
-        p.K = M;
-        p.splits = pl.dw.splits;
-        p.e.y = a->dweight.data;
-        p.e.y_ld = a->dweight.row_stride;
-        p.e.vec = 1;
-        TRY(launch_linear(p, pl.kind, pl.dw.tile, stream));
+        q.splits = pl.dw.splits;
+        TRY(launch_linear(q, pl.kind, pl.dw.tile, stream));
     }
     return MAG_OK;
 }

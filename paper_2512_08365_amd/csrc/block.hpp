@@ -78,6 +78,9 @@ hipError_t launch_mm_f32_parts(const Mm& p, int tile, hipStream_t stream);   // 
 // kind: MM_BF16 ... (tiles as above, no 256)
 hipError_t launch_mm_partial(const Mm& p, int kind, int tile, hipStream_t stream);
 hipError_t launch_mm_orth(const Mm& p, int tile, hipStream_t stream);
+// two unsplit products in 64 tiles, dx's a along the reduction, the other operands
+// across it; kind: not MM_HALVES
+hipError_t launch_mm_two(const Mm& dx, const Mm& dw, int kind, int wgs_dx, int wgs_dw, hipStream_t stream);
 // the partial sums of a split product added up and stored (dtype: of y)
 hipError_t launch_mm_join(const Mm& p, int dtype, hipStream_t stream);
 hipError_t launch_orth_join(const Mm& p, hipStream_t stream);

@@ -472,10 +472,28 @@ constexpr int wgs_per_cu(int side, int P, int stages)
 //   one part:    the halves of a step, 0 0 | 1 1
 //   two parts:   high high | low high | high low
 //   three parts: 1 1 | 1 2, 2 1, 2 2 | 3 1, 1 3 (the products below 2^-24 left out)
-template <class T, class TO, int EPI, int SIDE, int STAGES, int P, bool AMC, bool BMC>
-__global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
+//
+// This workgroup: pieces of work first(), first() + stride(), ...  (p by value: by
+// reference, the 256 tile spills 15 registers more.)
+template <int BYTES, int STAGES, int COLS>
+struct Lds {
+    // each tile an array of its own: what one is read from is not what is being
+    // filled
+    char (&la0)[BYTES], (&lb0)[BYTES], (&la1)[BYTES], (&lb1)[BYTES];
+    char (&la2)[STAGES > 2 ? BYTES : 16], (&lb2)[STAGES > 2 ? BYTES : 16];
+    char (&la3)[STAGES > 2 ? BYTES : 16], (&lb3)[STAGES > 2 ? BYTES : 16];
+    char (&lo)[4 * 16 * COLS * 4];
+};
+#define MM_LDS(T, SIDE, STAGES, P)                                                                     \
+    constexpr int BYTES_ = Tile<T, SIDE, false, P, 256>::BYTES, MORE_ = STAGES > 2 ? BYTES_ : 16;      \
+    __shared__ __attribute__((aligned(1024))) char la0[BYTES_], lb0[BYTES_], la1[BYTES_], lb1[BYTES_]; \
+    __shared__ __attribute__((aligned(1024))) char la2[MORE_], lb2[MORE_], la3[MORE_], lb3[MORE_];     \
+    __shared__ __attribute__((aligned(1024))) char lo[4 * 16 * (SIDE / 2) * 4];                        \
+    const Lds<BYTES_, STAGES, SIDE / 2> lds{la0, lb0, la1, lb1, la2, lb2, la3, lb3, lo}
+
+template <class T, class TO, int EPI, int SIDE, int STAGES, int P, bool AMC, bool BMC, class First, class Stride, class Arrays>
+__device__ __forceinline__ void walk(Mm p, First first, Stride stride, const Arrays& lds)
 {
-#ifdef __HIP_DEVICE_COMPILE__
     constexpr int THREADS = 256, W = 2;          // 2 x 2 waves
     constexpr int COLS = SIDE / W, F = COLS / 16;  // a wave's rows and columns, in 16s
     constexpr int STEP = step_of<T>(P);
@@ -485,13 +503,9 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
     using TB = Tile<T, SIDE, BMC, P, THREADS>;
     constexpr int L = TA::LOADS;
     static_assert(TA::LOADS == TB::LOADS, "");
-    // each tile an array of its own: what one is read from is not what is being
-    // filled
-    __shared__ __attribute__((aligned(1024))) char la0[TA::BYTES], lb0[TB::BYTES];
-    __shared__ __attribute__((aligned(1024))) char la1[TA::BYTES], lb1[TB::BYTES];
-    __shared__ __attribute__((aligned(1024))) char la2[STAGES > 2 ? TA::BYTES : 16], lb2[STAGES > 2 ? TB::BYTES : 16];
-    __shared__ __attribute__((aligned(1024))) char la3[STAGES > 2 ? TA::BYTES : 16], lb3[STAGES > 2 ? TB::BYTES : 16];
-    __shared__ __attribute__((aligned(1024))) char lo[4 * 16 * COLS * 4];
+    auto &la0 = lds.la0, &lb0 = lds.lb0, &la1 = lds.la1, &lb1 = lds.lb1;
+    auto &la2 = lds.la2, &lb2 = lds.lb2, &la3 = lds.la3, &lb3 = lds.lb3;
+    auto& lo = lds.lo;
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
     const int lane = (int)threadIdx.x & 63;
@@ -673,7 +687,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
         }
     };
 
-    uint32_t g = blockIdx.x;
+    uint32_t g = first();
     begin_tile(g);
     while (true) {
         meet(None{});
@@ -699,7 +713,7 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
         const int64_t rt = r0 + wr, st = s0 + ws;
         const int64_t bt = plane;
         const bool mirrored = mirror;
-        g += gridDim.x;
+        g += stride();
         if (g < units) begin_tile(g);
 
         // The sums go to rows through a wave's own piece of LDS, 16 rows at a
@@ -799,7 +813,41 @@ __global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
         }
         if (g >= units) break;
     }
+}
+
+template <class T, class TO, int EPI, int SIDE, int STAGES, int P, bool AMC, bool BMC>
+__global__ __launch_bounds__(256, wgs_per_cu(SIDE, P, STAGES)) void k_mm(Mm p)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    MM_LDS(T, SIDE, STAGES, P);
+    walk<T, TO, EPI, SIDE, STAGES, P, AMC, BMC>(
+        p, [] { return blockIdx.x; }, [] { return gridDim.x; }, lds);
 #endif
+}
+
+// A small layer's two gradients side by side, which would leave CUs idle one
+// after the other (1,000 x 777 by 2,050 half: 13 and 15 us, together 19): the
+// first `wgs` workgroups walk dx = dz weight, the others dweight = dz^T x.
+template <class T, class TO, int P>
+__global__ __launch_bounds__(256, wgs_per_cu(64, P, 4)) void k_mm_two(Mm dx, Mm dw, uint32_t wgs)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    MM_LDS(T, 64, 4, P);
+    if (blockIdx.x < wgs)
+        walk<T, TO, MM_LINEAR, 64, 4, P, false, true>(
+            dx, [] { return blockIdx.x; }, [=] { return wgs; }, lds);
+    else
+        walk<T, TO, MM_LINEAR, 64, 4, P, true, true>(
+            dw, [=] { return blockIdx.x - wgs; }, [=] { return gridDim.x - wgs; }, lds);
+#endif
+}
+
+template <class T, class TO, int P>
+hipError_t launch_mm_two_tiles(const Mm& dx, const Mm& dw, int wgs_dx, int wgs_dw, hipStream_t stream)
+{
+    hipLaunchKernelGGL((k_mm_two<T, TO, P>), dim3((unsigned)(wgs_dx + wgs_dw)), dim3(256), 0, stream, dx, dw,
+                       (uint32_t)wgs_dx);
+    return hipGetLastError();
 }
 
 template <class T, class TO, int EPI, int SIDE, int STAGES, int P>
