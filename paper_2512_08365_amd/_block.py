@@ -70,7 +70,7 @@ def _matrix(x, dtype, index, name):
 def _vector(x, dtype, index, width, name):
     if not isinstance(x, torch.Tensor) or x.dtype is not dtype or x.get_device() != index:
         _refuse(x, dtype, index, name)
-    if x.dim() != 1 or x.shape[0] != width or (width > 1 and x.stride(0) != 1):
+    if x.shape != (width,) or not x.is_contiguous():
         raise MagnetonError(N.MAG_E_SIZE, f"{name} must be {width} contiguous values")
     return x.data_ptr()
 
@@ -206,15 +206,14 @@ def _norm_args(x, weight, bias, y, dy, dx, mean, rstd, dweight, dbias, eps):
     dt, ty, dev = _dtype(x, "x"), x.dtype, x.get_device()
     mx = _matrix(x, ty, dev, "x")
     _, rows, width, _, _ = mx
-    wt = ty
+    wt, wdt = ty, dt
     for some in (weight, bias, dweight, dbias):
         if some is not None:
-            _dtype(some, "weight")
-            wt = some.dtype
+            wt, wdt = some.dtype, _dtype(some, "weight")
             break
     f32 = torch.float32
     return N.NORM_ARGS.pack(
-        dt, _DTYPES[wt], *mx, *(_NONE if y is None else _matrix(y, ty, dev, "out")),
+        dt, wdt, *mx, *(_NONE if y is None else _matrix(y, ty, dev, "out")),
         *(_NONE if dy is None else _matrix(dy, ty, dev, "dy")),
         *(_NONE if dx is None else _matrix(dx, ty, dev, "dx")),
         0 if weight is None else _vector(weight, wt, dev, width, "weight"),
@@ -232,8 +231,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, *, statistics=None, out=None
     the mean and rstd too (what layer_norm_backward reads).  out may be x itself.
     Returns out, or (out, mean, rstd)."""
     lib = _lib()
-    _dtype(x, "x")
     if out is None:
+        _dtype(x, "x")
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     mean = rstd = None
     if statistics is True:

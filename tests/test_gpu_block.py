@@ -692,6 +692,38 @@ def test_orthogonalize_steps_and_polynomials(steps):
     check_orthogonalize(1, 100, 168, "f32", steps=steps, coeff=(1.5, -0.5, 0.0))
 
 
+# shapes much wider or taller than their short side, several steps of which may be
+# taken at once, over spectra of full rank, of low rank and falling over six
+# decades, by a steep polynomial and by a flat one: the bound of
+# check_orthogonalize, and the quarter of a rounding that taking them at once may add
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("coeff", [COEFF, (1.5, -0.5, 0.0), (2.0, -1.5, 0.5)])
+@pytest.mark.parametrize("size,steps,spectrum", [((520, 4100), 2, "full"), ((520, 4100), 7, "falling"),
+                                                 ((96, 6000), 4, "low"), ((2100, 700), 5, "falling"),
+                                                 ((1030, 4104), 3, "low"), ((1030, 4104), 6, "full")])
+def test_orthogonalize_long_sides(size, steps, spectrum, coeff, ty):
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    print(f"[case] orthogonalize {size} {ty} {steps} {spectrum} {coeff}", flush=True)
+    g = _gen(33)
+    rows, cols = size
+    x = torch.randn(rows, cols, generator=g, device="cuda")
+    if spectrum != "full":
+        m = min(size)
+        side = torch.randn(m, m, generator=g, device="cuda") / math.sqrt(m)
+        scale = torch.logspace(0, -6, m, device="cuda")
+        if spectrum == "low":
+            scale = (torch.arange(m, device="cuda") < m // 4).float()
+        x = (side * scale) @ x if rows <= cols else x @ (side * scale)
+    x = (x * 0.02).to(_dt(ty))
+    want = plain_orthogonalize(x, steps, coeff, 1e-7, torch.float64)
+    own = plain_orthogonalize(x, steps, coeff, 1e-7, torch.float32)
+    unit = float((own.double() - want).norm() / want.norm())
+    got = float((mag.orthogonalize(x, steps, coeff).double() - want).norm() / want.norm())
+    bound = 16 * max(unit, 2.0 ** -22) + 1.25 * _u(ty)
+    assert got <= bound, (got, unit, bound)
+
+
 def test_orthogonalize_scales_zero_and_not_finite():
     torch = _torch()
     import paper_2512_08365_amd as mag
