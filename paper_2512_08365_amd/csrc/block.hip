@@ -163,9 +163,10 @@ struct Shape {
     double cost;   // estimated, in us
 };
 
-// What a workgroup's step, its tile beside the steps, and the call cost, in us,
-// measured with 256 and 512 workgroups over reductions of 512 and 4,096: alone
-// on a CU, and with a second one (0: there is no room for one).
+// What a workgroup's step, its tile beside the steps, and the call cost, in us:
+// alone on a CU, and with a second one (0: there is no room for one).  bfloat16 and
+// half are fitted to 148 products of sides 256 to 4,096 by 512 to 8,192 (most within
+// 6 %), the others to 256 and 512 workgroups over reductions of 512 and 4,096.
 struct TileCost {
     double alone, shared, tile;
 };
@@ -174,11 +175,11 @@ constexpr double JOIN_COST = 3.5;           // a split product's second launch
 constexpr double PARTIAL_BYTES = 4.5e6;     // of partial sums a us, written or read
 const TileCost TILE_COST[mag::MM_KINDS][mag::TILES] = {
     // 64 (four steps in LDS), 128, 256
-    {{0.19, 0.35, 1.8}, {0.64, 0.80, 3.5}, {1.43, 0.0, 11.5}},   // bfloat16: 64 k a step
-    {{0.19, 0.35, 1.8}, {0.64, 0.80, 3.5}, {1.43, 0.0, 11.5}},   // half
+    {{0.165, 0.33, 1.7}, {0.52, 0.77, 4.4}, {1.15, 0.0, 10.0}},   // bfloat16: 64 k a step
+    {{0.165, 0.33, 1.7}, {0.52, 0.77, 4.4}, {1.15, 0.0, 10.0}},   // half
     {{0.53, 1.00, 1.8}, {0.0, 0.0, 0.0}, {0.0, 0.0, 0.0}},       // fp32: 32 k
     {{0.35, 0.0, 3.6}, {1.20, 0.0, 10.5}, {0.0, 0.0, 0.0}},      // three parts: 32 k, six products
-    {{0.22, 0.36, 1.8}, {0.73, 1.19, 6.5}, {2.13, 0.0, 10.5}},   // two parts: 32 k, three products
+    {{0.22, 0.36, 1.8}, {0.58, 1.19, 6.5}, {2.13, 0.0, 10.5}},   // two parts: 32 k, three products
 };
 // (fp32 as it lies is bound by its instruction and gains nothing from a larger
 // tile; three parts cost six products of bfloat16 and a pass to cut them, and win
@@ -187,8 +188,8 @@ const TileCost TILE_COST[mag::MM_KINDS][mag::TILES] = {
 
 // The tile and split of the reduction that these costs make fastest: large tiles
 // move the least data where there are enough of them for the 256 CUs, small ones
-// and splits fill the CUs otherwise (1,024 cubed in bfloat16: 8 us with 64, 13 us
-// with 128; 4,096 cubed: 109 us with 256, 120 us with 128).  kind: MM_BF16 ...
+// and splits fill the CUs otherwise (1,024 cubed in bfloat16: 7 us with 64, 12 us
+// with 128; 4,096 cubed: 101 us with 256, 113 us with 128).  kind: MM_BF16 ...
 Shape choose(int64_t R, int64_t S, int64_t K, int kind, int64_t batch, bool symmetric)
 {
     constexpr int64_t CUS = 256;
@@ -509,7 +510,7 @@ double most_of_polynomial(double a, double b, double c, double u)
 // How many steps from step i on are done on the short side.  With Q the product of
 // their U = a I + b A + c A A, X <- Q X is all that is as long as X, and the next
 // A is U A U: of 2,048 x 8,192, three steps and two are 40 products of a side
-// cubed where five single ones are 65 (1,650 and 1,250 us).  What an A so made
+// cubed where five single ones are 65 (1,650 and 1,222 us).  What an A so made
 // costs is accuracy: its rounding, 2^-21 of the largest eigenvalue, grows by the
 // slope of one step's map of eigenvalues, l (a + b l + c l l)^2, from step to step
 // and enters U times the slope of that.  A quarter of the result's own rounding is

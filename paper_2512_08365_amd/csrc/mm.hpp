@@ -872,4 +872,17 @@ hipError_t launch_mm_tile(const Mm& p, hipStream_t stream)
     return hipGetLastError();
 }
 
+// The 128 tile, with four steps in LDS where every workgroup has a CU of its own
+// and the reduction is long (2,048 x 2,048 bfloat16: by 8,192 74 us, with two steps
+// 78 us; by 1,024, where starting counts, 16 and 13 us).
+template <class T, class TO, int EPI, int P>
+hipError_t launch_mm_128(const Mm& p, hipStream_t stream)
+{
+    const int64_t tr = (p.R + 127) / 128, ts = (p.S + 127) / 128;
+    const int64_t units = (p.symmetric ? tr * (tr + 1) / 2 : tr * ts) * p.splits * p.batch;
+    if (units <= device_cu_count() && p.K >= 32 * step_of<T>(P))
+        return launch_mm_tile<T, TO, EPI, 128, 4, P>(p, stream);
+    return launch_mm_tile<T, TO, EPI, 128, 2, P>(p, stream);
+}
+
 }  // namespace mag

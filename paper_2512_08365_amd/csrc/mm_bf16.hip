@@ -6,7 +6,7 @@ namespace mag {
 hipError_t launch_mm_bf16(const Mm& p, int tile, hipStream_t stream)
 {
     if (tile == TILE_256) return launch_mm_tile<bf16, bf16, MM_LINEAR, 256, 2, 1>(p, stream);
-    if (tile == TILE_128) return launch_mm_tile<bf16, bf16, MM_LINEAR, 128, 2, 1>(p, stream);
+    if (tile == TILE_128) return launch_mm_128<bf16, bf16, MM_LINEAR, 1>(p, stream);
     return launch_mm_tile<bf16, bf16, MM_LINEAR, 64, 4, 1>(p, stream);
 }
 
