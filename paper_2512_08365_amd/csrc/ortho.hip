@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void k_orth_join(Mm p)
     __shared__ float block[64][65];
     const uint32_t ts = (uint32_t)((p.S + 63) / 64);
     uint32_t bi = blockIdx.x / ts, bj = blockIdx.x % ts;
-    if (p.symmetric) tile_above(blockIdx.x, bi, bj);
+    if (p.symmetric) tile_above(blockIdx.x, ts, bi, bj);
     const int64_t r0 = (int64_t)bi * 64, s0 = (int64_t)bj * 64, bt = blockIdx.y;
     const bool mirror = p.symmetric && bi != bj;
     const int64_t across = p.o.z ? p.o.z_ld / 2 : p.S;
