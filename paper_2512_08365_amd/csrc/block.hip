@@ -510,7 +510,7 @@ double most_of_polynomial(double a, double b, double c, double u)
 // How many steps from step i on are done on the short side.  With Q the product of
 // their U = a I + b A + c A A, X <- Q X is all that is as long as X, and the next
 // A is U A U: of 2,048 x 8,192, three steps and two are 40 products of a side
-// cubed where five single ones are 65 (1,650 and 1,222 us).  What an A so made
+// cubed where five single ones are 65 (1,660 and 1,190 us).  What an A so made
 // costs is accuracy: its rounding, 2^-21 of the largest eigenvalue, grows by the
 // slope of one step's map of eigenvalues, l (a + b l + c l l)^2, from step to step
 // and enters U times the slope of that.  A quarter of the result's own rounding is
