@@ -93,7 +93,6 @@ bool same_shape(const mag_matrix& m, int64_t rows, int64_t cols)
 
 // ----------------------------------------------------------------- operands
 
-constexpr int64_t MOST_LD = 1LL << 22;  // 256 rows of it stay within 31 bits of bytes
 int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 // bytes of an element of a product's operand (kind: MM_*), elements of a packed
 // row of n: whole lines of 128 bytes, but for narrow ones (a step's 128 bytes of a
@@ -105,6 +104,19 @@ int64_t packed_ld(int64_t n, int kind)
     if (kind == mag::MM_F32_PARTS) return n > 32 ? (n + 63) / 64 * 192 : 96;
     const int64_t line = 128 / (int64_t)part_size(kind);
     return n > line ? (n + line - 1) / line * line : up8(n);
+}
+
+// The largest ld of an operand (kind: MM_*): a tile's loads have 31 bits for a
+// byte's offset from the tile's first one, and reach over a step of the reduction
+// (across: its elements are lines) or over the rows of the kind's largest tile.
+int64_t most_ld(int kind, bool across)
+{
+    const bool two_bytes = kind == mag::MM_BF16 || kind == mag::MM_F16;
+    const int64_t lines = across ? (two_bytes ? 64 : 32)
+                                 : mag::TILE_SIDE[kind == mag::MM_F32         ? mag::TILE_64
+                                                  : kind == mag::MM_F32_PARTS ? mag::TILE_128
+                                                                              : mag::TILE_256];
+    return (1LL << 31) / (lines * (int64_t)part_size(kind));
 }
 
 // How a product reads a matrix: where it lies, or as rows packed into the
@@ -124,9 +136,9 @@ Operand operand(const mag_matrix& m, int kind, bool along)
     if (kind != mag::MM_F32_PARTS && aligned(m.data, 16)) {
         const int64_t per = 16 / (int64_t)part_size(kind);
         const bool by_rows = (m.cols <= 1 || m.col_stride == 1) && m.cols % per == 0 &&
-                             (m.rows <= 1 || (m.row_stride % per == 0 && m.row_stride < MOST_LD));
+                             (m.rows <= 1 || (m.row_stride % per == 0 && m.row_stride <= most_ld(kind, !along)));
         const bool by_cols = m.row_stride == 1 && m.rows % per == 0 && m.rows > 1 &&
-                             (m.cols <= 1 || (m.col_stride % per == 0 && m.col_stride < MOST_LD));
+                             (m.cols <= 1 || (m.col_stride % per == 0 && m.col_stride <= most_ld(kind, along)));
         if (by_rows || by_cols) {
             o.op.p = m.data;
             o.op.ld = by_rows ? (m.rows <= 1 ? 0 : m.row_stride) : (m.cols <= 1 ? 0 : m.col_stride);
@@ -134,9 +146,11 @@ Operand operand(const mag_matrix& m, int kind, bool along)
             return o;
         }
     }
-    // (packed as it lies: by columns if these are what is contiguous)
+    // (packed as it lies: by columns if these are what is contiguous, unless there are
+    // too many rows; by rows ld follows from a layer's features and is never too large)
     o.packed = true;
-    o.by_cols = m.rows > 1 && m.row_stride == 1 && m.col_stride != 1;
+    o.by_cols = m.rows > 1 && m.row_stride == 1 && m.col_stride != 1 &&
+                packed_ld(m.rows, kind) <= most_ld(kind, along);
     o.op.ld = packed_ld(o.by_cols ? m.rows : m.cols, kind);
     o.op.mc = o.by_cols == along;
     o.bytes = (size_t)((o.by_cols ? m.cols : m.rows) * o.op.ld) * part_size(kind);
@@ -381,8 +395,10 @@ size_t plan_backward(const mag_linear_backward_args* a, void* ws, BackwardPlan& 
         pl.two = two;
     }
     pl.dy = operand(a->dy, pl.kind, true);
-    // (as for the sizes: room for dz whether or not dy can stand in for it)
-    pl.own_dz = a->activation != MAG_ACT_NONE || pl.dy.packed || !a->dy.data || (pl.skinny && pl.dy.op.mc);
+    // (as for the sizes: room for dz whether or not dy can stand in for it; dz is read
+    // along the reduction by one product and across it by the other)
+    pl.own_dz = a->activation != MAG_ACT_NONE || pl.dy.packed || !a->dy.data || (pl.skinny && pl.dy.op.mc) ||
+                pl.dy.op.ld > most_ld(pl.kind, false);
     if (pl.own_dz) {
         pl.dz = mag::MmOperand{};
         pl.dz.ld = packed_ld(N, pl.kind);

@@ -1,0 +1,109 @@
+"""What the feed-forward block's calls launch, for which sizes: their host code
+over launches that are only written down (block_launches.cpp), so no GPU is
+needed and no kernel runs."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+FAKE = 1 << 20
+NONE = (0, 0, 0, 0, 0)
+F32, F16, BF16 = 0, 1, 2
+# products: bfloat16, half, fp32, fp32 in three parts, an update's two halves
+K_BF16, K_F16, K_F32, K_PARTS, K_HALVES = range(5)
+SIDE = (64, 128, 256)
+
+
+class Calls:
+    def __init__(self, so):
+        from paper_2512_08365_amd import _build, _native
+        self.N = _native
+        subprocess.check_call([_build.hipcc(), "-x", "hip", "--cuda-host-only", "-std=c++17", "-O1",
+                               "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-o", so,
+                               os.path.join(HERE, "block_launches.cpp")])
+        self.lib = ctypes.CDLL(so)
+        self.lib.launches.restype = self.lib.last_error.restype = ctypes.c_char_p
+
+    def _call(self, name, args):
+        n = ctypes.c_size_t(0)
+        assert getattr(self.lib, f"mag_{name}_workspace_size")(args, ctypes.byref(n)) == 0, \
+            self.lib.last_error()
+        self.lib.clear_launches()
+        rc = getattr(self.lib, f"mag_{name}")(args, ctypes.c_void_p(FAKE), n, None)
+        assert rc == 0, (rc, self.lib.last_error())
+        return [{k: v if k == "what" else float(v) if k in ("scale", "mix", "diagonal") else int(v)
+                 for k, v in (f.split("=") for f in line.split())}
+                for line in self.lib.launches().decode().splitlines()]
+
+    def linear(self, dtype, x, weight):
+        y = _rows(x[1], weight[1])
+        return self._call("linear", self.N.LINEAR_ARGS.pack(dtype, 0, *x, *weight, *NONE, *NONE, *y, 0))
+
+    def linear_backward(self, dtype, x, weight, dy):
+        return self._call("linear_backward", self.N.LINEAR_BACKWARD_ARGS.pack(
+            dtype, 0, *x, *weight, *NONE, *dy, *_rows(x[1], x[2]), *_rows(weight[1], x[2]), FAKE))
+
+    def orthogonalize(self, dtype, rows, cols, steps=5, batch=1, coefficients=(3.4445, -4.775, 2.0315)):
+        m = _rows(rows, cols)
+        return self._call("orthogonalize", self.N.ORTHOGONALIZE_ARGS.pack(
+            dtype, steps, batch, *m, *m, rows * cols, rows * cols, *coefficients, 1e-7))
+
+
+@pytest.fixture(scope="module")
+def calls(tmp_path_factory):
+    return Calls(str(tmp_path_factory.mktemp("launches") / "block_launches.so"))
+
+
+def _rows(rows, cols, gap=0):
+    return (FAKE, rows, cols, cols + gap, 1)
+
+
+def _columns(rows, cols, gap=0):
+    return (FAKE, rows, cols, 1, rows + gap)
+
+
+def _products(launches):
+    return [p for p in launches if p["what"] in ("linear", "partial", "two", "update")]
+
+
+def _reach(p, o):
+    """bytes from a tile's first one to the end of what its loads read of operand o"""
+    parts = {K_PARTS: 3, K_HALVES: 2}.get(p["kind"], 1)
+    size = 4 if p["kind"] == K_F32 else 2
+    step = 64 if p["kind"] in (K_BF16, K_F16) else 32
+    side = SIDE[p["tile"]]
+    if p[f"{o}_mc"]:
+        lines, line = min(step, p["K"]), side * parts * size
+    else:
+        lines, line = min(side, p["R" if o == "a" else "S"]), step * parts * size
+    return (lines - 1) * p[f"{o}_ld"] * size + line
+
+
+ROWS = [40, 3_000_000, 3_000_001, 4_194_304, 4_300_000, 8_400_001, 11_600_000, 17_100_000, 20_000_000,
+        35_000_000, (1 << 30) - 8, 1 << 30]
+FEATURES = [(8, 8), (64, 16), (65, 70), (512, 512), (4096, 257), (257, 4096), (1 << 21, 8), (8, 1 << 21)]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("lay", [_rows, _columns])
+def test_offsets_inside_a_tile_stay_below_31_bits(calls, lay, dtype):
+    """a load's offset from its tile's first byte has 31 bits; beyond them lie zeros"""
+    for rows in ROWS:
+        for inner, outer in FEATURES:
+            for gap in (0, 3):
+                x, dy = lay(rows, inner, gap), lay(rows, outer, gap)
+                for w in (_rows(outer, inner, gap), _columns(outer, inner, gap)):
+                    for p in _products(calls.linear(dtype, x, w) + calls.linear_backward(dtype, x, w, dy)):
+                        for o in ("a", "b"):
+                            assert _reach(p, o) < (1 << 31) - 16, (rows, inner, outer, gap, p)
+
+
+@pytest.mark.parametrize("rows,cols", [(8, 1 << 21), (1 << 21, 8), (1 << 21, 3000), (3000, 1 << 21)])
+def test_offsets_of_long_updates_stay_below_31_bits(calls, rows, cols):
+    for dtype in (F32, F16, BF16):
+        for p in _products(calls.orthogonalize(dtype, rows, cols)):
+            for o in ("a", "b"):
+                assert _reach(p, o) < (1 << 31) - 16, p
