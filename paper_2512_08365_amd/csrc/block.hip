@@ -878,8 +878,9 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
     const int64_t m = pl.m, n = pl.n;
     const int64_t x_batch = a->g.rows * pl.ld;
     const int64_t a_batch = m * pl.lda;
-    // halves hold a value times a power of two that takes its bound near 2^15
-    auto scale_for = [](double bound) { return ldexp(1.0, 15 - ilogb(bound) - 1); };
+    // halves hold a value times a power of two that takes its bound near 2^15 (bounds
+    // from 2^-100 on: a polynomial that contracts takes them to zero)
+    auto scale_for = [](double bound) { return ldexp(1.0, 15 - ilogb(std::max(bound, 0x1p-100)) - 1); };
 
     mag::OrthParams o{};
     o.g = a->g.data;
@@ -948,7 +949,7 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         for (int j = i; j < i + group; ++j) {
             const double u2 = most[j] * most[j];
             const double of_u = fabs(a->b) * u2 + fabs(a->c) * u2 * u2 + (group > 1 ? fabs(a->a) : 0.0);
-            const double su = scale_for(1.01 * of_u + 0x1p-100);
+            const double su = scale_for(1.01 * of_u);
             // U = b A + c A A, of a group a I + b A + c A A
             const int u = j == i ? 1 : q % 3 + 1;
             mixed(side[A], a->b * su / sa);
@@ -960,7 +961,7 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
                 sq = su;
             } else {
                 // Q <- U Q
-                const double next = scale_for(1.01 * bound + 0x1p-100);
+                const double next = scale_for(1.01 * bound);
                 TRY(symmetric(side[u], side[q], m, next / (su * sq), other, pl.square));
                 sq = next;
                 q = other;
@@ -968,8 +969,8 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
             if (j + 1 < i + group) {
                 // A <- U A U
                 const int t = u == q ? u % 3 + 1 : 6 - q - u;
-                const double st = scale_for(1.01 * most[j] * most[j + 1] + 0x1p-100);
-                const double next = scale_for(1.01 * most[j + 1] * most[j + 1] + 0x1p-100);
+                const double st = scale_for(1.01 * most[j] * most[j + 1]);
+                const double next = scale_for(1.01 * most[j + 1] * most[j + 1]);
                 TRY(symmetric(side[u], side[A], m, st / (su * sa), t, pl.square));
                 TRY(symmetric(side[u], side[t], m, next / (su * st), A, pl.square));
                 sa = next;
@@ -979,7 +980,7 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
         i += group;
         // X <- rest X + Q X, or its transpose <- rest X^T + X^T Q (Q symmetric)
         const bool last = i == a->steps;
-        const double next = scale_for(most[i] + 0x1p-100), out = last ? 1.0 : next;
+        const double next = scale_for(most[i]), out = last ? 1.0 : next;
         X.mc = 0;
         if (rest != 0.0) mixed(X, rest * out / sx);
         p.symmetric = 0;

@@ -2,7 +2,9 @@
 over launches that are only written down (block_launches.cpp), so no GPU is
 needed and no kernel runs."""
 import ctypes
+import math
 import os
+import random
 import subprocess
 
 import pytest
@@ -107,3 +109,24 @@ def test_offsets_of_long_updates_stay_below_31_bits(calls, rows, cols):
         for p in _products(calls.orthogonalize(dtype, rows, cols)):
             for o in ("a", "b"):
                 assert _reach(p, o) < (1 << 31) - 16, p
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("size", [(40, 72), (96, 6000), (700, 100)])
+def test_scales_of_polynomials_that_contract_are_finite(calls, size, dtype):
+    """bounds that fall to zero, at once or step by step, beside ones that grow"""
+    rng = random.Random(7)
+    drawn = [tuple(rng.choice((-1, 1)) * 10 ** rng.uniform(-30, e) for e in (2, 1, 1)) for _ in range(50)]
+    for coefficients in [(0, 0, 0), (1e-200, 0, 0), (0.1, 0, 0), (1e-3, 1e-3, 0), (1e-160, 1e-160, 1e-160),
+                         (0.5, -0.25, 0.1), (2, -1.5, 0.5), (1.5, 0, 0), *drawn]:
+        for steps in (1, 2, 3, 8, 64):
+            try:
+                launches = calls.orthogonalize(dtype, *size, steps, 2, coefficients)
+            except AssertionError:
+                assert b"grows" in calls.lib.last_error()
+                continue
+            for p in launches:
+                if p["what"] == "begin":
+                    assert 0 < p["scale"] < math.inf
+                elif p["what"] in ("update", "partial"):
+                    assert all(math.isfinite(p[k]) for k in ("scale", "mix", "diagonal")), (coefficients, p)

@@ -1,0 +1,40 @@
+"""The feed-forward block's operators at values at the ends of their range."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    return torch
+
+
+def _normal(seed, *shape):
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("size", [(40, 72), (96, 6000), (700, 100)], ids=lambda s: "x".join(map(str, s)))
+def test_updates_by_polynomials_that_contract(size, dtype):
+    """a X, again and again: exactly zero where the type's smallest number is larger,
+    a^steps X otherwise, off by the operands' 22 bits a step and the result's rounding"""
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    g = _normal(1, *size).to(getattr(torch, dtype))
+    for coefficients, steps in (((0, 0, 0), 1), ((0, 0, 0), 2), ((0, 0, 0), 5), ((1e-200, 0, 0), 3),
+                                ((0.1, 0, 0), 64), ((1e-20, 1e-20, 1e-20), 5)):
+        out = mag.orthogonalize(g, steps, coefficients)
+        assert not bool(out.any()), (coefficients, steps)
+    x = g.double() / (g.double().norm() + 1e-7)
+    unit = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}[dtype]
+    tiny = {"float32": 2.0 ** -149, "float16": 2.0 ** -25, "bfloat16": 2.0 ** -133}[dtype]
+    for steps in (1, 4, 10, 20):
+        out = mag.orthogonalize(g, steps, (0.5, 0.0, 0.0)).double()
+        want = x * 0.5 ** steps
+        # (two halves under a scale that takes 1 near 2^15: 22 bits, and 2^-39 below them)
+        bound = steps * (2.0 ** -21 * want.abs() + 2.0 ** -39 * 0.5 ** steps) + unit * want.abs() + tiny
+        assert bool(((out - want).abs() <= bound).all()), steps
