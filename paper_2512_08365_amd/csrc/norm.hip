@@ -177,31 +177,34 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
 }
 
 // rows too wide for the threads' registers, or whose elements are not neighbours
-// in memory: read three times (the second and third time from L2)
+// in memory: read three times (the second and third time from L2).  Workgroups
+// walk the rows: one a row would pass a launch's 2^32 threads from 2^22 rows on.
 template <class T, class W>
 __global__ __launch_bounds__(1024) void k_norm_wide(NormParams p)
 {
     __shared__ float2 lds[2][16];
-    const int64_t i = blockIdx.x, n = p.N;
-    const T* x = static_cast<const T*>(p.x) + i * p.x_rs;
-    float s = 0.0f, unused = 0.0f;
-    for (int64_t j = threadIdx.x; j < n; j += 1024) s += (float)x[j * p.x_cs];
-    row_sums<1024>(s, unused, lds[0]);
-    const float mean = s / (float)n;
-    s = 0.0f;
-    for (int64_t j = threadIdx.x; j < n; j += 1024) {
-        const float d = (float)x[j * p.x_cs] - mean;
-        s = fmaf(d, d, s);
-    }
-    row_sums<1024>(s, unused, lds[1]);
-    const float rstd = 1.0f / sqrtf(s / (float)n + p.eps);
+    const int64_t n = p.N;
     const W *w = static_cast<const W*>(p.weight), *b = static_cast<const W*>(p.bias);
-    for (int64_t j = threadIdx.x; j < n; j += 1024)
-        static_cast<T*>(p.y)[i * p.y_ld + j] =
-            (T)fmaf(((float)x[j * p.x_cs] - mean) * rstd, w ? (float)w[j] : 1.0f, b ? (float)b[j] : 0.0f);
-    if (threadIdx.x == 0) {
-        if (p.mean) p.mean[i] = mean;
-        if (p.rstd) p.rstd[i] = rstd;
+    for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
+        const T* x = static_cast<const T*>(p.x) + i * p.x_rs;
+        float s = 0.0f, unused = 0.0f;
+        for (int64_t j = threadIdx.x; j < n; j += 1024) s += (float)x[j * p.x_cs];
+        row_sums<1024>(s, unused, lds[0]);
+        const float mean = s / (float)n;
+        s = 0.0f;
+        for (int64_t j = threadIdx.x; j < n; j += 1024) {
+            const float d = (float)x[j * p.x_cs] - mean;
+            s = fmaf(d, d, s);
+        }
+        row_sums<1024>(s, unused, lds[1]);
+        const float rstd = 1.0f / sqrtf(s / (float)n + p.eps);
+        for (int64_t j = threadIdx.x; j < n; j += 1024)
+            static_cast<T*>(p.y)[i * p.y_ld + j] =
+                (T)fmaf(((float)x[j * p.x_cs] - mean) * rstd, w ? (float)w[j] : 1.0f, b ? (float)b[j] : 0.0f);
+        if (threadIdx.x == 0) {
+            if (p.mean) p.mean[i] = mean;
+            if (p.rstd) p.rstd[i] = rstd;
+        }
     }
 }
 
@@ -336,27 +339,33 @@ __global__ __launch_bounds__(256) void k_norm_back_wide_columns(NormParams p)
 template <class T, class W>
 __global__ __launch_bounds__(1024) void k_norm_back_wide(NormParams p)
 {
-    __shared__ float2 lds[16];
-    const int64_t i = blockIdx.x, n = p.N;
-    const T* x = static_cast<const T*>(p.x) + i * p.x_rs;
-    const T* dy = static_cast<const T*>(p.dy) + i * p.dy_rs;
+    __shared__ float2 lds[2][16];
+    const int64_t n = p.N;
     const W* w = static_cast<const W*>(p.weight);
-    const float mean = p.mean[i], rstd = p.rstd[i];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int64_t j = threadIdx.x; j < n; j += 1024) {
-        const float h = (float)dy[j * p.dy_cs] * (w ? (float)w[j] : 1.0f);
-        s1 += h;
-        s2 = fmaf(h, ((float)x[j * p.x_cs] - mean) * rstd, s2);
-    }
-    row_sums<1024>(s1, s2, lds);
-    s1 /= (float)n;
-    s2 /= (float)n;
-    for (int64_t j = threadIdx.x; j < n; j += 1024) {
-        const float h = (float)dy[j * p.dy_cs] * (w ? (float)w[j] : 1.0f);
-        const float xh = ((float)x[j * p.x_cs] - mean) * rstd;
-        static_cast<T*>(p.y)[i * p.y_ld + j] = (T)(rstd * (h - s1 - xh * s2));
+    int turn = 0;
+    for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
+        const T* x = static_cast<const T*>(p.x) + i * p.x_rs;
+        const T* dy = static_cast<const T*>(p.dy) + i * p.dy_rs;
+        const float mean = p.mean[i], rstd = p.rstd[i];
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int64_t j = threadIdx.x; j < n; j += 1024) {
+            const float h = (float)dy[j * p.dy_cs] * (w ? (float)w[j] : 1.0f);
+            s1 += h;
+            s2 = fmaf(h, ((float)x[j * p.x_cs] - mean) * rstd, s2);
+        }
+        row_sums<1024>(s1, s2, lds[turn ^= 1]);
+        s1 /= (float)n;
+        s2 /= (float)n;
+        for (int64_t j = threadIdx.x; j < n; j += 1024) {
+            const float h = (float)dy[j * p.dy_cs] * (w ? (float)w[j] : 1.0f);
+            const float xh = ((float)x[j * p.x_cs] - mean) * rstd;
+            static_cast<T*>(p.y)[i * p.y_ld + j] = (T)(rstd * (h - s1 - xh * s2));
+        }
     }
 }
+
+// workgroups that walk M rows, one at a time each
+dim3 wide_grid(int64_t M) { return dim3((unsigned)std::min<int64_t>(M, 1 << 16)); }
 
 // threads of a row of width n
 int threads_of(int64_t n) { return n <= 64 * HELD ? 64 : n <= 256 * HELD ? 256 : n <= 512 * HELD ? 512 : 1024; }
@@ -385,8 +394,8 @@ void forward_held(const NormParams& p, hipStream_t stream)
 template <class T, class W>
 hipError_t forward(const NormParams& p, hipStream_t stream)
 {
-    if (p.N > MOST_HELD || p.x_cs != 1)
-        hipLaunchKernelGGL((k_norm_wide<T, W>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
+    if (p.N > MOST_HELD || (p.N > 1 && p.x_cs != 1))   // (one column: its stride may be anything)
+        hipLaunchKernelGGL((k_norm_wide<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
     else if (p.N % 8 == 0)
         forward_held<T, W, 8, false>(p, stream);
     else
@@ -413,7 +422,7 @@ template <class T, class W>
 hipError_t backward(const NormParams& p, hipStream_t stream)
 {
     const bool sums = p.dweight || p.dbias;
-    const bool wide = p.N > MOST_HELD || p.x_cs != 1 || p.dy_cs != 1;
+    const bool wide = p.N > MOST_HELD || (p.N > 1 && (p.x_cs != 1 || p.dy_cs != 1));
     const int parts = norm_parts(p.M, p.N, sizeof(T) == 4 ? MAG_F32 : MAG_BF16);
     if (wide && sums)
         hipLaunchKernelGGL(k_norm_back_wide_columns<T>, dim3((unsigned)((p.N + 255) / 256), parts),
@@ -434,7 +443,7 @@ hipError_t backward(const NormParams& p, hipStream_t stream)
         if (e != hipSuccess) return e;
     }
     if (wide && p.y && p.M > 0)
-        hipLaunchKernelGGL((k_norm_back_wide<T, W>), dim3((unsigned)p.M), dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_norm_back_wide<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
     return hipGetLastError();
 }
 

@@ -43,3 +43,31 @@ def test_many_rows_stored_by_columns():
     assert torch.equal(db, dy.sum(0, dtype=torch.float64).bfloat16())
     del x, dy
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("ty,wt", [("bf16", "f32"), ("f32", "f32")])
+def test_norms_of_many_rows_stored_by_columns(ty, wt):
+    """4.3M rows: a workgroup of 1,024 threads for each would pass 2^32 threads"""
+    torch = _torch()
+    from test_gpu_block import check_norm, check_norm_backward
+    check_norm(4_300_000, 8, ty, wt, lx="columns")
+    torch.cuda.empty_cache()
+    check_norm_backward(4_300_000, 8, ty, wt, lx="columns", ld="columns")
+    torch.cuda.empty_cache()
+
+
+def test_norms_of_one_column_with_any_stride():
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rows = 4_300_000
+    for n in (3, rows):
+        x, dy = (torch.randn(n, generator=g, device="cuda") for _ in range(2))
+        w, b = torch.tensor([2.0], device="cuda"), torch.tensor([0.75], device="cuda")
+        for stride in (1, 5, 1 << 20):
+            v, d = (t.as_strided((n, 1), (1, stride)) for t in (x, dy))
+            y, mean, rstd = mag.layer_norm(v, w, b, statistics=True)
+            assert bool((y == 0.75).all()) and torch.equal(mean, x)  # (x - mean is zero)
+            dx, dw, db = mag.layer_norm_backward(v, d, mean, rstd, w)
+            assert not bool(dx.any()) and not bool(dw.any())
+            assert abs(float(db) - float(dy.double().sum())) <= (n + 8) * 2.0 ** -24 * float(dy.abs().sum())
