@@ -77,8 +77,9 @@ __device__ __forceinline__ void slopes(float* z, int act)
         });
     case MAG_ACT_GELU_TANH:
         return each<N>(z, [](float v) {
-            const float s = gelu_logistic(v);
-            return s + v * s * (1.0f - s) * GELU_2K * (1.0f + 3.0f * GELU_C * v * v);
+            // (s (1 - s) is zero from 16 on, and v v, which would pass the range, counts no more)
+            const float s = gelu_logistic(v), u = __builtin_amdgcn_fmed3f(v, -16.0f, 16.0f);
+            return s + u * s * (1.0f - s) * GELU_2K * (1.0f + 3.0f * GELU_C * u * u);
         });
     case MAG_ACT_SILU:
         return each<N>(z, [](float v) {

@@ -38,3 +38,34 @@ def test_updates_by_polynomials_that_contract(size, dtype):
         # (two halves under a scale that takes 1 near 2^15: 22 bits, and 2^-39 below them)
         bound = steps * (2.0 ** -21 * want.abs() + 2.0 ** -39 * 0.5 ** steps) + unit * want.abs() + tiny
         assert bool(((out - want).abs() <= bound).all()), steps
+
+
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_and_slopes_of_the_largest_numbers(act, dtype):
+    """where an activation is z or 0 and its slope 1 or 0 in every type (silu of -40 is
+    -1.7e-16 yet, and its slope there)"""
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    from test_gpu_block import act64
+    dt = getattr(torch, dtype)
+    z = torch.tensor([v for v in (40.0, 1e3, 6e4, 1e10, 1.9e19, 1e30, 3.3e38) if v < torch.finfo(dt).max],
+                     dtype=dt, device="cuda")
+    z = torch.cat([z, -z])
+    for rows in (1, 40):   # few rows, and a tile
+        x, w = torch.zeros(rows, 1, dtype=dt, device="cuda"), torch.ones(len(z), 1, dtype=dt, device="cuda")
+        on = (z > 0) | torch.tensor(act == "none", device="cuda")
+        y = mag.linear(x, w, z, activation=act)
+        far = z.abs() >= 1e3
+        assert torch.equal(y[:, far], torch.where(on, z, torch.zeros_like(z))[far].expand(rows, -1)), act
+        for got, want in zip(y[:, ~far].double().unbind(1), act64(z[~far].double(), act)[0]):
+            assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -25).all())
+        dy = torch.ones(rows, len(z), dtype=dt, device="cuda")
+        dx, _, db = mag.linear_backward(x, w, dy, z.expand(rows, -1), activation=act)
+        assert torch.equal(db[far], (rows * on).to(dt)[far]), act
+        for got, want in zip(db[~far].double(), rows * act64(z[~far].double(), act)[1]):
+            assert float((got - want).abs()) <= 2.0 ** -8 * float(want.abs()) + 2.0 ** -25
+        assert bool((dx == on.sum()).all()), act
