@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeParams p, int64_t chunk)
                 if (acts) get8(static_cast<const T*>(p.pre) + r * p.pre_rs, p.pre_cs, j, p.N, z[u]);
             }
             if (acts) {
-                slopes<8 * SLOPE_ROWS>(z[0], p.act);
+                slopes<T, 8 * SLOPE_ROWS>(z[0], p.act);
 #pragma unroll
                 for (int e = 0; e < 8 * SLOPE_ROWS; ++e) d[0][e] *= z[0][e];
             }

@@ -339,7 +339,7 @@ __device__ __forceinline__ void store_linear(const Epilogue& e, int64_t r, int64
             for (int i = 0; i < 8; ++i) z[i] += b[i];
         }
         if (e.pre) store8(static_cast<T*>(e.pre) + r * e.pre_ld + s, z);
-        activate<8>(z, e.act);
+        activate<T, 8>(z, e.act);
         if (e.res) {
             load8(static_cast<const T*>(e.res) + r * e.res_rs + s, b);
 #pragma unroll
@@ -353,7 +353,7 @@ __device__ __forceinline__ void store_linear(const Epilogue& e, int64_t r, int64
             float v = z[i];
             if (e.bias) v += (float)static_cast<const T*>(e.bias)[s + i];
             if (e.pre) static_cast<T*>(e.pre)[r * e.pre_ld + s + i] = (T)v;
-            activate<1>(&v, e.act);
+            activate<T, 1>(&v, e.act);
             if (e.res) v += (float)static_cast<const T*>(e.res)[r * e.res_rs + (s + i) * e.res_cs];
             static_cast<T*>(e.y)[r * e.y_ld + s + i] = (T)v;
         }
@@ -780,7 +780,7 @@ __device__ __forceinline__ void walk(Mm p, First first, Stride stride, const Arr
                         for (int e = 0; e < 8; ++e) v[q][e] += bias[e];
                         if (p.e.pre) store8(static_cast<TO*>(p.e.pre) + r * p.e.pre_ld + s8, v[q]);
                     }
-                    activate<8 * PASSES>(v[0], p.e.act);
+                    activate<TO, 8 * PASSES>(v[0], p.e.act);
 #pragma unroll
                     for (int q = 0; q < PASSES; ++q) {
                         if (p.e.res)

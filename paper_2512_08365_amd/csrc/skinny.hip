@@ -105,7 +105,7 @@ __device__ __forceinline__ void finish(const SkinnyParams& p, f32x4 (&acc)[G][MF
             float z = s[j];
             if (e.bias) z += (float)static_cast<const T*>(e.bias)[n + j];
             if (e.pre) static_cast<T*>(e.pre)[m * e.pre_ld + n + j] = (T)z;
-            activate<1>(&z, e.act);
+            activate<T, 1>(&z, e.act);
             if (e.res) z += (float)static_cast<const T*>(e.res)[m * e.res_rs + (n + j) * e.res_cs];
             static_cast<T*>(e.y)[m * e.y_ld + n + j] = (T)z;
         }

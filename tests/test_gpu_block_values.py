@@ -69,3 +69,39 @@ def test_activations_and_slopes_of_the_largest_numbers(act, dtype):
         for got, want in zip(db[~far].double(), rows * act64(z[~far].double(), act)[1]):
             assert float((got - want).abs()) <= 2.0 ** -8 * float(want.abs()) + 2.0 ** -25
         assert bool((dx == on.sum()).all()), act
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+def test_activations_keep_their_digits_in_the_tails(act, dtype):
+    """Relative errors, down to where fp32 has its full digits.  fp32: an activation
+    is some twelve operations that are off by a last place (2^-23) at most; a slope
+    as many of each of its two terms.  Two bytes: 2^-15 for the six-term polynomial
+    and the arguments' rounding, and the result's own rounding."""
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    from test_gpu_block import act64
+    dt = getattr(torch, dtype)
+    z = torch.cat([torch.linspace(-20, 20, 160_001, device="cuda"), _normal(3, 40_000) * 4]).to(dt)
+    z64 = z.double()
+    off, tiny = {"float32": (12 * 2.0 ** -23, 2.0 ** -118), "float16": (2.0 ** -11 + 2.0 ** -15, 2.0 ** -25),
+                 "bfloat16": (2.0 ** -8 + 2.0 ** -15, 2.0 ** -118)}[dtype]
+    want, slope = act64(z64, act)
+    if act != "gelu":
+        # (the formulas' tails, which 1 + tanh and a sigmoid of z < -36 would cut off)
+        e = torch.exp(-(z64 if act == "silu" else 2 * (2 / torch.pi) ** 0.5 * (z64 + 0.044715 * z64 ** 3)))
+        s, c = 1 / (1 + e), e / (1 + e)
+        k = 1 if act == "silu" else 2 * (2 / torch.pi) ** 0.5 * (1 + 3 * 0.044715 * z64 * z64)
+        want, slope, terms = z64 * s, s + z64 * s * c * k, s + (z64 * s * c * k).abs()
+    else:
+        terms = 0.5 * torch.erfc(-z64 / 2 ** 0.5) + (z64 * torch.exp(-z64 * z64 / 2)).abs() / (2 * torch.pi) ** 0.5
+    for rows in (1, 40):
+        x, w = torch.zeros(rows, 1, dtype=dt, device="cuda"), torch.ones(len(z), 1, dtype=dt, device="cuda")
+        y = mag.linear(x, w, z, activation=act).double()
+        assert bool(((y - want).abs() <= off * want.abs() + tiny).all()), float(
+            ((y - want).abs() / (off * want.abs() + tiny)).max())
+    one = torch.ones(1, len(z), dtype=dt, device="cuda")
+    _, _, db = mag.linear_backward(x[:1], w, one, z[None], activation=act, need=(False, False))
+    rel = 12 * 2.0 ** -23 if dtype == "float32" else 2.0 ** -15
+    bound = rel * terms + (0 if dtype == "float32" else off) * slope.abs() + tiny
+    assert bool(((db.double() - slope).abs() <= bound).all()), float(((db.double() - slope).abs() / bound).max())
