@@ -165,6 +165,35 @@ __global__ __launch_bounds__(256) void k_prepare(PackParams a, PackParams b, Col
         column_sums<T>(c, blockIdx.x - blocks_a - blocks_b);
 }
 
+// Those of the m columns from s on of row r, a bit each, that have a NaN operand
+// there; every lane of a wave asks for its own, of which only the ones that are
+// wanted are looked at: each row and column once, by the whole wave.
+__device__ __forceinline__ uint32_t nan_operands(const Mm& p, int64_t r, int64_t s, int m, bool wanted)
+{
+    uint32_t nan = 0;
+    uint64_t left = __ballot(wanted);
+    while (left) {   // by rows
+        const int64_t row = __shfl(r, __ffsll((unsigned long long)left) - 1, 64);
+        const uint64_t same = __ballot(r == row);
+        if (row_has_nan(p.a, 0, row, p.K) && r == row) nan = 255u;
+        left &= ~same;
+    }
+    left = __ballot(wanted && nan == 0);
+    while (left) {   // ... and the others by columns
+        const int lane = __ffsll((unsigned long long)left) - 1;
+        const int64_t first = __shfl(s, lane, 64);
+        const int count = __shfl(m, lane, 64);
+        const uint64_t same = __ballot(s == first);
+        uint32_t found = 0;
+#pragma unroll 1
+        for (int e = 0; e < count; ++e)
+            if (row_has_nan(p.b, 0, first + e, p.K)) found |= 1u << e;
+        if (s == first && nan == 0) nan = found;
+        left &= ~same;
+    }
+    return nan;
+}
+
 // A split product's parts added up and stored, 8 neighbours of a row a thread.
 // Bound by latency where there are few (1,920 x 384 of 3 parts: 5 us), else by
 // memory.
@@ -173,14 +202,20 @@ __global__ __launch_bounds__(256) void k_mm_join(Mm p)
 {
     const int64_t per_row = p.partial_ld / 8, n = p.R * per_row;
     const int64_t plane = p.R * p.partial_ld;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = quotient(i, per_row), s = (i - r * per_row) * 8;
+    // (a wave's threads go together: they look for NaN operands side by side)
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x / 64 * 64; at < n; at += (int64_t)gridDim.x * 256) {
+        const int64_t i = at + threadIdx.x % 64;
+        const bool on = i < n;
+        const int64_t r = quotient(on ? i : n - 1, per_row), s = ((on ? i : n - 1) - r * per_row) * 8;
         float v[8] = {};
         add_parts(p.partial + r * p.partial_ld + s, plane, p.splits, v);
         const int m = (int)min((int64_t)8, p.S - s);
         if constexpr (sizeof(TO) == 4)
-            if (p.in_parts) make_whole(p, 0, r, s, m, v);
-        store_linear<TO>(p.e, r, s, m, v);
+            if (p.in_parts) {
+                const uint32_t nan = nan_operands(p, r, s, m, !all_finite(v));
+                make_whole(p, 0, r, s, m, nan, v);
+            }
+        if (on) store_linear<TO>(p.e, r, s, m, v);
     }
 }
 

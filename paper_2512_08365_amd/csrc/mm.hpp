@@ -225,7 +225,9 @@ __device__ __forceinline__ int64_t place(int64_t j)
 // from the operands in fp32 (a part of an infinite operand times a part that is
 // zero is NaN where the product may be infinite, and parts of huge operands may
 // overflow where the sum does not).  The parts of a finite number add up to it
-// exactly; an infinite or NaN one is its first part.
+// exactly; an infinite or NaN one is its first part.  A NaN operand needs none of
+// this, and is common where a step has diverged: one lane after the whole reduction
+// of every sum would take a thousand times the product's own time.
 __device__ __forceinline__ float whole_sum(const Mm& p, int64_t bt, int64_t r, int64_t s)
 {
     auto value = [](const MmOperand& o, int64_t bt, int64_t row, int64_t k) {
@@ -235,23 +237,57 @@ __device__ __forceinline__ float whole_sum(const Mm& p, int64_t bt, int64_t r, i
     };
     float sum = 0.0f;
 #pragma unroll 1
-    for (int64_t k = 0; k < p.K; ++k) sum = fmaf(value(p.a, bt, r, k), value(p.b, bt, s, k), sum);
+    for (int64_t k = 0; k < p.K && sum == sum; ++k) sum = fmaf(value(p.a, bt, r, k), value(p.b, bt, s, k), sum);
     return sum;
 }
 
-// ... of 8 neighbours of a row, from column s on (n of them)
-__device__ __forceinline__ void make_whole(const Mm& p, int64_t bt, int64_t r, int64_t s, int n, float* v)
+// whether a row of an operand in three parts holds a NaN, by the 64 lanes of a wave
+static __device__ __forceinline__ bool row_has_nan(const MmOperand& o, int64_t bt, int64_t row, int64_t K)
+{
+    const bf16* h = static_cast<const bf16*>(o.p) + bt * o.batch + (o.mc ? place<3>(row) : row * o.ld);
+    bool nan = false;
+#pragma unroll 4
+    for (int64_t k = threadIdx.x % 64; k < K; k += 64) {
+        const float v = (float)h[o.mc ? k * o.ld : place<3>(k)];
+        nan = nan || v != v;
+    }
+    return __any(nan);
+}
+
+// Those of up to 64 rows of an operand in three parts that hold a NaN, a bit each (a
+// call: within the tile product its code would cost the loop registers, and the
+// whole product a tenth of its time).
+__device__ __attribute__((noinline)) inline uint64_t rows_with_nan(const bf16* h, int64_t ld, bool across, int64_t row,
+                                                                  int rows, int64_t K)
+{
+    const MmOperand o{h, ld, 0, across};
+    uint64_t found = 0;
+#pragma unroll 1
+    for (int i = 0; i < rows; ++i)
+        if (row_has_nan(o, 0, row + i, K)) found |= 1ull << i;
+    return found;
+}
+
+__device__ __forceinline__ bool all_finite(const float* v)
 {
     bool all = true;
 #pragma unroll
     for (int i = 0; i < 8; ++i) all = all && fabsf(v[i]) < __builtin_inff();
-    if (__builtin_expect(all, 1)) return;
+    return all;
+}
+
+// ... of 8 neighbours of a row, from column s on (n of them); nan: those, a bit each,
+// that have a NaN operand
+__device__ __forceinline__ void make_whole(const Mm& p, int64_t bt, int64_t r, int64_t s, int n, uint32_t nan,
+                                           float* v)
+{
+    if (__builtin_expect(all_finite(v), 1)) return;
 #pragma unroll 1
     for (int e = 0; e < n; ++e) {
         float x = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x = i == e ? v[i] : x;
-        if (fabsf(x) < __builtin_inff()) continue;
+        if (nan >> e & 1 || fabsf(x) < __builtin_inff()) continue;
         x = whole_sum(p, bt, r, s + e);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i == e ? x : v[i];
@@ -704,6 +740,9 @@ __device__ __forceinline__ void walk(Mm p, First first, Stride stride, const Arr
     uint32_t g = first();
     begin_tile(g);
     while (true) {
+        // (said to the compiler too, which would otherwise wait in the loop for what it
+        // takes to be on its way to the fragments' registers: with it for the steps' loads)
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
         meet(None{});
 #pragma unroll
         for (int i = 0; i < F; ++i) {
@@ -726,6 +765,13 @@ __device__ __forceinline__ void walk(Mm p, First first, Stride stride, const Arr
         settle();
         const int64_t rt = r0 + wr, st = s0 + ws;
         const int64_t bt = plane;
+        // the wave's rows and columns that hold a NaN, looked for once a sum is not finite
+        uint64_t nan_rows = 0, nan_cols = 0;
+        bool looked = !(P == 3 && EPI == MM_LINEAR);
+        // of the 8 neighbours from column s on of row r
+        auto nans = [&](int64_t r, int64_t s) -> uint32_t {
+            return nan_rows >> (r - rt) & 1 ? 255u : (uint32_t)(nan_cols >> (s - st)) & 255u;
+        };
         const bool mirrored = mirror;
         g += stride();
         if (g < units) begin_tile(g);
@@ -757,12 +803,24 @@ __device__ __forceinline__ void walk(Mm p, First first, Stride stride, const Arr
 #pragma unroll
                     for (int q = 0; q < PASSES; ++q)
                         load8(static_cast<const TO*>(p.e.res) + (r8 + q * (64 / LANES)) * p.e.res_rs + s8, res[q]);
+            float zero = 0.0f;
 #pragma unroll
             for (int i = 0; i < F; ++i)
                 if (i == ph)
 #pragma unroll
-                    for (int j = 0; j < F; ++j)
+                    for (int j = 0; j < F; ++j) {
                         *(f32x4*)at(lane & 15, j * 4 + (lane >> 4)) = acc[i][j];
+                        if constexpr (P == 3 && EPI == MM_LINEAR)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) zero = fmaf(acc[i][j][e], 0.0f, zero);
+                    }
+            if (!looked && __builtin_expect(__any(zero != 0.0f), 0)) {
+                looked = true;
+                nan_rows = rows_with_nan(static_cast<const bf16*>(p.a.p) + bt * p.a.batch, p.a.ld, p.a.mc, rt,
+                                         (int)min((int64_t)COLS, p.R - rt), p.K);
+                nan_cols = rows_with_nan(static_cast<const bf16*>(p.b.p) + bt * p.b.batch, p.b.ld, p.b.mc, st,
+                                         (int)min((int64_t)COLS, p.S - st), p.K);
+            }
             if constexpr (EPI == MM_LINEAR)
                 if (inside) {
                     float v[PASSES][8];
@@ -775,7 +833,7 @@ __device__ __forceinline__ void walk(Mm p, First first, Stride stride, const Arr
 #pragma unroll
                     for (int q = 0; q < PASSES; ++q) {
                         const int64_t r = r8 + q * (64 / LANES);
-                        if constexpr (P == 3) make_whole(p, bt, r, s8, 8, v[q]);
+                        if constexpr (P == 3) make_whole(p, bt, r, s8, 8, nans(r, s8), v[q]);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[q][e] += bias[e];
                         if (p.e.pre) store8(static_cast<TO*>(p.e.pre) + r * p.e.pre_ld + s8, v[q]);
@@ -805,7 +863,7 @@ __device__ __forceinline__ void walk(Mm p, First first, Stride stride, const Arr
                     *(f32x4*)q = *(f32x4*)v;
                     *(f32x4*)(q + 4) = *(f32x4*)(v + 4);
                 } else if constexpr (EPI == MM_LINEAR) {
-                    if constexpr (P == 3) make_whole(p, bt, r, s, n, v);
+                    if constexpr (P == 3) make_whole(p, bt, r, s, n, nans(r, s), v);
                     store_linear<TO>(p.e, r, s, n, v);
                 } else {
                     store_orth(p, bt, r, s, n, v);

@@ -105,3 +105,63 @@ def test_activations_keep_their_digits_in_the_tails(act, dtype):
     rel = 12 * 2.0 ** -23 if dtype == "float32" else 2.0 ** -15
     bound = rel * terms + (0 if dtype == "float32" else off) * slope.abs() + tiny
     assert bool(((db.double() - slope).abs() <= bound).all()), float(((db.double() - slope).abs() / bound).max())
+
+
+def _ms(call):
+    torch = _torch()
+    best = 1e9
+    for _ in range(3):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        call()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+# fp32 products that are taken in parts: one tile of each size, a reduction that is
+# split, and two gradients at once
+@pytest.mark.parametrize("size", [(1000, 2050, 777), (2048, 1024, 4096), (512, 8192, 1024), (8192, 512, 2048),
+                                  (2048, 1024, 1536)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("where", ["all", "last of each row", "one row of the weight", "half the rows"])
+def test_nan_in_large_float_products(size, where):
+    """NaN where an operand has one and nowhere else, and no call much longer for it:
+    taking every such sum again is 200 to 500 times the time without"""
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    rows, inner, outer = size
+    x, w, dy = _normal(1, rows, inner), _normal(2, outer, inner) * 0.1, _normal(3, rows, outer)
+    mag.linear(x, w)
+    y0, grads0 = mag.linear(x, w), mag.linear_backward(x, w, dy)
+    t0, b0 = _ms(lambda: mag.linear(x, w)), _ms(lambda: mag.linear_backward(x, w, dy))
+    nan = float("nan")
+    bad_rows, bad_cols = torch.zeros(rows, dtype=torch.bool), torch.zeros(outer, dtype=torch.bool)
+    if where == "all":
+        x[:] = nan
+        dy[:] = nan
+        bad_rows[:] = True
+    elif where == "last of each row":
+        x[:, -1] = nan
+        dy[:, -1] = nan
+        bad_rows[:] = True
+    elif where == "half the rows":
+        x[::2, 3] = nan
+        dy[::2, 3] = nan
+        bad_rows[::2] = True
+    else:
+        w[outer // 2, inner // 3] = nan
+        bad_cols[outer // 2] = True
+    y = mag.linear(x, w)
+    bad = bad_rows[:, None].cuda() | bad_cols[None].cuda()
+    assert torch.equal(torch.isnan(y), bad) and torch.equal(y[~bad], y0[~bad])
+    dx, dw, db = mag.linear_backward(x, w, dy)
+    # what has a NaN where: dx = dy w, dw = dy^T x, db = the sum of dy
+    nx, nw, nd = (torch.isnan(v) for v in (x, w, dy))
+    bad_dx = nd.any(1)[:, None] | nw.any(0)[None]
+    bad_dw = nd.any(0)[:, None] | nx.any(0)[None]
+    for got, want, bad in ((dx, grads0[0], bad_dx), (dw, grads0[1], bad_dw), (db, grads0[2], nd.any(0))):
+        assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], want[~bad])
+    t1, b1 = _ms(lambda: mag.linear(x, w)), _ms(lambda: mag.linear_backward(x, w, dy))
+    print(f"[time] {size} {where}: {t0:.3f} -> {t1:.3f}, gradients {b0:.3f} -> {b1:.3f} ms", flush=True)
+    assert t1 <= 40 * t0 and b1 <= 40 * b0
