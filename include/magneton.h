@@ -751,8 +751,10 @@ int mag_stream_push_host(mag_stream* handle, const double* t_host, const float* 
 #define MAG_MAX_FEATURES (1LL << 21)
 
 /* A matrix on the device.  Element (i, j) is data[i * row_stride + j *
-   col_stride].  Inputs may have any strides >= 0 (0: one row or column read
-   again and again); outputs need col_stride 1 and rows that do not overlap.
+   col_stride].  Inputs may have any strides from 0 (one row or column read
+   again and again) to 2^32 elements; outputs need col_stride 1 and rows that do
+   not overlap.  From its first to its last element a matrix, or a batch of them,
+   spans less than 2^60 elements.
    data must be aligned to the element; rows that start at multiples of 16
    bytes are read fastest.  Two of its fields may be anything where the matrix
    has one row or one column: that one's stride. */

@@ -15,6 +15,7 @@ using mag::set_hip_error;
 namespace {
 
 constexpr int64_t MAX_DIM = MAG_MAX_EXTENT;
+constexpr int64_t MOST_SPAN = 1LL << 60;   // elements from an array's first to its last: bytes fit 63 bits
 
 size_t element(int dtype) { return dtype == MAG_F32 ? 4 : 2; }
 bool known_dtype(int d) { return d == MAG_F32 || d == MAG_F16 || d == MAG_BF16; }
@@ -41,10 +42,12 @@ int check_shape(const mag_matrix& m, bool out)
     if (m.rows < 0 || m.cols < 0 || m.rows > MAX_DIM || m.cols > MAX_DIM)
         return set_error(MAG_E_SIZE, "a matrix extent is negative or exceeds MAG_MAX_EXTENT");
     if (m.rows == 0 || m.cols == 0) return MAG_OK;
-    // (the last element's offset stays far inside 63 bits)
     if ((m.rows > 1 && (m.row_stride < 0 || m.row_stride > (1LL << 32))) ||
         (m.cols > 1 && (m.col_stride < 0 || m.col_stride > (1LL << 32))))
         return set_error(MAG_E_SIZE, "a matrix stride is negative or exceeds 2^32 elements");
+    const uint64_t last = (m.rows > 1 ? (uint64_t)((m.rows - 1) * m.row_stride) : 0) +
+                          (m.cols > 1 ? (uint64_t)((m.cols - 1) * m.col_stride) : 0);
+    if (last >= (uint64_t)MOST_SPAN) return set_error(MAG_E_SIZE, "a matrix spans 2^60 elements or more");
     if (out && ((m.cols > 1 && m.col_stride != 1) || (m.rows > 1 && m.row_stride < m.cols)))
         return set_error(MAG_E_SIZE, "an output matrix needs col_stride 1 and rows that do not overlap");
     return MAG_OK;
@@ -504,7 +507,7 @@ int check_orth(const mag_orthogonalize_args* a)
     TRY(check_shape(a->g, false));
     if (a->g.rows > MAG_MAX_FEATURES || a->g.cols > MAG_MAX_FEATURES)
         return set_error(MAG_E_SIZE, "a side exceeds MAG_MAX_FEATURES");
-    if (a->g_batch_stride < 0 || a->g_batch_stride > (1LL << 62) / std::max<int64_t>(a->batch, 1))
+    if (a->g_batch_stride < 0 || a->g_batch_stride > MOST_SPAN / std::max<int64_t>(a->batch, 1))
         return set_error(MAG_E_SIZE, "g_batch_stride out of range");
     return MAG_OK;
 }
@@ -858,6 +861,8 @@ int mag_orthogonalize(const mag_orthogonalize_args* a, void* workspace, size_t w
     if (a->batch > 1 && a->out_batch_stride <
                             (a->out.rows - 1) * (a->out.rows > 1 ? a->out.row_stride : 0) + a->out.cols)
         return set_error(MAG_E_SIZE, "the matrices of out overlap");
+    if (a->batch > 1 && a->out_batch_stride > MOST_SPAN / a->batch)
+        return set_error(MAG_E_SIZE, "out_batch_stride out of range");
     if (!isfinite(a->a) || !isfinite(a->b) || !isfinite(a->c) || !(a->eps >= 0.0) || isinf(a->eps))
         return set_error(MAG_E_SIZE, "coefficients must be finite and eps finite and >= 0");
     // bounds of X's singular values step by step, and with them of its elements

@@ -130,3 +130,28 @@ def test_scales_of_polynomials_that_contract_are_finite(calls, size, dtype):
                     assert 0 < p["scale"] < math.inf
                 elif p["what"] in ("update", "partial"):
                     assert all(math.isfinite(p[k]) for k in ("scale", "mix", "diagonal")), (coefficients, p)
+
+
+def test_spans_beyond_63_bits_of_bytes_are_refused(calls):
+    """2^30 rows 2^32 elements apart are 2^64 bytes of fp32"""
+    N, lib = calls.N, calls.lib
+    size = ctypes.c_size_t(0)
+
+    def linear(x):
+        return lib.mag_linear_workspace_size(
+            N.LINEAR_ARGS.pack(F32, 0, *x, *_rows(8, x[2]), *NONE, *NONE, *NONE, 0), ctypes.byref(size))
+
+    assert linear((FAKE, 1 << 30, 16, 1 << 32, 1)) == N.MAG_E_SIZE and b"2^60" in lib.last_error()
+    assert linear((FAKE, 1 << 28, 1 << 21, 1 << 32, 1 << 32)) == N.MAG_E_SIZE
+    assert linear((FAKE, 1 << 28, 16, 1 << 31, 1)) == 0
+    assert linear((FAKE, 1, 16, 1 << 62, 1)) == 0   # (one row: its stride may be anything)
+
+    def update(batch, g_stride, out_stride):
+        m = _rows(8, 16)
+        return lib.mag_orthogonalize(N.ORTHOGONALIZE_ARGS.pack(
+            F32, 5, batch, *m, *m, g_stride, out_stride, 2.0, -1.5, 0.5, 1e-7), ctypes.c_void_p(FAKE),
+            ctypes.c_size_t(1 << 40), None)
+
+    assert update(2, 128, 128) == 0 and update(2, 0, 1 << 40) == 0
+    for g_stride, out_stride in (((1 << 60) // 2 + 1, 128), (128, (1 << 60) // 2 + 1), (128, 1 << 62)):
+        assert update(2, g_stride, out_stride) == N.MAG_E_SIZE, (g_stride, out_stride)
