@@ -7,6 +7,7 @@ import os
 import random
 import subprocess
 
+import block_sizes
 import pytest
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -155,3 +156,46 @@ def test_spans_beyond_63_bits_of_bytes_are_refused(calls):
     assert update(2, 128, 128) == 0 and update(2, 0, 1 << 40) == 0
     for g_stride, out_stride in (((1 << 60) // 2 + 1, 128), (128, (1 << 60) // 2 + 1), (128, 1 << 62)):
         assert update(2, g_stride, out_stride) == N.MAG_E_SIZE, (g_stride, out_stride)
+
+
+def _variant(p):
+    """what a product is compiled for: its result, kind, tile, steps in LDS, operands across"""
+    side, steps = SIDE[p["tile"]], 2 if p["tile"] else 4
+    if side == 128 and p["what"] in ("linear", "update") and p["kind"] != K_PARTS:
+        tr, ts = -(-p["R"] // 128), -(-p["S"] // 128)
+        units = (tr * (tr + 1) // 2 if p["symmetric"] else tr * ts) * p["batch"]
+        steps = 4 if units <= 256 and p["K"] >= 32 * (64 if p["kind"] in (K_BF16, K_F16) else 32) else 2
+    return p["what"], p["kind"], side, steps, p["a_mc"], p["b_mc"]
+
+
+def test_the_sizes_of_the_gpu_tests_reach_every_variant(calls):
+    """a change of the costs that a tile is chosen by must not leave one untested"""
+    types = {"f32": F32, "f16": F16, "bf16": BF16}
+    reached = set()
+    for ty, dtype in types.items():
+        for rows, inner, outer in block_sizes.LINEAR[ty]:
+            for lx in (_rows, _columns):
+                for lw in (_rows, _columns):
+                    reached |= {_variant(p) for p in _products(calls.linear(
+                        dtype, lx(rows, inner), lw(outer, inner)))}
+        for rows, inner, outer in block_sizes.LINEAR_BACKWARD[ty]:
+            reached |= {_variant(p) for p in _products(calls.linear_backward(
+                dtype, _rows(rows, inner), _rows(outer, inner), _rows(rows, outer)))}
+    for batch, rows, cols in block_sizes.UPDATES:
+        for dtype in types.values():
+            reached |= {_variant(p) for p in _products(calls.orthogonalize(dtype, rows, cols, batch=batch))}
+    every = [(a, b) for a in (0, 1) for b in (0, 1)]
+    want = set()
+    for kind in (K_BF16, K_F16):
+        want |= {("linear", kind, *tile, *ab) for tile in ((64, 4), (128, 2), (128, 4), (256, 2)) for ab in every}
+        want |= {("partial", kind, *tile, *ab) for tile in ((64, 4), (128, 2)) for ab in every}
+    want |= {(what, K_F32, 64, 4, *ab) for what in ("linear", "partial") for ab in every}
+    want |= {(what, K_PARTS, *tile, *ab) for what in ("linear", "partial") for tile in ((64, 4), (128, 2))
+             for ab in every}
+    want |= {("two", kind, 64, 4, a, 1) for kind in (K_BF16, K_F16, K_F32, K_PARTS) for a in (0, 1)}
+    # an update's X X^T takes both operands alike, its long product X across or neither
+    want |= {("partial", K_HALVES, *tile, a, a) for tile in ((64, 4), (128, 2)) for a in (0, 1)}
+    want |= {("update", K_HALVES, *tile, *ab) for tile in ((64, 4), (128, 2), (128, 4), (256, 2))
+             for ab in ((0, 0), (0, 1), (1, 1))}
+    assert want - reached == set()
+    assert reached - want == set()
