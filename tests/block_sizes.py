@@ -24,3 +24,7 @@ LINEAR_BACKWARD = {
 UPDATES = [(1, 100, 100), (1, 257, 100), (1, 100, 777), (1, 777, 100), (12, 100, 4100), (12, 4100, 100),
            (3, 777, 4100), (3, 4100, 777), (1, 1030, 3000), (1, 3000, 1030), (3, 1030, 4100), (3, 4100, 1030),
            (3, 2050, 1536), (3, 3000, 2050), (12, 2050, 1536)]
+# updates of two bytes that take several steps at once: sides, steps, spectrum
+GROUPED = [((520, 4100), 2, "full"), ((520, 4100), 7, "falling"), ((520, 8200), 4, "low"),
+           ((4100, 520), 5, "falling"), ((1030, 4104), 3, "low"), ((1030, 4104), 6, "full"),
+           ((2048, 8192), 5, "full"), ((8192, 2048), 5, "falling")]

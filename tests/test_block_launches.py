@@ -199,3 +199,11 @@ def test_the_sizes_of_the_gpu_tests_reach_every_variant(calls):
              for ab in ((0, 0), (0, 1), (1, 1))}
     assert want - reached == set()
     assert reached - want == set()
+
+
+@pytest.mark.parametrize("size,steps,_", block_sizes.GROUPED)
+def test_sizes_that_take_several_steps_at_once(calls, size, steps, _):
+    """fewer long products than steps, for two-byte results alone"""
+    for dtype in (F32, F16, BF16):
+        long = [p for p in _products(calls.orthogonalize(dtype, *size, steps)) if not p["symmetric"]]
+        assert len(long) == steps if dtype == F32 else len(long) < steps, (dtype, len(long))
