@@ -6,6 +6,10 @@ include/magneton.h).
 Every call is asynchronous on the current stream of its tensors' device.
 Outputs and workspaces may be given (`out`, `workspace`: a program that calls
 in a loop keeps them) and are allocated otherwise.
+
+These are operators on values, as the rest of this package: autograd does not see
+them.  Results of tensors that require a gradient carry none; linear_backward and
+layer_norm_backward compute it.
 """
 from __future__ import annotations
 
@@ -142,7 +146,8 @@ def linear(x, weight, bias=None, residual=None, *, activation=None, pre=None, ou
     stored input by output), bias: [out], residual: [..., out]; one type, float32,
     float16 or bfloat16.  activation: None, "relu", "gelu", "gelu_tanh", "silu".
     pre: True, or a tensor, for x weight^T + bias as well (what linear_backward
-    reads).  residual may be `out` itself.  Returns out, or (out, pre).
+    reads).  residual may be `out` itself.  Returns out, or (out, pre), which carry
+    no gradient: call linear_backward for it.
     """
     lib = _lib()
     act = _activation(activation)
@@ -229,7 +234,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, *, statistics=None, out=None
     sqrt(variance + eps).  weight and bias: [width], of x's type or float32, or
     None.  statistics: True, or two float32 tensors of one value per row, for
     the mean and rstd too (what layer_norm_backward reads).  out may be x itself.
-    Returns out, or (out, mean, rstd)."""
+    Returns out, or (out, mean, rstd), which carry no gradient: call
+    layer_norm_backward for it."""
     lib = _lib()
     if out is None:
         _dtype(x, "x")
@@ -299,7 +305,8 @@ def orthogonalize(g, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, 
     """An update with its singular values driven towards one (Newton-Schulz):
     X = g / (|g| + eps), then `steps` times X <- a X + (b A + c A A) X with A = X
     X^T (on the transpose where g is taller than wide).  g: [rows, cols], or
-    [batch, rows, cols] for several on their own.  out may be g itself."""
+    [batch, rows, cols] for several on their own.  out may be g itself.  The result
+    carries no gradient."""
     lib = _lib()
     _dtype(g, "g")
     if out is None:

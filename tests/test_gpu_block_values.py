@@ -165,3 +165,17 @@ def test_nan_in_large_float_products(size, where):
     t1, b1 = _ms(lambda: mag.linear(x, w)), _ms(lambda: mag.linear_backward(x, w, dy))
     print(f"[time] {size} {where}: {t0:.3f} -> {t1:.3f}, gradients {b0:.3f} -> {b1:.3f} ms", flush=True)
     assert t1 <= 40 * t0 and b1 <= 40 * b0
+
+
+def test_results_carry_no_gradient():
+    """as the docstrings say: the backward calls compute it"""
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    x, w = _normal(1, 40, 64).requires_grad_(), _normal(2, 24, 64).requires_grad_()
+    y, pre = mag.linear(x, w, pre=True)
+    z, mean, rstd = mag.layer_norm(x, statistics=True)
+    outs = [y, pre, z, mean, rstd, mag.orthogonalize(w), *mag.linear_backward(x, w, y),
+            *mag.layer_norm_backward(x, z, mean, rstd)]
+    assert not any(o.requires_grad for o in outs)
+    for f in (mag.linear, mag.layer_norm, mag.orthogonalize):
+        assert "no gradient" in " ".join(f.__doc__.split())
