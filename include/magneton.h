@@ -784,10 +784,11 @@ typedef struct mag_linear_args {
  *   strides and the 16-byte alignment of data count; the rest of args is not
  *   read).
  * fp32 operands of small products are multiplied as they are.  Those of large
- * ones (from some 10^10 operations on) are cut into three bfloat16
- * parts each, whose sum is the operand exactly, and the six largest of the nine
- * products are summed in fp32 (the rest is below 2^-24 of a product); a sum that
- * is not finite is taken again from the operands themselves.
+ * ones (from some 10^10 operations on; 10^8 where their layout has to be changed
+ * for the product anyway) are cut into three bfloat16 parts each, whose sum is the operand exactly (within 2^-134 for operands below 2^-110),
+ * and the six largest of the nine products are summed in fp32 (the rest is below
+ * 2^-24 of a product); a sum that is not finite is taken again from the operands
+ * themselves, unless one of them is NaN.
  * Errors: MAG_E_NULL, MAG_E_SIZE (types, sizes, strides), MAG_E_ALIGN,
  * MAG_E_WORKSPACE, MAG_E_HIP.
  */

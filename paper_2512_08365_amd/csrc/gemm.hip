@@ -13,7 +13,8 @@ typedef __attribute__((ext_vector_type(8))) short h8;
 __device__ __forceinline__ short bits(bf16 v) { return __builtin_bit_cast(short, v); }
 
 // An fp32 number as three bfloat16 parts that add up to it exactly: 8 bits of
-// it, 8 of the rest, what is left.  Rounding to nearest keeps every part's
+// it, 8 of the rest, what is left (of numbers below 2^-110 the last part ends where
+// bfloat16 does, half of 2^-133 off).  Rounding to nearest keeps every part's
 // remainder small; the largest numbers, which it would take to infinity, are
 // cut instead.  Infinities and NaN have the first part alone.
 __device__ __forceinline__ void three_parts(float v, short& a, short& b, short& c)
