@@ -179,3 +179,19 @@ def test_results_carry_no_gradient():
     assert not any(o.requires_grad for o in outs)
     for f in (mag.linear, mag.layer_norm, mag.orthogonalize):
         assert "no gradient" in " ".join(f.__doc__.split())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+def test_reductions_over_nothing(dtype):
+    """no inputs, more rows than a decode step has: act(bias) + residual; no outputs: dx 0"""
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    new = dict(dtype=getattr(torch, dtype), device="cuda")
+    b, r = torch.arange(-40, 40, **new), torch.ones(100, 80, **new)
+    y, z = mag.linear(torch.empty(100, 0, **new), torch.empty(80, 0, **new), b, r, activation="relu", pre=True)
+    assert torch.equal(z, b.expand(100, 80)) and torch.equal(y, b.clamp(min=0).expand(100, 80) + 1)
+    dx, dw, db = mag.linear_backward(torch.empty(100, 0, **new), torch.empty(80, 0, **new), r)
+    assert dx.shape == (100, 0) and dw.shape == (80, 0) and bool((db == 100).all())
+    dx, dw, db = mag.linear_backward(torch.ones(100, 72, **new), torch.empty(0, 72, **new),
+                                     torch.empty(100, 0, **new))
+    assert dx.shape == (100, 72) and not bool(dx.any()) and dw.shape == (0, 72) and db.shape == (0,)
