@@ -200,7 +200,7 @@ const TileCost TILE_COST[mag::MM_KINDS][mag::TILES] = {
 };
 // (fp32 as it lies is bound by its instruction and gains nothing from a larger
 // tile; three parts cost six products of bfloat16 and a pass to cut them, and win
-// from some 10 GFLOP on: 2,048 x 1,024 by 4,096 102 us, as it lies 136 us; 256 x
+// from some 10 GFLOP on: 2,048 x 1,024 by 4,096 97 to 110 us, as it lies 136 us; 256 x
 // 2,048 by 512 21.6 and 14.5 us.)
 
 // The tile and split of the reduction that these costs make fastest: large tiles

@@ -82,7 +82,10 @@ __device__ __forceinline__ void pack_some(const PackParams& p, int64_t block, in
 constexpr int SLOPE_COLS = 512;  // columns of a workgroup: 64 lanes of 8
 constexpr int SLOPE_ROWS = 2;    // rows a wave has in flight (4: too many registers, 40 % slower)
 
-// dz and the column sums of one chunk of rows: four waves take its rows in
+// dz and the column sums of one chunk of rows.  dz is rounded to the operands' type,
+// as x and weight are held, because the products' matrix instructions take no other:
+// of two bytes the gradients are 1.4 times as far off as their own rounding (0.0023
+// and 0.0017 of bfloat16); the sums take it unrounded.  Four waves take the rows in
 // turn, 8 columns a lane, and add their sums up in LDS at the end.  Bound by
 // memory (a prompt's 805 MB in 170 us).
 template <class T, bool PARTS>

@@ -507,8 +507,8 @@ constexpr int wgs_per_cu(int side, int P, int stages)
 }
 
 // out[r][s] = sum over k of a(r, k) b(s, k).  Bound by the matrix cores in the
-// 256 tile (8,192 x 16,384 x 4,096 bfloat16 with its epilogue 910 us, 1,208
-// TFLOP/s; two such gradients 1,640 us, 1,340), by what the L2s deliver to LDS, 10
+// 256 tile (8,192 x 16,384 x 4,096 bfloat16 with its epilogue 920 us, 1,195
+// TFLOP/s; two such gradients 1,670 us, 1,315), by what the L2s deliver to LDS, 10
 // to 12 TB/s, in the smaller ones: a 64 tile moves four times a 256 one's bytes.
 // Steps of 128 bytes a row: half as long ones double the L2's requests.
 //

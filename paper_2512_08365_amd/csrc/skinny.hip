@@ -3,8 +3,8 @@
 // The weight is read once and bounds the call; everything is one launch, since a
 // second one would cost as much as a small weight.  Each workgroup has 16 or 32
 // outputs of every row and its waves share the reduction, so that a 4096 x 4096
-// weight is read by 2,048 waves with all of their loads in flight; their sums
-// meet in LDS.  The products run on the matrix cores with the weight as the left
+// weight is read by 2,048 waves, each with half of its loads in flight at once (two
+// rounds of four lines); their sums meet in LDS.  The products run on the matrix cores with the weight as the left
 // operand, straight from registers where it lies along the reduction, and
 // through a transposing LDS read where it is stored input by output.  Rows of
 // any alignment: vector loads at any element.  fp32 takes the fp32 matrix
