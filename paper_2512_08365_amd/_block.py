@@ -214,7 +214,7 @@ def _norm_args(x, weight, bias, y, dy, dx, mean, rstd, dweight, dbias, eps):
     wt, wdt = ty, dt
     for some in (weight, bias, dweight, dbias):
         if some is not None:
-            wt, wdt = some.dtype, _dtype(some, "weight")
+            wdt, wt = _dtype(some, "weight"), some.dtype
             break
     f32 = torch.float32
     return N.NORM_ARGS.pack(
@@ -265,6 +265,8 @@ def layer_norm_backward(x, dy, mean, rstd, weight=None, *, need=(True, True, Tru
     a weight)."""
     lib = _lib()
     _dtype(x, "x")
+    if weight is not None:
+        _dtype(weight, "weight")
     if out is None:
         wt = torch.float32 if weight is None else weight.dtype
         out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None,

@@ -195,3 +195,17 @@ def test_reductions_over_nothing(dtype):
     dx, dw, db = mag.linear_backward(torch.ones(100, 72, **new), torch.empty(0, 72, **new),
                                      torch.empty(100, 0, **new))
     assert dx.shape == (100, 72) and not bool(dx.any()) and dw.shape == (0, 72) and db.shape == (0,)
+
+
+def test_norm_weights_that_are_no_tensors_are_refused():
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    from paper_2512_08365_amd import _native as N
+    x, rows = torch.ones(4, 16, device="cuda"), torch.ones(4, device="cuda")
+    for bad, code in ((2.0, N.MAG_E_NULL), ([1.0] * 16, N.MAG_E_NULL), (torch.ones(16), N.MAG_E_NULL),
+                      (torch.ones(16, device="cuda", dtype=torch.float64), N.MAG_E_SIZE)):
+        for call in (lambda: mag.layer_norm(x, bad), lambda: mag.layer_norm(x, None, bad),
+                     lambda: mag.layer_norm_backward(x, x, rows, rows, bad)):
+            with pytest.raises(mag.MagnetonError) as e:
+                call()
+            assert e.value.code == code, e.value
