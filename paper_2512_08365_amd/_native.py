@@ -41,6 +41,8 @@ MAG_STATIC_SCRATCH_BYTES = 64 << 20
 MAG_F32 = 0
 MAG_F16 = 1
 MAG_BF16 = 2
+MAG_E4M3 = 3
+MAG_E5M2 = 4
 MAG_ACT_NONE = 0
 MAG_ACT_RELU = 1
 MAG_ACT_GELU = 2
@@ -67,6 +69,7 @@ EXPORTED = (
     "mag_linear_backward_workspace_size", "mag_linear_backward",
     "mag_layer_norm", "mag_layer_norm_backward_workspace_size", "mag_layer_norm_backward",
     "mag_orthogonalize_workspace_size", "mag_orthogonalize",
+    "mag_quantize_fp8", "mag_linear_fp8_workspace_size", "mag_linear_fp8",
     "mag_strerror", "mag_last_error", "mag_version",
 )
 
@@ -133,6 +136,8 @@ _MAT = "Pqqqq"
 LINEAR_ARGS = struct.Struct("@ii" + 5 * _MAT + "P")
 LINEAR_BACKWARD_ARGS = struct.Struct("@ii" + 6 * _MAT + "P")
 NORM_ARGS = struct.Struct("@ii" + 4 * _MAT + "PPPPPPd")
+QUANTIZE_ARGS = struct.Struct("@iiii" + 5 * _MAT)
+LINEAR_FP8_ARGS = struct.Struct("@iiii" + 7 * _MAT + "P")
 ORTHOGONALIZE_ARGS = struct.Struct("@iiq" + 2 * _MAT + "qqdddd")
 
 _lib = None
@@ -228,7 +233,7 @@ def load(path: str = LIB_PATH):
     lib.mag_stream_push_host.restype = ctypes.c_int
     # (the argument structs come packed, as bytes)
     c_bytes, c_size = ctypes.c_char_p, ctypes.c_size_t
-    for name in ("linear", "linear_backward", "layer_norm_backward", "orthogonalize"):
+    for name in ("linear", "linear_backward", "layer_norm_backward", "orthogonalize", "linear_fp8"):
         size = getattr(lib, f"mag_{name}_workspace_size")
         size.argtypes = [c_bytes, P(c_size)]
         size.restype = ctypes.c_int
@@ -237,6 +242,8 @@ def load(path: str = LIB_PATH):
         call.restype = ctypes.c_int
     lib.mag_layer_norm.argtypes = [c_bytes, c_vp]
     lib.mag_layer_norm.restype = ctypes.c_int
+    lib.mag_quantize_fp8.argtypes = [c_bytes, c_vp]
+    lib.mag_quantize_fp8.restype = ctypes.c_int
     lib.mag_strerror.argtypes = [ctypes.c_int]
     lib.mag_strerror.restype = ctypes.c_char_p
     lib.mag_last_error.argtypes = []

@@ -1,0 +1,11 @@
+// mm_fp8_128.hip -- the 8-bit product's tiles of 128.
+#include "mm_fp8.hpp"
+
+namespace mag {
+
+hipError_t launch_mm8_128(const Mm8& p, int dtype, hipStream_t stream)
+{
+    return launch_mm8<Shape8<128, 2, 2>>(p, dtype, stream);
+}
+
+}  // namespace mag

@@ -1,0 +1,264 @@
+// quantize.hip -- numbers cut to 8 bits with a scale for each block.
+//
+// Bound by memory: x is read once, q and qt are written once.  A block of a row is 16
+// lanes of 8 neighbours, its largest magnitude a reduction within them.  For the
+// transpose (and blocks of 128 x 128) a workgroup holds a tile of 128 x 128 in
+// registers, 8 x 8 a thread, takes the largest of rows and columns from there and
+// turns the transpose's bytes in LDS, 8 neighbours of a column at a time.
+
+#include <algorithm>
+
+#include "fp8.hpp"
+#include "mm.hpp"
+
+namespace mag {
+namespace {
+
+// How a block's numbers x become x / scale, scale = max(most / LARGEST, 2^-126).  The
+// largest numbers of both formats are 0.875 times a power of two, 2^9 and 2^16: x /
+// scale = 0.875 x / (most 2^-9), whose parts are exact for two-byte x, and whose
+// quotient, a reciprocal and one correction, is right to the last place: ties
+// between two numbers of the format are then seen as such (by a product with the
+// reciprocal of a rounded scale, of 8,192 x 4,096 one number in 10,000 went the
+// other way).
+template <int FORMAT>
+struct Cut {
+    static constexpr float LARGEST = FORMAT == MAG_E4M3 ? 448.0f : 57344.0f;
+    static constexpr float DOWN = FORMAT == MAG_E4M3 ? 0x1p-9f : 0x1p-16f;
+    float d, inverse;
+
+    __device__ __forceinline__ explicit Cut(float most)
+    {
+        d = fmaxf(most * DOWN, 0.875f * 0x1p-126f);
+        inverse = 1.0f / d;
+        // (an infinite one: finite numbers become 0, infinite ones NaN)
+        if (most == __builtin_inff()) d = 1.0f, inverse = 0.0f;
+    }
+    static __device__ __forceinline__ float scale(float most)
+    {
+        return fmaxf(most / LARGEST, (float)MAG_FP8_LEAST_SCALE);
+    }
+    __device__ __forceinline__ float operator()(float x) const
+    {
+        const float n = 0.875f * x, q = n * inverse;
+        return fmaf(fmaf(-q, d, n), inverse, q);
+    }
+    // four neighbours
+    __device__ __forceinline__ uint32_t four(float a, float b, float c, float e) const
+    {
+        int v = 0;
+        if constexpr (FORMAT == MAG_E4M3) {
+            v = __builtin_amdgcn_cvt_pk_fp8_f32((*this)(a), (*this)(b), v, false);
+            v = __builtin_amdgcn_cvt_pk_fp8_f32((*this)(c), (*this)(e), v, true);
+        } else {
+            v = __builtin_amdgcn_cvt_pk_bf8_f32((*this)(a), (*this)(b), v, false);
+            v = __builtin_amdgcn_cvt_pk_bf8_f32((*this)(c), (*this)(e), v, true);
+        }
+        return (uint32_t)v;
+    }
+};
+
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+// eight bytes from column j of a row on (n of them)
+__device__ __forceinline__ void put8(uint8_t* p, u32x2 v, int n)
+{
+    typedef u32x2 Any __attribute__((aligned(1)));
+    if (n >= 8) {
+        *(Any*)p = v;
+    } else {
+        for (int i = 0; i < n; ++i) p[i] = (uint8_t)(v[i / 4] >> (i % 4 * 8));
+    }
+}
+
+// the largest of 16 neighbouring lanes
+__device__ __forceinline__ float most_of_16(float v)
+{
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+    return v;
+}
+
+constexpr int BLOCKS = 4;   // of a row, by each 16 lanes
+
+// blocks of rows whose elements are neighbours: 16 rows by 4 blocks a workgroup (16
+// rows' scales are then neighbours where they lie by columns)
+template <class T, int FORMAT>
+__global__ __launch_bounds__(256) void k_quantize_rows(QuantizeParams p, uint32_t across)
+{
+    const int64_t r = (int64_t)(blockIdx.x / across) * 16 + threadIdx.x / 16;
+    const int64_t b0 = (int64_t)(blockIdx.x % across) * BLOCKS;
+    const int c = threadIdx.x % 16 * 8;
+    if (r >= p.rows) return;   // (16 lanes together)
+    const T* x = static_cast<const T*>(p.x) + r * p.rs;
+    float v[BLOCKS][8];
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) get8(x, 1, (b0 + i) * FP8_BLOCK + c, p.cols, v[i]);
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+        const int64_t j = (b0 + i) * FP8_BLOCK + c;
+        if ((b0 + i) * FP8_BLOCK >= p.cols) break;
+        float most = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[i][e]));
+        most = most_of_16(most);
+        const Cut<FORMAT> cut(most);
+        put8(p.q + r * p.q_ld + j, u32x2{cut.four(v[i][0], v[i][1], v[i][2], v[i][3]),
+                                         cut.four(v[i][4], v[i][5], v[i][6], v[i][7])},
+             (int)max((int64_t)0, min((int64_t)8, p.cols - j)));
+        if (c == 0) p.scale.p[r * p.scale.rs + (b0 + i) * p.scale.cs] = Cut<FORMAT>::scale(most);
+    }
+}
+
+// tiles of 128 x 128, of any strides
+template <class T, int FORMAT, bool SQUARE>
+__global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_t across)
+{
+    constexpr int PITCH = FP8_BLOCK + 8;
+    __shared__ float most_lds[4][FP8_BLOCK];
+    __shared__ __attribute__((aligned(16))) uint8_t turned[FP8_BLOCK * PITCH];
+    const int64_t bi = blockIdx.x / across, bj = blockIdx.x % across;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int rg = threadIdx.x / 16 * 8, cg = threadIdx.x % 16 * 8;   // first of this thread's rows and columns
+    const int64_t r0 = bi * FP8_BLOCK, c0 = bj * FP8_BLOCK;
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + rg + i;
+        if (r < p.rows)
+            get8(static_cast<const T*>(p.x) + r * p.rs, p.cs, c0 + cg, p.cols, v[i]);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+    }
+    float row[8], col[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) row[i] = col[i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float a = fabsf(v[i][e]);
+            row[i] = fmaxf(row[i], a);
+            col[e] = fmaxf(col[e], a);
+        }
+    if constexpr (SQUARE) {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, row[i]);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+        if (lane == 0) most_lds[wave][0] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(most_lds[0][0], most_lds[1][0]), fmaxf(most_lds[2][0], most_lds[3][0]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row[i] = col[i] = most;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row[i] = most_of_16(row[i]);
+        if (p.qt) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                col[e] = fmaxf(col[e], __shfl_xor(col[e], 16, 64));
+                col[e] = fmaxf(col[e], __shfl_xor(col[e], 32, 64));
+                if (lane < 16) most_lds[wave][cg + e] = col[e];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                col[e] = fmaxf(fmaxf(most_lds[0][cg + e], most_lds[1][cg + e]),
+                               fmaxf(most_lds[2][cg + e], most_lds[3][cg + e]));
+        }
+    }
+    if (p.q) {
+        const int n = (int)max((int64_t)0, min((int64_t)8, p.cols - c0 - cg));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = r0 + rg + i;
+            if (r >= p.rows) break;
+            const Cut<FORMAT> cut(row[i]);
+            put8(p.q + r * p.q_ld + c0 + cg, u32x2{cut.four(v[i][0], v[i][1], v[i][2], v[i][3]),
+                                                   cut.four(v[i][4], v[i][5], v[i][6], v[i][7])}, n);
+            if (!SQUARE && cg == 0) p.scale.p[r * p.scale.rs + bj * p.scale.cs] = Cut<FORMAT>::scale(row[i]);
+        }
+        if (SQUARE && threadIdx.x == 0) p.scale.p[bi * p.scale.rs + bj * p.scale.cs] = Cut<FORMAT>::scale(row[0]);
+    }
+    if (!p.qt) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const Cut<FORMAT> cut(col[e]);
+        *(u32x2*)(turned + (cg + e) * PITCH + rg) =
+            u32x2{cut.four(v[0][e], v[1][e], v[2][e], v[3][e]), cut.four(v[4][e], v[5][e], v[6][e], v[7][e])};
+        if (!SQUARE && rg == 0 && c0 + cg + e < p.cols)
+            p.scale_t.p[(c0 + cg + e) * p.scale_t.rs + bi * p.scale_t.cs] = Cut<FORMAT>::scale(col[e]);
+    }
+    if (SQUARE && threadIdx.x == 0) p.scale_t.p[bj * p.scale_t.rs + bi * p.scale_t.cs] = Cut<FORMAT>::scale(col[0]);
+    __syncthreads();
+    for (int f = threadIdx.x; f < FP8_BLOCK * 16; f += 256) {
+        const int c = f / 16, h = f % 16 * 8;
+        if (c0 + c >= p.cols) break;
+        put8(p.qt + (c0 + c) * p.qt_ld + r0 + h, *(const u32x2*)(turned + c * PITCH + h),
+             (int)max((int64_t)0, min((int64_t)8, p.rows - r0 - h)));
+    }
+}
+
+template <class T, int FORMAT>
+hipError_t launch(const QuantizeParams& p, bool square, hipStream_t stream)
+{
+    const int64_t nb = (p.cols + FP8_BLOCK - 1) / FP8_BLOCK, mb = (p.rows + FP8_BLOCK - 1) / FP8_BLOCK;
+    if (!square && !p.qt && (p.cs == 1 || p.cols <= 1)) {
+        const int64_t across = (nb + BLOCKS - 1) / BLOCKS, down = (p.rows + 15) / 16;
+        if (across > 0xffffff / down) return hipErrorInvalidConfiguration;
+        hipLaunchKernelGGL((k_quantize_rows<T, FORMAT>), dim3((unsigned)(across * down)), dim3(256), 0, stream, p,
+                           (uint32_t)across);
+        return hipGetLastError();
+    }
+    if (nb > 0xffffff / mb) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)(nb * mb));
+    if (square)
+        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, true>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
+    else
+        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, false>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch(const QuantizeParams& p, int format, bool square, hipStream_t stream)
+{
+    return format == MAG_E4M3 ? launch<T, MAG_E4M3>(p, square, stream) : launch<T, MAG_E5M2>(p, square, stream);
+}
+
+__global__ __launch_bounds__(256) void k_pack8(Pack8Params p)
+{
+    const int64_t per_row = (p.cols + 15) / 16, n = p.rows * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = quotient(i, per_row), c = (i - r * per_row) * 16;
+        const uint8_t* src = p.src + r * p.rs;
+        uint8_t v[16];
+        if (p.cs == 1 && c + 16 <= p.cols) {
+            __builtin_memcpy(v, src + c, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = c + e < p.cols ? src[(c + e) * p.cs] : (uint8_t)0;
+        }
+        __builtin_memcpy(p.dst + r * p.ld + c, v, 16);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantizeParams& p, int dtype, int format, bool square, hipStream_t stream)
+{
+    if (dtype == MAG_F32) return launch<float>(p, format, square, stream);
+    if (dtype == MAG_F16) return launch<f16>(p, format, square, stream);
+    return launch<bf16>(p, format, square, stream);
+}
+
+hipError_t launch_pack8(const Pack8Params& p, hipStream_t stream)
+{
+    const int64_t n = p.rows * ((p.cols + 15) / 16);
+    hipLaunchKernelGGL(k_pack8, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16)), dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace mag
