@@ -950,6 +950,108 @@ int mag_linear_fp8_workspace_size(const mag_linear_fp8_args* args, size_t* bytes
 int mag_linear_fp8(const mag_linear_fp8_args* args, void* workspace, size_t workspace_bytes,
                    hipStream_t stream);
 
+#define MAG_NORM_LAYER 0 /* (x - mean) / sqrt(variance + eps)                      */
+#define MAG_NORM_RMS 1   /* x / sqrt(mean square + eps)                            */
+
+typedef struct mag_residual_norm_args {
+    int32_t dtype;        /* of the rows                                           */
+    int32_t weight_dtype; /* of weights and biases: dtype or MAG_F32               */
+    int32_t gate_dtype;   /* of the gate: dtype or MAG_F32                         */
+    int32_t kind;         /* MAG_NORM_*, of both norms                             */
+    int32_t post;         /* 1: the branch is normed too                           */
+    int32_t reserved;     /* 0                                                     */
+    mag_matrix residual;  /* [rows, width], width >= 1                             */
+    mag_matrix branch;    /* [rows, width], the block's output                     */
+    mag_matrix out;       /* output [rows, width]; may be residual itself          */
+    mag_matrix normed;    /* output [rows, width]; may be branch itself            */
+    mag_matrix gate;      /* [groups, width], its columns neighbours, data NULL:   */
+                          /* ones.  rows come as `groups` samples of one length    */
+    const void *weight, *bias;           /* [width] or NULL (ones, zeros)          */
+    const void *post_weight, *post_bias; /* likewise, of the branch's norm         */
+    float *mean, *rstd;           /* [rows], written where not NULL (an rms        */
+    float *post_mean, *post_rstd; /* norm's mean is 0)                             */
+    double scale;         /* of the branch                                         */
+    double eps;           /* >= 0                                                  */
+} mag_residual_norm_args;
+
+/*
+ * mag_residual_norm -- the norms around a block in one pass: a = the branch, or with
+ * post its norm times post_weight + post_bias; out = residual + scale gate a; normed =
+ * the norm of out (as it is stored) times weight + bias, the next block's input.
+ * Errors: MAG_E_NULL, MAG_E_SIZE (types, sizes, strides; rows that are no multiple of
+ * groups), MAG_E_ALIGN, MAG_E_HIP.
+ */
+int mag_residual_norm(const mag_residual_norm_args* args, hipStream_t stream);
+
+typedef struct mag_residual_norm_backward_args {
+    int32_t dtype, weight_dtype, gate_dtype, kind, post, reserved; /* as above     */
+    mag_matrix residual;  /* the forward pass's out                                */
+    mag_matrix branch;    /* the forward pass's branch                             */
+    mag_matrix d_normed;  /* the gradient of normed                                */
+    mag_matrix d_out;     /* the gradient of out beside it, data NULL: zeros       */
+    mag_matrix d_residual; /* output, data NULL: not wanted; may be d_out itself   */
+    mag_matrix d_branch;  /* output, data NULL: not wanted; may be branch or       */
+                          /* d_normed itself                                       */
+    mag_matrix gate;      /* as above                                              */
+    mag_matrix d_gate;    /* output [groups, width] of the gate's type, data NULL: */
+                          /* not wanted                                            */
+    const void *weight, *post_weight, *post_bias; /* as above                      */
+    const float *mean, *rstd, *post_mean, *post_rstd; /* of the forward pass       */
+    void *dweight, *dbias, *dpost_weight, *dpost_bias; /* outputs [width] or NULL  */
+    double scale;
+} mag_residual_norm_backward_args;
+
+/*
+ * mag_residual_norm_backward -- with N' the gradient of a norm: g = d_out + N'(d_normed
+ * weight) = d_residual; d = scale gate g; d_branch = d, with post N'(d post_weight);
+ * d_gate = scale times the sum over the group's rows of g a; dweight, dbias,
+ * dpost_weight and dpost_bias the sums over all rows of d_normed and d times the
+ * normed rows, and of themselves.  rows = 0 gives zeros.
+ *   workspace_size: of args' sizes of residual and gate.
+ * Errors as mag_residual_norm, and MAG_E_WORKSPACE.
+ */
+int mag_residual_norm_backward_workspace_size(const mag_residual_norm_backward_args* args, size_t* bytes);
+int mag_residual_norm_backward(const mag_residual_norm_backward_args* args, void* workspace,
+                               size_t workspace_bytes, hipStream_t stream);
+
+#define MAG_NORM_TWO 0 /* the root of the sum of all squares                       */
+#define MAG_NORM_INF 1 /* the largest magnitude                                    */
+#define MAG_MAX_TENSORS 65536
+
+/* One tensor of a list, on the device: count neighbours, or (cols > 0) count / cols
+   rows of cols neighbours that are in_stride and out_stride elements apart. */
+typedef struct mag_tensor_ref {
+    const void* in;
+    void* out;            /* mag_clip_gradients: may be in itself                  */
+    int64_t count, cols, in_stride, out_stride;
+    int32_t dtype;        /* MAG_F32 / MAG_F16 / MAG_BF16                          */
+    int32_t reserved;     /* 0                                                     */
+} mag_tensor_ref;
+
+typedef struct mag_tensors_args {
+    const mag_tensor_ref* tensors; /* a host array of n                            */
+    int64_t n;
+    int32_t kind;         /* MAG_NORM_TWO / MAG_NORM_INF                           */
+    int32_t reserved;     /* 0                                                     */
+    double max_norm, eps; /* mag_clip_gradients: finite, >= 0                      */
+    float* norm;          /* output (device), one value; or NULL when clipping     */
+} mag_tensors_args;
+
+/*
+ * mag_gradient_norm -- the norm of all elements of the tensors together.
+ * mag_clip_gradients -- that, and out = in min(1, max_norm / (norm + eps)), without a
+ * wait: the norm stays on the device.  An infinite norm makes finite elements zero, a
+ * norm that is NaN makes all NaN.  An output may be its own tensor, and otherwise
+ * overlaps no tensor of the list.  Squares are summed in fp64.
+ *   workspace_size: of the list's sizes.
+ * Errors: MAG_E_NULL, MAG_E_SIZE, MAG_E_ALIGN, MAG_E_WORKSPACE, MAG_E_HIP.
+ */
+int mag_clip_gradients_workspace_size(const mag_tensors_args* args, size_t* bytes);
+int mag_gradient_norm(const mag_tensors_args* args, void* workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+int mag_clip_gradients(const mag_tensors_args* args, void* workspace, size_t workspace_bytes,
+                       hipStream_t stream);
+
 /* Static description of a status code. */
 const char* mag_strerror(int status);
 /* Detail of the last error on the calling thread ("" if none). */

@@ -790,3 +790,6 @@ from ._block import (layer_norm, layer_norm_backward, layer_norm_backward_worksp
                      linear, linear_backward, linear_backward_workspace_size,
                      linear_workspace_size, orthogonalize, orthogonalize_workspace_size)
 from ._fp8 import linear_fp8, linear_fp8_workspace_size, quantize_fp8  # noqa: E402
+from ._training import (TensorList, clip_gradients, clip_gradients_workspace_size,  # noqa: E402
+                        gradient_norm, residual_norm, residual_norm_backward,
+                        residual_norm_backward_workspace_size)

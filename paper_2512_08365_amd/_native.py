@@ -43,6 +43,10 @@ MAG_F16 = 1
 MAG_BF16 = 2
 MAG_E4M3 = 3
 MAG_E5M2 = 4
+MAG_NORM_LAYER = 0
+MAG_NORM_RMS = 1
+MAG_NORM_TWO = 0
+MAG_NORM_INF = 1
 MAG_ACT_NONE = 0
 MAG_ACT_RELU = 1
 MAG_ACT_GELU = 2
@@ -70,6 +74,8 @@ EXPORTED = (
     "mag_layer_norm", "mag_layer_norm_backward_workspace_size", "mag_layer_norm_backward",
     "mag_orthogonalize_workspace_size", "mag_orthogonalize",
     "mag_quantize_fp8", "mag_linear_fp8_workspace_size", "mag_linear_fp8",
+    "mag_residual_norm", "mag_residual_norm_backward_workspace_size", "mag_residual_norm_backward",
+    "mag_clip_gradients_workspace_size", "mag_gradient_norm", "mag_clip_gradients",
     "mag_strerror", "mag_last_error", "mag_version",
 )
 
@@ -138,7 +144,18 @@ LINEAR_BACKWARD_ARGS = struct.Struct("@ii" + 6 * _MAT + "P")
 NORM_ARGS = struct.Struct("@ii" + 4 * _MAT + "PPPPPPd")
 QUANTIZE_ARGS = struct.Struct("@iiii" + 5 * _MAT)
 LINEAR_FP8_ARGS = struct.Struct("@iiii" + 7 * _MAT + "P")
+RESIDUAL_NORM_ARGS = struct.Struct("@iiiiii" + 5 * _MAT + "PPPPPPPPdd")
+RESIDUAL_NORM_BACKWARD_ARGS = struct.Struct("@iiiiii" + 8 * _MAT + "PPPPPPPPPPPd")
+TENSOR_REF = struct.Struct("@PPqqqqii")
+TENSORS_ARGS = struct.Struct("@PqiiddP")
 ORTHOGONALIZE_ARGS = struct.Struct("@iiq" + 2 * _MAT + "qqdddd")
+
+
+
+def address(data: bytes) -> int:
+    """where the bytes of `data` lie, as long as it is kept"""
+    return ctypes.cast(ctypes.c_char_p(data), ctypes.c_void_p).value or 0
+
 
 _lib = None
 
@@ -233,7 +250,8 @@ def load(path: str = LIB_PATH):
     lib.mag_stream_push_host.restype = ctypes.c_int
     # (the argument structs come packed, as bytes)
     c_bytes, c_size = ctypes.c_char_p, ctypes.c_size_t
-    for name in ("linear", "linear_backward", "layer_norm_backward", "orthogonalize", "linear_fp8"):
+    for name in ("linear", "linear_backward", "layer_norm_backward", "orthogonalize", "linear_fp8",
+                 "residual_norm_backward", "clip_gradients"):
         size = getattr(lib, f"mag_{name}_workspace_size")
         size.argtypes = [c_bytes, P(c_size)]
         size.restype = ctypes.c_int
@@ -242,6 +260,10 @@ def load(path: str = LIB_PATH):
         call.restype = ctypes.c_int
     lib.mag_layer_norm.argtypes = [c_bytes, c_vp]
     lib.mag_layer_norm.restype = ctypes.c_int
+    lib.mag_gradient_norm.argtypes = [c_bytes, c_vp, c_size, c_vp]
+    lib.mag_gradient_norm.restype = ctypes.c_int
+    lib.mag_residual_norm.argtypes = [c_bytes, c_vp]
+    lib.mag_residual_norm.restype = ctypes.c_int
     lib.mag_quantize_fp8.argtypes = [c_bytes, c_vp]
     lib.mag_quantize_fp8.restype = ctypes.c_int
     lib.mag_strerror.argtypes = [ctypes.c_int]

@@ -17,7 +17,7 @@
 
 #include <algorithm>
 
-#include "block.hpp"
+#include "rows.hpp"
 
 namespace mag {
 namespace {
@@ -26,101 +26,6 @@ constexpr int HELD = 16;          // elements a thread
 constexpr int64_t MOST_HELD = 1024 * HELD;  // width of a row that 1,024 threads hold
 constexpr int BACK_WGS = 256;     // workgroups of the backward pass, each with its own sums over
                                   // rows (twice as many where a CU's registers hold two)
-
-// The G threads of a row hold V neighbours each, G V further on the next V, and
-// so on.  V is 8 (the hardware takes vector loads and stores at any element);
-// TAIL: the width is no multiple of 8, and one thread has elements of fewer.
-// fp32 rows of such widths go element by element, V = 1: 64 lanes' 4 bytes are
-// whole lines at once (13,399 x 791: 16 us, in vectors 20 us; bfloat16, 3,739 x
-// 11,918 backward: 94 us in vectors, 201 us by element).
-template <class T, int V>
-struct Held {
-    T v[HELD];
-};
-
-template <int G, int V>
-__device__ __forceinline__ int column(int lane, int e)
-{
-    return (e / V * G + lane) * V + e % V;
-}
-
-template <int G, int V, bool TAIL, class T>
-__device__ __forceinline__ void get(Held<T, V>& r, const T* row, int lane, int n)
-{
-#pragma unroll
-    for (int c = 0; c < HELD / V; ++c) {
-        const int j = (c * G + lane) * V;
-        T* to = r.v + c * V;
-        if (j + (TAIL ? V - 1 : 0) < n) {
-            // (at once: by memcpy, what else TAIL loads comes into the same registers by
-            // copies, ten too many for two workgroups of the backward pass a CU)
-            typedef T Piece __attribute__((ext_vector_type(TAIL ? V : 1), aligned(sizeof(T))));
-            if constexpr (TAIL) {
-                const Piece t = *(const Piece*)(row + j);
-#pragma unroll
-                for (int i = 0; i < V; ++i) to[i] = t[i];
-            } else {
-                __builtin_memcpy(to, row + j, V * sizeof(T));
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) to[i] = (T)0.0f;
-            if (TAIL && j < n)
-#pragma unroll
-                for (int i = 0; i < V - 1; ++i)
-                    if (j + i < n) to[i] = row[j + i];
-        }
-    }
-}
-
-template <int G, int V, bool TAIL, class T>
-__device__ __forceinline__ void put(T* row, int lane, int n, const float* v)
-{
-#pragma unroll
-    for (int c = 0; c < HELD / V; ++c) {
-        const int j = (c * G + lane) * V;
-        T o[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = (T)v[c * V + i];
-        if (j + (TAIL ? V - 1 : 0) < n) {
-            __builtin_memcpy(row + j, o, V * sizeof(T));
-        } else if (TAIL && j < n) {
-#pragma unroll
-            for (int i = 0; i < V - 1; ++i)
-                if (j + i < n) row[j + i] = o[i];
-        }
-    }
-}
-
-__device__ __forceinline__ float wave_sum(float v)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
-}
-
-// The sums of a and b over the G threads of a row.  lds: two floats a wave,
-// another place from one call to the next of the same row and the next row's
-// first (one barrier a call: a place is written again two calls later).
-template <int G>
-__device__ __forceinline__ void row_sums(float& a, float& b, float2* lds)
-{
-    a = wave_sum(a);
-    b = wave_sum(b);
-    if constexpr (G > 64) {
-        constexpr int WAVES = G / 64;
-        const int wave = threadIdx.x / 64, first = wave / WAVES * WAVES;
-        if (threadIdx.x % 64 == 0) lds[wave] = float2{a, b};
-        __syncthreads();
-        a = b = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float2 s = lds[first + w];
-            a += s.x;
-            b += s.y;
-        }
-    }
-}
 
 template <class T, class W, int G, int V, bool TAIL, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
@@ -133,7 +38,7 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
     const T* x = static_cast<const T*>(p.x);
     float w[HELD], b[HELD];
     {
-        Held<W, V> a{}, d{};
+        Held<W, HELD> a{}, d{};
         if (p.weight) get<G, V, TAIL>(a, static_cast<const W*>(p.weight), lane, n);
         if (p.bias) get<G, V, TAIL>(d, static_cast<const W*>(p.bias), lane, n);
 #pragma unroll
@@ -142,7 +47,7 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
             b[e] = (float)d.v[e];
         }
     }
-    Held<T, V> next{};
+    Held<T, HELD> next{};
     const int64_t i0 = (int64_t)blockIdx.x * ROWS;
     if (i0 + sub < p.M) get<G, V, TAIL>(next, x + (i0 + sub) * p.x_rs, lane, n);
     // (the workgroup's rows go together: its barriers are everybody's)
@@ -168,7 +73,7 @@ __global__ __launch_bounds__(THREADS) void k_norm(NormParams p)
         if (i >= p.M) continue;
 #pragma unroll
         for (int e = 0; e < HELD; ++e) v[e] = fmaf(v[e] * rstd, w[e], b[e]);
-        put<G, V, TAIL>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, v);
+        put<G, V, TAIL, HELD>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, v);
         if (lane == 0) {
             if (p.mean) p.mean[i] = mean;
             if (p.rstd) p.rstd[i] = rstd;
@@ -226,12 +131,12 @@ __global__ __launch_bounds__(THREADS) void k_norm_back(NormParams p)
     const T *x = static_cast<const T*>(p.x), *dy = static_cast<const T*>(p.dy);
     float w[HELD], dw[HELD] = {}, db[HELD] = {};
     {
-        Held<W, V> a{};
+        Held<W, HELD> a{};
         if (p.weight) get<G, V, TAIL>(a, static_cast<const W*>(p.weight), lane, n);
 #pragma unroll
         for (int e = 0; e < HELD; ++e) w[e] = p.weight ? (float)a.v[e] : 1.0f;
     }
-    Held<T, V> nx{}, ny{};
+    Held<T, HELD> nx{}, ny{};
     auto load = [&](int64_t i) {
         get<G, V, TAIL>(nx, x + i * p.x_rs, lane, n);
         get<G, V, TAIL>(ny, dy + i * p.dy_rs, lane, n);
@@ -265,13 +170,13 @@ __global__ __launch_bounds__(THREADS) void k_norm_back(NormParams p)
         s2 /= (float)n;
 #pragma unroll
         for (int e = 0; e < HELD; ++e) h[e] = r * (h[e] - s1 - xh[e] * s2);
-        put<G, V, TAIL>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, h);
+        put<G, V, TAIL, HELD>(static_cast<T*>(p.y) + i * p.y_ld, lane, n, h);
     }
     if (!p.dweight && !p.dbias) return;
     float* part = p.part + (int64_t)blockIdx.x * 2 * n;
     if constexpr (ROWS == 1) {
-        put<G, V, TAIL>(part, lane, n, dw);
-        put<G, V, TAIL>(part + n, lane, n, db);
+        put<G, V, TAIL, HELD>(part, lane, n, dw);
+        put<G, V, TAIL, HELD>(part + n, lane, n, db);
     } else {
         for (int t = 0; t < ROWS; ++t) {
             if (sub == t)

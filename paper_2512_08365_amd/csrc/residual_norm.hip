@@ -1,0 +1,675 @@
+// residual_norm.hip -- the norms around a block, fused with its gate, its residual scale
+// and the addition between them, forward and backward.
+//
+// Both passes are bound by memory: the forward one reads the residual stream and the
+// block's output and writes the new stream and its normed rows, the backward one
+// reads four matrices and writes two.  Every row is read once into the registers of
+// 64 to 1,024 threads, 8 elements each (of rows above 8,192 16), the next one while the
+// present one's sums are taken.  Workgroups walk neighbouring rows, so that a
+// gate that many rows share is read once for them.
+//
+// Sums over a row and over rows, statistics and gradients are fp32; the stream's sum
+// is rounded to its type before the norm behind it reads it, as a reader of the
+// stored rows would.
+
+#include <algorithm>
+
+#include "rows.hpp"
+#include "step.hpp"
+
+namespace mag {
+namespace {
+
+constexpr int64_t MOST_HELD = 16384;   // width of a row that 1,024 threads hold
+constexpr int VECTORS = 5;             // of partial sums
+
+// a vector's elements of this thread (ones or zeros: of one that is not there)
+template <class W, int G, int V, bool TAIL, int E>
+__device__ __forceinline__ void vector(float* to, const void* p, int lane, int n, float missing)
+{
+    Held<W, E> a{};
+    if (p) get<G, V, TAIL>(a, static_cast<const W*>(p), lane, n);
+#pragma unroll
+    for (int e = 0; e < E; ++e) to[e] = p ? (float)a.v[e] : missing;
+}
+
+template <class T, int G, int V, bool TAIL, int E>
+__device__ __forceinline__ void gate_of(float* to, const ResidualNorm& p, int64_t group, int lane)
+{
+    if (!p.gate) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) to[e] = p.scale;
+        return;
+    }
+    if (p.gate_f32)
+        vector<float, G, V, TAIL, E>(to, static_cast<const float*>(p.gate) + group * p.gate_ld, lane, (int)p.N, 0.0f);
+    else
+        vector<T, G, V, TAIL, E>(to, static_cast<const T*>(p.gate) + group * p.gate_ld, lane, (int)p.N, 0.0f);
+#pragma unroll
+    for (int e = 0; e < E; ++e) to[e] *= p.scale;
+}
+
+// v, zeros behind the width, less its mean, which is left in `mean` (rms: as it is); the
+// return value is 1 / sqrt(its mean square + eps)
+template <int G, int V, int E, int WAVES>
+__device__ __forceinline__ float centre(float* v, float& mean, bool rms, int lane, int n, float eps,
+                                        float2 (&lds)[2][WAVES], int& turn)
+{
+    float s = 0.0f, unused = 0.0f;
+    mean = 0.0f;
+    if (!rms) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += v[e];
+        row_sums<G>(s, unused, lds[turn ^= 1]);
+        mean = s / (float)n;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = column<G, V>(lane, e) < n ? v[e] - mean : 0.0f;
+        s = 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) s = fmaf(v[e], v[e], s);
+    row_sums<G>(s, unused, lds[turn ^= 1]);
+    return 1.0f / sqrtf(s / (float)n + eps);
+}
+
+// rows [from, to) of a workgroup that takes ROWS at a time
+template <int ROWS>
+__device__ __forceinline__ void my_rows(int64_t M, int64_t& from, int64_t& to)
+{
+    const int64_t rounds = (M + ROWS - 1) / ROWS;
+    from = rounds * blockIdx.x / gridDim.x * ROWS;
+    to = min(M, rounds * (blockIdx.x + 1) / gridDim.x * ROWS);
+}
+
+template <class T, class W, int G, int E, int V, bool TAIL, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
+{
+    constexpr int ROWS = THREADS / G;
+    // (16 elements a thread: the vectors come from L2 for every row, there are no
+    // registers for them)
+    constexpr bool KEEP = E == 8;
+    __shared__ float2 lds[2][THREADS / 64];
+    int turn = 0;
+    const int lane = threadIdx.x % G, n = (int)p.N;
+    const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x / G);
+    int64_t from, to;
+    my_rows<ROWS>(p.M, from, to);
+    float w[E], b[E], pw[E], pb[E], gate[E];
+    auto pre_vectors = [&] {
+        vector<W, G, V, TAIL, E>(w, p.weight, lane, n, 1.0f);
+        vector<W, G, V, TAIL, E>(b, p.bias, lane, n, 0.0f);
+    };
+    auto post_vectors = [&] {
+        vector<W, G, V, TAIL, E>(pw, p.post_weight, lane, n, 1.0f);
+        vector<W, G, V, TAIL, E>(pb, p.post_bias, lane, n, 0.0f);
+    };
+    if constexpr (KEEP) {
+        pre_vectors();
+        post_vectors();
+    }
+    Held<T, E> nh{}, ny{};
+    auto load = [&](int64_t i) {
+        get<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
+        get<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
+    };
+    if (from + sub < to) load(from + sub);
+    int64_t group = -1, group_end = 0;
+    // (the workgroup's rows go together: its barriers are everybody's)
+    for (int64_t base = from; base < to; base += ROWS) {
+        const int64_t i = base + sub;
+        const bool on = i < to;
+        if (on && (!KEEP || i >= group_end)) {
+            group = i / p.length;
+            group_end = (group + 1) * p.length;
+            gate_of<T, G, V, TAIL, E>(gate, p, group, lane);
+        }
+        float v[E], y[E], mean, rstd, post_mean, post_rstd;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[e] = (float)nh.v[e];
+            y[e] = (float)ny.v[e];
+        }
+        if (i + ROWS < to) load(i + ROWS);
+        if (p.post) {
+            post_rstd = centre<G, V, E>(y, post_mean, p.rms, lane, n, p.eps, lds, turn);
+            if constexpr (!KEEP) post_vectors();
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] = fmaf(y[e] * post_rstd, pw[e], pb[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[e] = (float)(T)fmaf(gate[e], y[e], v[e]);
+            if (column<G, V>(lane, e) >= n) v[e] = 0.0f;
+        }
+        if (on) put<G, V, TAIL, E>(static_cast<T*>(p.out) + i * p.out_ld, lane, n, v);
+        rstd = centre<G, V, E>(v, mean, p.rms, lane, n, p.eps, lds, turn);
+        if (!on) continue;
+        if constexpr (!KEEP) pre_vectors();
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = fmaf(v[e] * rstd, w[e], b[e]);
+        put<G, V, TAIL, E>(static_cast<T*>(p.normed) + i * p.normed_ld, lane, n, v);
+        if (lane == 0) {
+            if (p.mean) p.mean[i] = mean;
+            if (p.rstd) p.rstd[i] = rstd;
+            if (p.post && p.post_mean) p.post_mean[i] = post_mean;
+            if (p.post && p.post_rstd) p.post_rstd[i] = post_rstd;
+        }
+    }
+}
+
+// The rows of a workgroup of the backward pass: groups [first, last), of each its
+// rows [from, to) (a chunk of one group, or whole groups).
+struct Mine {
+    int64_t first, last;
+    int64_t begin, end;   // of the first group's rows, chunks only
+    __device__ __forceinline__ explicit Mine(const ResidualNorm& p, uint32_t part)
+    {
+        if (p.chunks) {
+            first = part / (uint32_t)p.chunks;
+            last = first + 1;
+            const int64_t c = part % (uint32_t)p.chunks;
+            begin = first * p.length + p.length * c / p.chunks;
+            end = first * p.length + p.length * (c + 1) / p.chunks;
+        } else {
+            first = p.groups * part / p.parts;
+            last = p.groups * (part + 1) / p.parts;
+            begin = first * p.length;
+            end = begin + p.length;
+        }
+    }
+};
+
+// g = dr + rstd (dn w - m1 - hh m2), dy = post ? post_rstd (d pw - m3 - yn m4) : d with d =
+// scale gate g.  Each workgroup keeps its columns' sums over the rows, of a group
+// (g yn and g, from which the gate's and the post norm's gradients follow) and of all
+// its rows; they meet at the end of a group, or in the partial sums.
+template <class T, class W, int G, int E, int V, bool TAIL, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
+{
+    constexpr int ROWS = THREADS / G;
+    constexpr bool KEEP = E == 8;
+    __shared__ float2 lds[2][THREADS / 64];
+    __shared__ float sums[ROWS == 1 ? 1 : G * E];
+    int turn = 0;
+    const int lane = threadIdx.x % G, n = (int)p.N;
+    const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x / G);
+    const Mine mine(p, blockIdx.x);
+    float w[E], pw[E], pb[E], gate[E];
+    auto vectors = [&] {
+        vector<W, G, V, TAIL, E>(w, p.weight, lane, n, 1.0f);
+        vector<W, G, V, TAIL, E>(pw, p.post_weight, lane, n, 1.0f);
+    };
+    if constexpr (KEEP) {
+        vectors();
+        vector<W, G, V, TAIL, E>(pb, p.post_bias, lane, n, 0.0f);
+    }
+    float dw[E] = {}, db[E] = {}, dpw[E] = {}, dpb[E] = {}, s1[E] = {}, s2[E] = {};
+    Held<T, E> nh{}, ny{}, nn{}, nr{};
+    auto load = [&](int64_t i) {
+        get<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
+        get<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
+        get<G, V, TAIL>(nn, static_cast<const T*>(p.dn.p) + i * p.dn.rs, lane, n);
+        if (p.dr.p) get<G, V, TAIL>(nr, static_cast<const T*>(p.dr.p) + i * p.dr.rs, lane, n);
+    };
+    // the sums of all threads of a column, in the first row's threads (a fixed order)
+    auto over_rows = [&](float* v) {
+        if constexpr (ROWS > 1) {
+#pragma unroll 1
+            for (int t = ROWS - 1; t >= 0; --t) {
+                if (sub == t)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        // (by element, so that neighbouring lanes meet no bank twice)
+                        const int at = e * G + lane;
+                        v[e] = t == ROWS - 1 ? v[e] : sums[at] + v[e];
+                        if (t > 0) sums[at] = v[e];
+                    }
+                __syncthreads();
+            }
+        }
+    };
+    if (mine.begin + sub < mine.end) load(mine.begin + sub);
+    int64_t begin = mine.begin, end = mine.end;
+    for (int64_t group = mine.first; group < mine.last; ++group, begin = end, end += p.length) {
+        gate_of<T, G, V, TAIL, E>(gate, p, group, lane);
+        for (int64_t base = begin; base < end; base += ROWS) {
+            const int64_t i = base + sub;
+            const bool on = i < end;
+            const float mean = on && !p.rms ? p.mean[i] : 0.0f, rstd = on ? p.rstd[i] : 0.0f;
+            const float post_mean = on && p.post && !p.rms ? p.post_mean[i] : 0.0f;
+            const float post_rstd = on && p.post ? p.post_rstd[i] : 0.0f;
+            float hh[E], t[E], g[E], yn[E], m1 = 0.0f, m2 = 0.0f;
+            if constexpr (!KEEP) vectors();
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                // (beyond the width, and for a row beyond the last: 0)
+                const bool in = on && column<G, V>(lane, e) < n;
+                hh[e] = in ? ((float)nh.v[e] - mean) * rstd : 0.0f;
+                const float d = in ? (float)nn.v[e] : 0.0f;
+                dw[e] = fmaf(d, hh[e], dw[e]);
+                db[e] += d;
+                t[e] = d * w[e];
+                m1 += t[e];
+                m2 = fmaf(t[e], hh[e], m2);
+                g[e] = in && p.dr.p ? (float)nr.v[e] : 0.0f;
+                yn[e] = in ? (float)ny.v[e] : 0.0f;
+                if (p.post) yn[e] = in ? (yn[e] - post_mean) * post_rstd : 0.0f;
+            }
+            // the next row: of this group, or the next one's first
+            const int64_t next = min(base + ROWS, end) + sub;
+            const int64_t stop = base + ROWS < end ? end : group + 1 < mine.last ? end + p.length : 0;
+            if (next < stop) load(next);
+            row_sums<G>(m1, m2, lds[turn ^= 1]);
+            m1 = p.rms ? 0.0f : m1 / (float)n;
+            m2 /= (float)n;
+            float m3 = 0.0f, m4 = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool in = on && column<G, V>(lane, e) < n;
+                g[e] = in ? fmaf(rstd, t[e] - m1 - hh[e] * m2, g[e]) : 0.0f;
+                s1[e] = fmaf(g[e], yn[e], s1[e]);
+                s2[e] += g[e];
+            }
+            if (on && p.out) put<G, V, TAIL, E>(static_cast<T*>(p.out) + i * p.out_ld, lane, n, g);
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] *= gate[e];
+            if (p.post) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    g[e] *= pw[e];
+                    m3 += g[e];
+                    m4 = fmaf(g[e], yn[e], m4);
+                }
+                row_sums<G>(m3, m4, lds[turn ^= 1]);
+                m3 = p.rms ? 0.0f : m3 / (float)n;
+                m4 /= (float)n;
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] = post_rstd * (g[e] - m3 - yn[e] * m4);
+            }
+            if (on && p.normed) put<G, V, TAIL, E>(static_cast<T*>(p.normed) + i * p.normed_ld, lane, n, g);
+        }
+        // the group's sums: the gate's gradient is scale (pw s1 + pb s2), the post norm's
+        // weights' are scale gate s1 and scale gate s2
+        if constexpr (!KEEP) {
+            vectors();
+            vector<W, G, V, TAIL, E>(pb, p.post_bias, lane, n, 0.0f);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            dpw[e] = fmaf(gate[e], s1[e], dpw[e]);
+            dpb[e] = fmaf(gate[e], s2[e], dpb[e]);
+            s1[e] = p.scale * (p.post ? fmaf(pw[e], s1[e], pb[e] * s2[e]) : s1[e]);
+            s2[e] = 0.0f;
+        }
+        if (p.chunks) continue;   // (one group, its gate's partial sums in s1)
+        if (p.d_gate) {
+            over_rows(s1);
+            if (sub == 0) {
+                if (p.gate_f32)
+                    put<G, V, TAIL, E>(static_cast<float*>(p.d_gate) + group * p.d_gate_ld, lane, n, s1);
+                else
+                    put<G, V, TAIL, E>(static_cast<T*>(p.d_gate) + group * p.d_gate_ld, lane, n, s1);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) s1[e] = 0.0f;
+    }
+    float* part = p.part + (int64_t)blockIdx.x * VECTORS * n;
+    auto leave = [&](bool wanted, float* v, int at) {
+        if (!wanted) return;
+        over_rows(v);
+        if (sub == 0) put<G, V, TAIL, E>(part + (int64_t)at * n, lane, n, v);
+    };
+    leave(p.dweight, dw, 0);
+    leave(p.dbias, db, 1);
+    leave(p.dpost_weight, dpw, 2);
+    leave(p.dpost_bias, dpb, 3);
+    leave(p.d_gate && p.chunks, s1, 4);
+}
+
+// The workgroups' sums added up: 16 columns a workgroup, 64 threads each that have
+// all of their loads in flight.  blockIdx.y: a vector's sums over all parts, or from
+// the fifth on a group's gate over its chunks.
+template <class T, class W>
+__global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
+{
+    __shared__ float sums[64][17];
+    const int col = threadIdx.x % 16, row = threadIdx.x / 16;
+    const int64_t j = (int64_t)blockIdx.x * 16 + col, n = p.N;
+    const int vector = min((int)blockIdx.y, VECTORS - 1);
+    void* const of[4] = {p.dweight, p.dbias, p.dpost_weight, p.dpost_bias};
+    const int64_t group = (int64_t)blockIdx.y - (VECTORS - 1);
+    const bool gate = group >= 0;
+    if (!gate && !of[vector & 3]) return;
+    const int first = gate ? (int)group * p.chunks : 0, count = gate ? p.chunks : p.parts;
+    const float* part = p.part + ((int64_t)first * VECTORS + vector) * n + j;
+    float t[8] = {};
+    if (j < n)
+        for (int k = row; k < count; k += 512)
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (k + 64 * u < count) t[u] += part[(int64_t)(k + 64 * u) * VECTORS * n];
+    sums[row][col] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+    __syncthreads();
+    if (threadIdx.x >= 16 || j >= n) return;
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 64; ++k) s += sums[k][col];
+    if (!gate)
+        static_cast<W*>(of[vector & 3])[j] = (W)s;
+    else if (p.gate_f32)
+        static_cast<float*>(p.d_gate)[group * p.d_gate_ld + j] = s;
+    else
+        static_cast<T*>(p.d_gate)[group * p.d_gate_ld + j] = (T)s;
+}
+
+// ------------------------------------------------- rows that no registers hold
+// Too wide, or with elements that are not neighbours: read element by element, two or
+// three times, the later ones from L2.
+
+template <class T>
+__device__ __forceinline__ float at(const Strided& m, int64_t i, int64_t j)
+{
+    return (float)static_cast<const T*>(m.p)[i * m.rs + j * m.cs];
+}
+template <class W>
+__device__ __forceinline__ float at(const void* v, int64_t j, float missing)
+{
+    return v ? (float)static_cast<const W*>(v)[j] : missing;
+}
+template <class T>
+__device__ __forceinline__ float gate_at(const ResidualNorm& p, int64_t group, int64_t j)
+{
+    if (!p.gate) return p.scale;
+    return p.scale * (p.gate_f32 ? static_cast<const float*>(p.gate)[group * p.gate_ld + j]
+                                 : (float)static_cast<const T*>(p.gate)[group * p.gate_ld + j]);
+}
+
+template <class F>
+__device__ __forceinline__ float centre_wide(F value, int64_t n, bool rms, float eps, float& mean,
+                                             float2 (&lds)[2][16], int& turn)
+{
+    float s = 0.0f, unused = 0.0f;
+    mean = 0.0f;
+    if (!rms) {
+        for (int64_t j = threadIdx.x; j < n; j += 1024) s += value(j);
+        row_sums<1024>(s, unused, lds[turn ^= 1]);
+        mean = s / (float)n;
+        s = 0.0f;
+    }
+    for (int64_t j = threadIdx.x; j < n; j += 1024) {
+        const float d = value(j) - mean;
+        s = fmaf(d, d, s);
+    }
+    row_sums<1024>(s, unused, lds[turn ^= 1]);
+    return 1.0f / sqrtf(s / (float)n + eps);
+}
+
+template <class T, class W>
+__global__ __launch_bounds__(1024) void k_residual_norm_wide(ResidualNorm p)
+{
+    __shared__ float2 lds[2][16];
+    int turn = 0;
+    const int64_t n = p.N;
+    for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
+        const int64_t group = i / p.length;
+        float mean, rstd, post_mean = 0.0f, post_rstd = 1.0f;
+        if (p.post)
+            post_rstd = centre_wide([&](int64_t j) { return at<T>(p.y, i, j); }, n, p.rms, p.eps, post_mean, lds, turn);
+        T* out = static_cast<T*>(p.out) + i * p.out_ld;
+        for (int64_t j = threadIdx.x; j < n; j += 1024) {
+            float y = at<T>(p.y, i, j);
+            if (p.post)
+                y = fmaf((y - post_mean) * post_rstd, at<W>(p.post_weight, j, 1.0f), at<W>(p.post_bias, j, 0.0f));
+            out[j] = (T)fmaf(gate_at<T>(p, group, j), y, at<T>(p.h, i, j));
+        }
+        // (each thread reads what it wrote itself)
+        rstd = centre_wide([&](int64_t j) { return (float)out[j]; }, n, p.rms, p.eps, mean, lds, turn);
+        for (int64_t j = threadIdx.x; j < n; j += 1024)
+            static_cast<T*>(p.normed)[i * p.normed_ld + j] =
+                (T)fmaf(((float)out[j] - mean) * rstd, at<W>(p.weight, j, 1.0f), at<W>(p.bias, j, 0.0f));
+        if (threadIdx.x == 0) {
+            if (p.mean) p.mean[i] = mean;
+            if (p.rstd) p.rstd[i] = rstd;
+            if (p.post && p.post_mean) p.post_mean[i] = post_mean;
+            if (p.post && p.post_rstd) p.post_rstd[i] = post_rstd;
+        }
+    }
+}
+
+// an element's normed row, its stream's gradient and its normed block output
+template <class T, class W>
+struct Element {
+    float hh, dn, g, yn;
+    __device__ __forceinline__ Element(const ResidualNorm& p, int64_t i, int64_t j, float m1, float m2)
+    {
+        const float rstd = p.rstd[i];
+        hh = (at<T>(p.h, i, j) - (p.rms ? 0.0f : p.mean[i])) * rstd;
+        dn = at<T>(p.dn, i, j);
+        g = fmaf(rstd, dn * at<W>(p.weight, j, 1.0f) - m1 - hh * m2, p.dr.p ? at<T>(p.dr, i, j) : 0.0f);
+        yn = at<T>(p.y, i, j);
+        if (p.post) yn = (yn - (p.rms ? 0.0f : p.post_mean[i])) * p.post_rstd[i];
+    }
+};
+
+// the means that a row's elements need of their neighbours
+template <class T, class W>
+__global__ __launch_bounds__(1024) void k_residual_norm_back_means(ResidualNorm p)
+{
+    __shared__ float2 lds[2][16];
+    int turn = 0;
+    const int64_t n = p.N;
+    for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
+        const int64_t group = i / p.length;
+        float m1 = 0.0f, m2 = 0.0f, m3 = 0.0f, m4 = 0.0f;
+        for (int64_t j = threadIdx.x; j < n; j += 1024) {
+            const Element<T, W> x(p, i, j, 0.0f, 0.0f);
+            const float t = x.dn * at<W>(p.weight, j, 1.0f);
+            m1 += t;
+            m2 = fmaf(t, x.hh, m2);
+        }
+        row_sums<1024>(m1, m2, lds[turn ^= 1]);
+        m1 = p.rms ? 0.0f : m1 / (float)n;
+        m2 /= (float)n;
+        if (p.post) {
+            for (int64_t j = threadIdx.x; j < n; j += 1024) {
+                const Element<T, W> x(p, i, j, m1, m2);
+                const float d = x.g * gate_at<T>(p, group, j) * at<W>(p.post_weight, j, 1.0f);
+                m3 += d;
+                m4 = fmaf(d, x.yn, m4);
+            }
+            row_sums<1024>(m3, m4, lds[turn ^= 1]);
+            m3 = p.rms ? 0.0f : m3 / (float)n;
+            m4 /= (float)n;
+        }
+        if (threadIdx.x == 0) {
+            float* m = p.rows + i * 4;
+            m[0] = m1, m[1] = m2, m[2] = m3, m[3] = m4;
+        }
+    }
+}
+
+// the sums over the rows, by column...
+template <class T, class W>
+__global__ __launch_bounds__(256) void k_residual_norm_back_wide_columns(ResidualNorm p)
+{
+    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x, n = p.N;
+    if (j >= n) return;
+    for (int64_t part = blockIdx.y; part < p.parts; part += gridDim.y) {
+        const Mine mine(p, (uint32_t)part);
+        const float pw = at<W>(p.post_weight, j, 1.0f), pb = at<W>(p.post_bias, j, 0.0f);
+        float dw = 0.0f, db = 0.0f, dpw = 0.0f, dpb = 0.0f, dg = 0.0f;
+        int64_t begin = mine.begin, end = mine.end;
+        for (int64_t group = mine.first; group < mine.last; ++group, begin = end, end += p.length) {
+            const float gate = gate_at<T>(p, group, j);
+            float s1 = 0.0f, s2 = 0.0f;
+            for (int64_t i = begin; i < end; ++i) {
+                const Element<T, W> x(p, i, j, p.rows[i * 4], p.rows[i * 4 + 1]);
+                dw = fmaf(x.dn, x.hh, dw);
+                db += x.dn;
+                s1 = fmaf(x.g, x.yn, s1);
+                s2 += x.g;
+            }
+            dpw = fmaf(gate, s1, dpw);
+            dpb = fmaf(gate, s2, dpb);
+            dg = p.scale * (p.post ? fmaf(pw, s1, pb * s2) : s1);
+            if (p.d_gate && !p.chunks) {
+                if (p.gate_f32)
+                    static_cast<float*>(p.d_gate)[group * p.d_gate_ld + j] = dg;
+                else
+                    static_cast<T*>(p.d_gate)[group * p.d_gate_ld + j] = (T)dg;
+            }
+        }
+        float* to = p.part + part * VECTORS * n + j;
+        to[0] = dw, to[n] = db, to[2 * n] = dpw, to[3 * n] = dpb, to[4 * n] = dg;
+    }
+}
+
+// ... and the rows' gradients, after them (they may be written over what was read)
+template <class T, class W>
+__global__ __launch_bounds__(1024) void k_residual_norm_back_wide(ResidualNorm p)
+{
+    for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
+        const int64_t group = i / p.length;
+        const float* m = p.rows + i * 4;
+        for (int64_t j = threadIdx.x; j < p.N; j += 1024) {
+            const Element<T, W> x(p, i, j, m[0], m[1]);
+            float d = x.g * gate_at<T>(p, group, j);
+            if (p.post) d = p.post_rstd[i] * (d * at<W>(p.post_weight, j, 1.0f) - m[2] - x.yn * m[3]);
+            if (p.out) static_cast<T*>(p.out)[i * p.out_ld + j] = (T)x.g;
+            if (p.normed) static_cast<T*>(p.normed)[i * p.normed_ld + j] = (T)d;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------ launches
+
+bool neighbours(const Strided& m, int64_t n) { return !m.p || n <= 1 || m.cs == 1; }
+
+// threads of a row of width n, and rows that a workgroup takes at a time
+int threads_of(int64_t n) { return n <= 512 ? 64 : n <= 2048 ? 256 : n <= 4096 ? 512 : 1024; }
+int rows_at_once(int64_t n) { return n <= 512 ? 4 : 1; }
+
+template <class T, class W, int V, bool TAIL>
+void forward_held(const ResidualNorm& p, hipStream_t stream)
+{
+    const int64_t rounds = (p.M + rows_at_once(p.N) - 1) / rows_at_once(p.N);
+    const int G = threads_of(p.N);
+    const int64_t most = G == 1024 ? 512 : G == 512 ? 1024 : 2048;
+    const dim3 grid((unsigned)std::min(rounds, most));
+    if (G == 64)
+        hipLaunchKernelGGL((k_residual_norm<T, W, 64, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 256)
+        hipLaunchKernelGGL((k_residual_norm<T, W, 256, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 512)
+        hipLaunchKernelGGL((k_residual_norm<T, W, 512, 8, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
+    else if (p.N <= 8192)
+        hipLaunchKernelGGL((k_residual_norm<T, W, 1024, 8, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+    else
+        hipLaunchKernelGGL((k_residual_norm<T, W, 1024, 16, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+}
+
+template <class T, class W, int V, bool TAIL>
+void backward_held(const ResidualNorm& p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)p.parts);
+    const int G = threads_of(p.N);
+    if (G == 64)
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 64, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 256)
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 256, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 512)
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 512, 8, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
+    else if (p.N <= 8192)
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 1024, 8, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+    else
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 1024, 16, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+}
+
+// workgroups that walk M rows, one at a time each
+dim3 wide_grid(int64_t M) { return dim3((unsigned)std::min<int64_t>(M, 1 << 16)); }
+
+bool wide(const ResidualNorm& p)
+{
+    return p.N > MOST_HELD || !neighbours(p.h, p.N) || !neighbours(p.y, p.N) || !neighbours(p.dn, p.N) ||
+           !neighbours(p.dr, p.N);
+}
+
+template <class T, class W>
+hipError_t forward(const ResidualNorm& p, hipStream_t stream)
+{
+    if (wide(p))
+        hipLaunchKernelGGL((k_residual_norm_wide<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
+    else if (p.N % 8 == 0)
+        forward_held<T, W, 8, false>(p, stream);
+    else
+        forward_held<T, W, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, stream);
+    return hipGetLastError();
+}
+
+template <class T, class W>
+hipError_t backward(const ResidualNorm& p, hipStream_t stream)
+{
+    const bool sums = p.dweight || p.dbias || p.dpost_weight || p.dpost_bias || p.d_gate;
+    if (!sums && !p.out && !p.normed) return hipSuccess;
+    const bool by_element = wide(p);
+    hipError_t e = hipSuccess;
+    if (by_element) {
+        if (p.M > 0)
+            hipLaunchKernelGGL((k_residual_norm_back_means<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if (sums)
+            hipLaunchKernelGGL((k_residual_norm_back_wide_columns<T, W>),
+                               dim3((unsigned)((p.N + 255) / 256), (unsigned)std::min(p.parts, 1024)), dim3(256), 0,
+                               stream, p);
+    } else if (p.N % 8 == 0) {
+        backward_held<T, W, 8, false>(p, stream);
+    } else {
+        backward_held<T, W, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, stream);
+    }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (sums) {
+        const int64_t jobs = VECTORS - 1 + (p.d_gate && p.chunks ? p.groups : 0);
+        hipLaunchKernelGGL((k_residual_norm_columns<T, W>), dim3((unsigned)((p.N + 15) / 16), (unsigned)jobs),
+                           dim3(1024), 0, stream, p);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (by_element && p.M > 0 && (p.out || p.normed))
+        hipLaunchKernelGGL((k_residual_norm_back_wide<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// A group of many rows is cut into chunks, each a workgroup; many groups are dealt out
+// whole, so that a workgroup writes their gates' gradients itself.
+RowParts residual_norm_parts(const ResidualNorm& p)
+{
+    const bool by_element = wide(p);
+    const int64_t rows = by_element ? 1 : rows_at_once(p.N);
+    const int64_t most = !by_element && p.N > 4096 ? 256 : 512;
+    if (p.M == 0) return {1, 0, by_element};
+    if (2 * p.groups > most) return {(int)std::min(most, p.groups), 0, by_element};
+    const int64_t rounds = (p.length + rows - 1) / rows;
+    const int64_t chunks = std::max<int64_t>(1, std::min(most / p.groups, rounds));
+    return {(int)(chunks * p.groups), (int)chunks, by_element};
+}
+
+hipError_t launch_residual_norm(const ResidualNorm& p, int dtype, int weight_dtype, hipStream_t stream)
+{
+    if (p.M == 0) return hipSuccess;
+    const bool full = weight_dtype == MAG_F32;
+    if (dtype == MAG_F32) return forward<float, float>(p, stream);
+    if (dtype == MAG_F16) return full ? forward<f16, float>(p, stream) : forward<f16, f16>(p, stream);
+    return full ? forward<bf16, float>(p, stream) : forward<bf16, bf16>(p, stream);
+}
+
+hipError_t launch_residual_norm_backward(const ResidualNorm& p, int dtype, int weight_dtype, hipStream_t stream)
+{
+    const bool full = weight_dtype == MAG_F32;
+    if (dtype == MAG_F32) return backward<float, float>(p, stream);
+    if (dtype == MAG_F16) return full ? backward<f16, float>(p, stream) : backward<f16, f16>(p, stream);
+    return full ? backward<bf16, float>(p, stream) : backward<bf16, bf16>(p, stream);
+}
+
+}  // namespace mag
