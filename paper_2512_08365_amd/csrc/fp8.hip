@@ -120,6 +120,8 @@ size_t plan_linear(const mag_linear_fp8_args* a, void* ws, Plan& pl)
     pl.skinny = a->x.rows <= mag::SKINNY_ROWS;
     pl.pack_x = pl.skinny ? a->x.cols > 1 && a->x.col_stride != 1 : !in_place(a->x);
     pl.pack_w = pl.skinny ? a->weight.cols > 1 && a->weight.col_stride != 1 : !in_place(a->weight);
+    // (few rows: 16 bytes of a row at least)
+    if (pl.skinny && a->x.cols > 0 && a->x.cols < 16) pl.pack_x = pl.pack_w = true;
     pl.ld_x = pl.pack_x ? packed_ld(a->x.cols) : a->x.rows > 1 ? a->x.row_stride : 0;
     pl.ld_w = pl.pack_w ? packed_ld(a->weight.cols) : a->weight.rows > 1 ? a->weight.row_stride : 0;
     pl.splits = 1;
@@ -271,6 +273,7 @@ int mag_linear_fp8(const mag_linear_fp8_args* a, void* workspace, size_t workspa
     p.e.y_ld = a->y.row_stride;
     p.e.vec = !p.e.res || p.e.res_cs == 1;
     if (pl.skinny) {
+        if (K > 0) p.K = std::max<int64_t>(K, 16);
         TRY_HIP(mag::launch_skinny8(p, a->dtype, stream), "linear_fp8 launch");
         return MAG_OK;
     }

@@ -45,7 +45,7 @@ struct Mm8 {
 hipError_t launch_mm8_64(const Mm8& p, int dtype, hipStream_t stream);
 hipError_t launch_mm8_128(const Mm8& p, int dtype, hipStream_t stream);
 hipError_t launch_mm8_256(const Mm8& p, int dtype, hipStream_t stream);
-// at most SKINNY_ROWS rows, operands at any alignment and distance
+// at most SKINNY_ROWS rows, operands at any alignment and distance, K 0 or at least 16
 hipError_t launch_skinny8(const Mm8& p, int dtype, hipStream_t stream);
 
 // rows x cols bytes of any strides as rows of ld bytes

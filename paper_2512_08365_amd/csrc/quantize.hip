@@ -10,6 +10,7 @@
 
 #include "fp8.hpp"
 #include "mm.hpp"
+#include "rows.hpp"
 
 namespace mag {
 namespace {
@@ -25,18 +26,23 @@ template <int FORMAT>
 struct Cut {
     static constexpr float LARGEST = FORMAT == MAG_E4M3 ? 448.0f : 57344.0f;
     static constexpr float DOWN = FORMAT == MAG_E4M3 ? 0x1p-9f : 0x1p-16f;
+    static constexpr float ONE = 1.0f / LARGEST;
     float d, inverse;
 
     __device__ __forceinline__ explicit Cut(float most)
     {
         d = fmaxf(most * DOWN, 0.875f * 0x1p-126f);
-        inverse = 1.0f / d;
+        // (d and 1 / d lie between 2^-127 and 2^127: neither argument nor result of the
+        // hardware's reciprocal, off by a unit of the last place, is a small number)
+        inverse = __builtin_amdgcn_rcpf(d * 16.0f) * 16.0f;
         // (an infinite one: finite numbers become 0, infinite ones NaN)
         if (most == __builtin_inff()) d = 1.0f, inverse = 0.0f;
     }
     static __device__ __forceinline__ float scale(float most)
     {
-        return fmaxf(most / LARGEST, (float)MAG_FP8_LEAST_SCALE);
+        // (most / LARGEST, to the last place by a correction; an infinite one stays it)
+        const float q = most * ONE, s = fmaf(fmaf(-q, LARGEST, most), ONE, q);
+        return fmaxf(most == __builtin_inff() ? most : s, (float)MAG_FP8_LEAST_SCALE);
     }
     __device__ __forceinline__ float operator()(float x) const
     {
@@ -71,19 +77,62 @@ __device__ __forceinline__ void put8(uint8_t* p, u32x2 v, int n)
     }
 }
 
+// v of another lane of a group of 16 (CONTROL: the data-parallel one of the instruction)
+template <int CONTROL>
+__device__ __forceinline__ float moved(float v)
+{
+    const int i = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, CONTROL, 0xf, 0xf, true));
+}
+
 // the largest of 16 neighbouring lanes
 __device__ __forceinline__ float most_of_16(float v)
 {
+    v = fmaxf(v, moved<0xb1>(v));    // lane ^ 1
+    v = fmaxf(v, moved<0x4e>(v));    // lane ^ 2
+    v = fmaxf(v, moved<0x141>(v));   // 7 - lane % 8
+    return fmaxf(v, moved<0x140>(v));   // 15 - lane % 16
+}
+
+// the largest of the four lanes 16 apart
+__device__ __forceinline__ float most_of_rows(float v)
+{
+    const unsigned a = __builtin_bit_cast(unsigned, v);
+    const auto x = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    const unsigned x0 = x[0], x1 = x[1];
+    v = fmaxf(__builtin_bit_cast(float, x0), __builtin_bit_cast(float, x1));
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto y = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    const unsigned y0 = y[0], y1 = y[1];
+    return fmaxf(__builtin_bit_cast(float, y0), __builtin_bit_cast(float, y1));
+}
+
+// Eight neighbours from column j on, whose places and values settled() gives: zeros from
+// column `cols` on.  WHOLE: neighbours in memory, in rows of whole blocks.
+template <bool WHOLE, class T>
+__device__ __forceinline__ void eight(Held<T, 8>& h, const T* row, int64_t cs, int64_t j, int64_t cols)
+{
+    if (WHOLE)
+        get<1, 8, false>(h, row + j, 0, 8);
+    else if (cs == 1 && cols >= 8)
+        fetch<1, 8, true>(h, row, (int)(j / 8), (int)cols);
+    else
 #pragma unroll
-    for (int d = 8; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-    return v;
+        for (int i = 0; i < 8; ++i) h.v[i] = row[min(j + i, cols - 1) * cs];
+}
+template <bool WHOLE, class T>
+__device__ __forceinline__ void settled(Held<T, 8>& h, int64_t cs, int64_t j, int64_t cols, float* v)
+{
+    if (!WHOLE && cs == 1 && cols >= 8) settle<1, 8, true>(h, (int)(j / 8), (int)cols);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = WHOLE || j + i < cols ? (float)h.v[i] : 0.0f;
 }
 
 constexpr int BLOCKS = 4;   // of a row, by each 16 lanes
 
 // blocks of rows whose elements are neighbours: 16 rows by 4 blocks a workgroup (16
 // rows' scales are then neighbours where they lie by columns)
-template <class T, int FORMAT>
+template <class T, int FORMAT, bool WHOLE>
 __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeParams p, uint32_t across)
 {
     const int64_t r = (int64_t)(blockIdx.x / across) * 16 + threadIdx.x / 16;
@@ -91,27 +140,30 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeParams p, uint32_
     const int c = threadIdx.x % 16 * 8;
     if (r >= p.rows) return;   // (16 lanes together)
     const T* x = static_cast<const T*>(p.x) + r * p.rs;
-    float v[BLOCKS][8];
+    Held<T, 8> h[BLOCKS];
 #pragma unroll
-    for (int i = 0; i < BLOCKS; ++i) get8(x, 1, (b0 + i) * FP8_BLOCK + c, p.cols, v[i]);
+    for (int i = 0; i < BLOCKS; ++i)
+        if (!WHOLE || (b0 + i) * FP8_BLOCK < p.cols) eight<WHOLE>(h[i], x, 1, (b0 + i) * FP8_BLOCK + c, p.cols);
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) {
         const int64_t j = (b0 + i) * FP8_BLOCK + c;
         if ((b0 + i) * FP8_BLOCK >= p.cols) break;
+        float v[8];
+        settled<WHOLE>(h[i], 1, j, p.cols, v);
         float most = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[i][e]));
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
         most = most_of_16(most);
         const Cut<FORMAT> cut(most);
-        put8(p.q + r * p.q_ld + j, u32x2{cut.four(v[i][0], v[i][1], v[i][2], v[i][3]),
-                                         cut.four(v[i][4], v[i][5], v[i][6], v[i][7])},
+        put8(p.q + r * p.q_ld + j, u32x2{cut.four(v[0], v[1], v[2], v[3]),
+                                         cut.four(v[4], v[5], v[6], v[7])},
              (int)max((int64_t)0, min((int64_t)8, p.cols - j)));
         if (c == 0) p.scale.p[r * p.scale.rs + (b0 + i) * p.scale.cs] = Cut<FORMAT>::scale(most);
     }
 }
 
 // tiles of 128 x 128, of any strides
-template <class T, int FORMAT, bool SQUARE>
+template <class T, int FORMAT, bool SQUARE, bool WHOLE>
 __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_t across)
 {
     constexpr int PITCH = FP8_BLOCK + 8;
@@ -122,14 +174,14 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_
     const int rg = threadIdx.x / 16 * 8, cg = threadIdx.x % 16 * 8;   // first of this thread's rows and columns
     const int64_t r0 = bi * FP8_BLOCK, c0 = bj * FP8_BLOCK;
     float v[8][8];
+    {
+        // (behind the last row: it once more, which no largest number changes with)
+        Held<T, 8> h[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t r = r0 + rg + i;
-        if (r < p.rows)
-            get8(static_cast<const T*>(p.x) + r * p.rs, p.cs, c0 + cg, p.cols, v[i]);
-        else
+        for (int i = 0; i < 8; ++i)
+            eight<WHOLE>(h[i], static_cast<const T*>(p.x) + min(r0 + rg + i, p.rows - 1) * p.rs, p.cs, c0 + cg, p.cols);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+        for (int i = 0; i < 8; ++i) settled<WHOLE>(h[i], p.cs, c0 + cg, p.cols, v[i]);
     }
     float row[8], col[8];
 #pragma unroll
@@ -146,8 +198,7 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) most = fmaxf(most, row[i]);
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+        most = most_of_rows(most_of_16(most));
         if (lane == 0) most_lds[wave][0] = most;
         __syncthreads();
         most = fmaxf(fmaxf(most_lds[0][0], most_lds[1][0]), fmaxf(most_lds[2][0], most_lds[3][0]));
@@ -159,8 +210,7 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_
         if (p.qt) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                col[e] = fmaxf(col[e], __shfl_xor(col[e], 16, 64));
-                col[e] = fmaxf(col[e], __shfl_xor(col[e], 32, 64));
+                col[e] = most_of_rows(col[e]);
                 if (lane < 16) most_lds[wave][cg + e] = col[e];
             }
             __syncthreads();
@@ -176,6 +226,7 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_
         for (int i = 0; i < 8; ++i) {
             const int64_t r = r0 + rg + i;
             if (r >= p.rows) break;
+            __builtin_amdgcn_sched_barrier(0);   // (a row at a time: registers)
             const Cut<FORMAT> cut(row[i]);
             put8(p.q + r * p.q_ld + c0 + cg, u32x2{cut.four(v[i][0], v[i][1], v[i][2], v[i][3]),
                                                    cut.four(v[i][4], v[i][5], v[i][6], v[i][7])}, n);
@@ -186,6 +237,7 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_
     if (!p.qt) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+        __builtin_amdgcn_sched_barrier(0);
         const Cut<FORMAT> cut(col[e]);
         *(u32x2*)(turned + (cg + e) * PITCH + rg) =
             u32x2{cut.four(v[0][e], v[1][e], v[2][e], v[3][e]), cut.four(v[4][e], v[5][e], v[6][e], v[7][e])};
@@ -202,24 +254,33 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_
     }
 }
 
-template <class T, int FORMAT>
+template <class T, int FORMAT, bool WHOLE>
 hipError_t launch(const QuantizeParams& p, bool square, hipStream_t stream)
 {
     const int64_t nb = (p.cols + FP8_BLOCK - 1) / FP8_BLOCK, mb = (p.rows + FP8_BLOCK - 1) / FP8_BLOCK;
     if (!square && !p.qt && (p.cs == 1 || p.cols <= 1)) {
         const int64_t across = (nb + BLOCKS - 1) / BLOCKS, down = (p.rows + 15) / 16;
         if (across > 0xffffff / down) return hipErrorInvalidConfiguration;
-        hipLaunchKernelGGL((k_quantize_rows<T, FORMAT>), dim3((unsigned)(across * down)), dim3(256), 0, stream, p,
-                           (uint32_t)across);
+        hipLaunchKernelGGL((k_quantize_rows<T, FORMAT, WHOLE>), dim3((unsigned)(across * down)), dim3(256), 0, stream,
+                           p, (uint32_t)across);
         return hipGetLastError();
     }
     if (nb > 0xffffff / mb) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)(nb * mb));
     if (square)
-        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, true>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
+        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, true, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
     else
-        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, false>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
+        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, false, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
     return hipGetLastError();
+}
+
+// (rows that end amid eight neighbours: 32,768 x 1,021 and its transpose 61 us by
+// element, so 46 us; its bounds cost whole blocks 5%)
+template <class T, int FORMAT>
+hipError_t launch(const QuantizeParams& p, bool square, hipStream_t stream)
+{
+    return p.cs == 1 && p.cols % FP8_BLOCK == 0 ? launch<T, FORMAT, true>(p, square, stream)
+                                                : launch<T, FORMAT, false>(p, square, stream);
 }
 
 template <class T>

@@ -52,6 +52,61 @@ __device__ __forceinline__ void get(Held<T, E>& r, const T* row, int lane, int n
     }
 }
 
+// The same, of rows of at least 8, in two steps without a wait between them: fetch() has the thread at a row's
+// end load the eight elements that end there, settle() moves them down to their
+// places (zeros behind).  By element, each of the seven is a load of its own that is
+// waited for: 48,000 x 1,021 forward 188 us, so 104 us (two-byte numbers).
+template <int G, int V, bool TAIL, class T, int E>
+__device__ __forceinline__ void fetch(Held<T, E>& r, const T* row, int lane, int n)
+{
+    if constexpr (!TAIL) {
+        get<G, V, TAIL>(r, row, lane, n);
+    } else {
+#pragma unroll
+        for (int c = 0; c < E / V; ++c) {
+            typedef T Piece __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+            const Piece t = *(const Piece*)(row + min((c * G + lane) * V, n - V));
+#pragma unroll
+            for (int i = 0; i < V; ++i) r.v[c * V + i] = t[i];
+        }
+    }
+}
+
+// words w, moved down by so many bytes (whole elements of SIZE; zeros behind)
+template <int SIZE, int WORDS>
+__device__ __forceinline__ void move_down(uint32_t* w, uint32_t bytes)
+{
+    if constexpr (SIZE < 4)
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i)
+            w[i] = __builtin_amdgcn_alignbyte(i + 1 < WORDS ? w[i + 1] : 0u, w[i], bytes & (4 - SIZE));
+#pragma unroll
+    for (int d = 1; d <= WORDS; d *= 2)
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const uint32_t from = i + d < WORDS ? w[i + d] : 0u;
+            w[i] = bytes & (4 * d) ? from : w[i];
+        }
+}
+
+template <int G, int V, bool TAIL, class T, int E>
+__device__ __forceinline__ void settle(Held<T, E>& r, int lane, int n)
+{
+    if constexpr (TAIL) {
+        static_assert(V == 8, "");
+#pragma unroll
+        for (int c = 0; c < E / V; ++c) {
+            const int by = (c * G + lane) * V - (n - V);   // places to move, from 8 on: none is left
+            if (__builtin_amdgcn_ballot_w64(by > 0) == 0) continue;
+            // (in words: single halves would take a register each)
+            uint32_t w[V * sizeof(T) / 4];
+            __builtin_memcpy(w, r.v + c * V, sizeof w);
+            move_down<sizeof(T), V * sizeof(T) / 4>(w, by <= 0 ? 0 : by >= V ? V * sizeof(T) : by * sizeof(T));
+            __builtin_memcpy(r.v + c * V, w, sizeof w);
+        }
+    }
+}
+
 template <int G, int V, bool TAIL, int E, class T>
 __device__ __forceinline__ void put(T* row, int lane, int n, const float* v)
 {
