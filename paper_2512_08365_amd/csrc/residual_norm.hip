@@ -6,7 +6,8 @@
 // reads four matrices and writes two.  Every row is read once into the registers of
 // 64 to 1,024 threads, 8 elements each (of rows above 8,192 16), the next one while the
 // present one's sums are taken.  Workgroups walk neighbouring rows, so that a
-// gate that many rows share is read once for them.
+// gate that many rows share is read once for them.  Of a copy's 5.1 TB/s: 32,768 x
+// 4,096 forward 5.0, backward 4.7; backward above 8,192 in two passes, 2.2 to 3.3.
 //
 // Sums over a row and over rows, statistics and gradients are fp32; the stream's sum
 // is rounded to its type before the norm behind it reads it, as a reader of the
@@ -21,6 +22,7 @@ namespace mag {
 namespace {
 
 constexpr int64_t MOST_HELD = 16384;   // width of a row that 1,024 threads hold
+constexpr int64_t MOST_SUMMED = 8192;  // ... with its columns' sums
 constexpr int VECTORS = 5;             // of partial sums
 
 // a vector's elements of this thread (ones or zeros: of one that is not there)
@@ -28,7 +30,10 @@ template <class W, int G, int V, bool TAIL, int E>
 __device__ __forceinline__ void vector(float* to, const void* p, int lane, int n, float missing)
 {
     Held<W, E> a{};
-    if (p) get<G, V, TAIL>(a, static_cast<const W*>(p), lane, n);
+    if (p) {
+        fetch<G, V, TAIL>(a, static_cast<const W*>(p), lane, n);
+        settle<G, V, TAIL>(a, lane, n);
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) to[e] = p ? (float)a.v[e] : missing;
 }
@@ -109,8 +114,8 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
     }
     Held<T, E> nh{}, ny{};
     auto load = [&](int64_t i) {
-        get<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
-        get<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
+        fetch<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
+        fetch<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
     };
     if (from + sub < to) load(from + sub);
     int64_t group = -1, group_end = 0;
@@ -124,6 +129,8 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
             gate_of<T, G, V, TAIL, E>(gate, p, group, lane);
         }
         float v[E], y[E], mean, rstd, post_mean, post_rstd;
+        settle<G, V, TAIL>(nh, lane, n);
+        settle<G, V, TAIL>(ny, lane, n);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             v[e] = (float)nh.v[e];
@@ -180,36 +187,56 @@ struct Mine {
 };
 
 // g = dr + rstd (dn w - m1 - hh m2), dy = post ? post_rstd (d pw - m3 - yn m4) : d with d =
-// scale gate g.  Each workgroup keeps its columns' sums over the rows, of a group
-// (g yn and g, from which the gate's and the post norm's gradients follow) and of all
-// its rows; they meet at the end of a group, or in the partial sums.
-template <class T, class W, int G, int E, int V, bool TAIL, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
+// scale gate g.  Each workgroup keeps its columns' sums over the rows in registers, of a
+// group (g yn and g, from which the gate's and the post norm's gradients follow) and
+// of all its rows; they meet at the end of a group, or in the partial sums.
+//
+// From 512 threads on, what a column has beside them lies in LDS, so that 128 registers do
+// and two workgroups of 512 fit a CU: 32,768 x 4,096 with 184 registers 427 us, so 335 us.
+// Smaller workgroups have registers for it (24,414 x 2,048 by LDS 136 us, so 129 us).
+template <class T, class W, int G, int V, bool TAIL, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) void k_residual_norm_back(ResidualNorm p)
 {
-    constexpr int ROWS = THREADS / G;
-    constexpr bool KEEP = E == 8;
+    constexpr int ROWS = THREADS / G, E = 8;
+    static_assert(ROWS == 1 || THREADS == 256, "");
     __shared__ float2 lds[2][THREADS / 64];
     __shared__ float sums[ROWS == 1 ? 1 : G * E];
+    // the weight, scale gate pw, and what the post norm's weight and bias have so far:
+    // a thread's columns by four
+    enum { WEIGHT, GATE, DPOST, DPOST_BIAS };
+    __shared__ __attribute__((aligned(16))) float column_lds[4][2][G][4];
+    constexpr bool HELD = THREADS == 256;
+    float w[HELD ? E : 1], gate[HELD ? E : 1];
     int turn = 0;
     const int lane = threadIdx.x % G, n = (int)p.N;
     const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x / G);
-    const Mine mine(p, blockIdx.x);
-    float w[E], pw[E], pb[E], gate[E];
-    auto vectors = [&] {
-        vector<W, G, V, TAIL, E>(w, p.weight, lane, n, 1.0f);
-        vector<W, G, V, TAIL, E>(pw, p.post_weight, lane, n, 1.0f);
+    auto to_lds = [&](int what, const float* v) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) column_lds[what][e / 4][lane][e % 4] = v[e];
     };
-    if constexpr (KEEP) {
-        vectors();
-        vector<W, G, V, TAIL, E>(pb, p.post_bias, lane, n, 0.0f);
+    auto weight_of = [&](int e) { return HELD ? w[HELD ? e : 0] : column_lds[WEIGHT][e / 4][lane][e % 4]; };
+    auto gate_of_column = [&](int e) { return HELD ? gate[HELD ? e : 0] : column_lds[GATE][e / 4][lane][e % 4]; };
+    const Mine mine(p, blockIdx.x);
+    float v[E];
+    vector<W, G, V, TAIL, E>(v, p.weight, lane, n, 1.0f);
+    if constexpr (HELD)
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e] = v[e];
+    else
+        to_lds(WEIGHT, v);
+    if (sub == 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = 0.0f;
+        to_lds(DPOST, v);
+        to_lds(DPOST_BIAS, v);
     }
-    float dw[E] = {}, db[E] = {}, dpw[E] = {}, dpb[E] = {}, s1[E] = {}, s2[E] = {};
+    float dw[E] = {}, db[E] = {}, s1[E] = {}, s2[E] = {};
     Held<T, E> nh{}, ny{}, nn{}, nr{};
     auto load = [&](int64_t i) {
-        get<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
-        get<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
-        get<G, V, TAIL>(nn, static_cast<const T*>(p.dn.p) + i * p.dn.rs, lane, n);
-        if (p.dr.p) get<G, V, TAIL>(nr, static_cast<const T*>(p.dr.p) + i * p.dr.rs, lane, n);
+        fetch<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
+        fetch<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
+        fetch<G, V, TAIL>(nn, static_cast<const T*>(p.dn.p) + i * p.dn.rs, lane, n);
+        if (p.dr.p) fetch<G, V, TAIL>(nr, static_cast<const T*>(p.dr.p) + i * p.dr.rs, lane, n);
     };
     // the sums of all threads of a column, in the first row's threads (a fixed order)
     auto over_rows = [&](float* v) {
@@ -228,10 +255,21 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
             }
         }
     };
+    float* const part = p.part + (int64_t)blockIdx.x * VECTORS * n;
     if (mine.begin + sub < mine.end) load(mine.begin + sub);
     int64_t begin = mine.begin, end = mine.end;
     for (int64_t group = mine.first; group < mine.last; ++group, begin = end, end += p.length) {
-        gate_of<T, G, V, TAIL, E>(gate, p, group, lane);
+        gate_of<T, G, V, TAIL, E>(v, p, group, lane);
+        {
+            float pw[E];
+            vector<W, G, V, TAIL, E>(pw, p.post ? p.post_weight : nullptr, lane, n, 1.0f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                v[e] *= pw[e];
+                if constexpr (HELD) gate[e] = v[e];
+            }
+        }
+        if constexpr (!HELD) to_lds(GATE, v);
         for (int64_t base = begin; base < end; base += ROWS) {
             const int64_t i = base + sub;
             const bool on = i < end;
@@ -239,7 +277,10 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
             const float post_mean = on && p.post && !p.rms ? p.post_mean[i] : 0.0f;
             const float post_rstd = on && p.post ? p.post_rstd[i] : 0.0f;
             float hh[E], t[E], g[E], yn[E], m1 = 0.0f, m2 = 0.0f;
-            if constexpr (!KEEP) vectors();
+            settle<G, V, TAIL>(nh, lane, n);
+            settle<G, V, TAIL>(ny, lane, n);
+            settle<G, V, TAIL>(nn, lane, n);
+            if (p.dr.p) settle<G, V, TAIL>(nr, lane, n);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 // (beyond the width, and for a row beyond the last: 0)
@@ -248,7 +289,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
                 const float d = in ? (float)nn.v[e] : 0.0f;
                 dw[e] = fmaf(d, hh[e], dw[e]);
                 db[e] += d;
-                t[e] = d * w[e];
+                t[e] = d * weight_of(e);
                 m1 += t[e];
                 m2 = fmaf(t[e], hh[e], m2);
                 g[e] = in && p.dr.p ? (float)nr.v[e] : 0.0f;
@@ -272,11 +313,10 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
             }
             if (on && p.out) put<G, V, TAIL, E>(static_cast<T*>(p.out) + i * p.out_ld, lane, n, g);
 #pragma unroll
-            for (int e = 0; e < E; ++e) g[e] *= gate[e];
+            for (int e = 0; e < E; ++e) g[e] *= gate_of_column(e);
             if (p.post) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    g[e] *= pw[e];
                     m3 += g[e];
                     m4 = fmaf(g[e], yn[e], m4);
                 }
@@ -290,31 +330,39 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
         }
         // the group's sums: the gate's gradient is scale (pw s1 + pb s2), the post norm's
         // weights' are scale gate s1 and scale gate s2
-        if constexpr (!KEEP) {
-            vectors();
-            vector<W, G, V, TAIL, E>(pb, p.post_bias, lane, n, 0.0f);
-        }
+        over_rows(s1);
+        over_rows(s2);
+        if (sub == 0) {
+            gate_of<T, G, V, TAIL, E>(v, p, group, lane);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            dpw[e] = fmaf(gate[e], s1[e], dpw[e]);
-            dpb[e] = fmaf(gate[e], s2[e], dpb[e]);
-            s1[e] = p.scale * (p.post ? fmaf(pw[e], s1[e], pb[e] * s2[e]) : s1[e]);
-            s2[e] = 0.0f;
-        }
-        if (p.chunks) continue;   // (one group, its gate's partial sums in s1)
-        if (p.d_gate) {
-            over_rows(s1);
-            if (sub == 0) {
-                if (p.gate_f32)
+            for (int e = 0; e < E; ++e) {
+                float& dpost = column_lds[DPOST][e / 4][lane][e % 4];
+                float& dpost_bias = column_lds[DPOST_BIAS][e / 4][lane][e % 4];
+                dpost = fmaf(v[e], s1[e], dpost);
+                dpost_bias = fmaf(v[e], s2[e], dpost_bias);
+            }
+            if (p.d_gate) {
+                if (p.post) {
+                    vector<W, G, V, TAIL, E>(v, p.post_weight, lane, n, 1.0f);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s1[e] *= v[e];
+                    vector<W, G, V, TAIL, E>(v, p.post_bias, lane, n, 0.0f);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s1[e] = fmaf(v[e], s2[e], s1[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) s1[e] *= p.scale;
+                if (p.chunks)   // (one group, its gate's partial sums)
+                    put<G, V, TAIL, E>(part + (int64_t)(VECTORS - 1) * n, lane, n, s1);
+                else if (p.gate_f32)
                     put<G, V, TAIL, E>(static_cast<float*>(p.d_gate) + group * p.d_gate_ld, lane, n, s1);
                 else
                     put<G, V, TAIL, E>(static_cast<T*>(p.d_gate) + group * p.d_gate_ld, lane, n, s1);
             }
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e) s1[e] = 0.0f;
+        for (int e = 0; e < E; ++e) s1[e] = s2[e] = 0.0f;
     }
-    float* part = p.part + (int64_t)blockIdx.x * VECTORS * n;
     auto leave = [&](bool wanted, float* v, int at) {
         if (!wanted) return;
         over_rows(v);
@@ -322,20 +370,183 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm_back(ResidualNorm p)
     };
     leave(p.dweight, dw, 0);
     leave(p.dbias, db, 1);
-    leave(p.dpost_weight, dpw, 2);
-    leave(p.dpost_bias, dpb, 3);
-    leave(p.d_gate && p.chunks, s1, 4);
+    if (sub) return;
+    for (int what : {DPOST, DPOST_BIAS}) {
+        if (!(what == DPOST ? p.dpost_weight : p.dpost_bias)) continue;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = column_lds[what][e / 4][lane][e % 4];
+        put<G, V, TAIL, E>(part + (int64_t)(what - DPOST + 2) * n, lane, n, v);
+    }
 }
 
-// The workgroups' sums added up: 16 columns a workgroup, 64 threads each that have
-// all of their loads in flight.  blockIdx.y: a vector's sums over all parts, or from
-// the fifth on a group's gate over its chunks.
+// Rows above 8,192: a workgroup's registers hold one row, and not its columns' sums
+// (with both, 1,024 threads with 128 registers each, 3,051 x 16,384 took 720 us).  So the
+// means of a row's elements come first...
+template <class T, class W, int V, bool TAIL>
+__global__ __launch_bounds__(1024) void k_residual_norm_back_sums(ResidualNorm p)
+{
+    constexpr int G = 1024, E = 16;
+    __shared__ float2 lds[2][16];
+    int turn = 0;
+    const int lane = threadIdx.x, n = (int)p.N;
+    for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
+        const int64_t group = i / p.length;
+        Held<T, E> nh{}, ny{}, nn{}, nr{};
+        Held<W, E> w{};
+        fetch<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
+        fetch<G, V, TAIL>(nn, static_cast<const T*>(p.dn.p) + i * p.dn.rs, lane, n);
+        if (p.weight) fetch<G, V, TAIL>(w, static_cast<const W*>(p.weight), lane, n);
+        if (p.post) {
+            fetch<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
+            if (p.dr.p) fetch<G, V, TAIL>(nr, static_cast<const T*>(p.dr.p) + i * p.dr.rs, lane, n);
+        }
+        const float mean = p.rms ? 0.0f : p.mean[i], rstd = p.rstd[i];
+        settle<G, V, TAIL>(nh, lane, n);
+        settle<G, V, TAIL>(nn, lane, n);
+        settle<G, V, TAIL>(w, lane, n);
+        float m1 = 0.0f, m2 = 0.0f, m3 = 0.0f, m4 = 0.0f;
+        auto normed = [&](int e) { return column<G, V>(lane, e) < n ? ((float)nh.v[e] - mean) * rstd : 0.0f; };
+        auto above = [&](int e) { return (float)nn.v[e] * (p.weight ? (float)w.v[e] : 1.0f); };
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            m1 += above(e);
+            m2 = fmaf(above(e), normed(e), m2);
+        }
+        row_sums<G>(m1, m2, lds[turn ^= 1]);
+        m1 = p.rms ? 0.0f : m1 / (float)n;
+        m2 /= (float)n;
+        if (p.post) {
+            const float post_mean = p.rms ? 0.0f : p.post_mean[i], post_rstd = p.post_rstd[i];
+            settle<G, V, TAIL>(ny, lane, n);
+            settle<G, V, TAIL>(nr, lane, n);
+            float g[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] = fmaf(rstd, above(e) - m1 - normed(e) * m2, (float)nr.v[e]);
+            float by[E];
+            gate_of<T, G, V, TAIL, E>(by, p, group, lane);
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] *= by[e];
+            vector<W, G, V, TAIL, E>(by, p.post_weight, lane, n, 1.0f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool in = column<G, V>(lane, e) < n;
+                const float d = in ? g[e] * by[e] : 0.0f;
+                m3 += d;
+                m4 = fmaf(d, in ? ((float)ny.v[e] - post_mean) * post_rstd : 0.0f, m4);
+            }
+            row_sums<G>(m3, m4, lds[turn ^= 1]);
+            m3 = p.rms ? 0.0f : m3 / (float)n;
+            m4 /= (float)n;
+        }
+        if (lane == 0) {
+            float* m = p.rows + i * 4;
+            m[0] = m1, m[1] = m2, m[2] = m3, m[3] = m4;
+        }
+    }
+}
+
+// ... and with them every element stands for itself: 2,048 columns a workgroup, which
+// walks rows, sums up and writes over what it alone has read.
+template <class T, class W, int V, bool TAIL>
+__global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
+{
+    constexpr int G = 256, E = 8;
+    // (in vectors, lanes are counted through all workgroups: a row's last eight are whole)
+    const int64_t c0 = V == 8 ? 0 : (int64_t)blockIdx.x * (G * E);
+    const int lane = (int)threadIdx.x + (V == 8 ? (int)blockIdx.x * G : 0), n = (int)(p.N - c0);
+    const Mine mine(p, blockIdx.y);
+    auto columns_of = [&](const void* v) { return v ? static_cast<const W*>(v) + c0 : nullptr; };
+    float w[E], pw[E], gate[E];
+    vector<W, G, V, TAIL, E>(w, columns_of(p.weight), lane, n, 1.0f);
+    vector<W, G, V, TAIL, E>(pw, columns_of(p.post ? p.post_weight : nullptr), lane, n, 1.0f);
+    float dw[E] = {}, db[E] = {}, dpw[E] = {}, dpb[E] = {}, s1[E] = {}, s2[E] = {};
+    Held<T, E> nh{}, ny{}, nn{}, nr{};
+    auto load = [&](int64_t i) {
+        fetch<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs + c0, lane, n);
+        fetch<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs + c0, lane, n);
+        fetch<G, V, TAIL>(nn, static_cast<const T*>(p.dn.p) + i * p.dn.rs + c0, lane, n);
+        if (p.dr.p) fetch<G, V, TAIL>(nr, static_cast<const T*>(p.dr.p) + i * p.dr.rs + c0, lane, n);
+    };
+    float* const part = p.part + (int64_t)blockIdx.y * VECTORS * p.N + c0;
+    int64_t begin = mine.begin, end = mine.end;
+    const int64_t last = p.chunks ? end : mine.last * p.length;
+    if (begin < last) load(begin);
+    for (int64_t group = mine.first; group < mine.last; ++group, begin = end, end += p.length) {
+        ResidualNorm q{};
+        q.gate = p.gate ? (const char*)p.gate + c0 * (p.gate_f32 ? 4 : sizeof(T)) : nullptr;
+        q.gate_ld = p.gate_ld;
+        q.gate_f32 = p.gate_f32;
+        q.scale = p.scale;
+        q.N = n;
+        gate_of<T, G, V, TAIL, E>(gate, q, group, lane);
+        for (int64_t i = begin; i < end; ++i) {
+            const float mean = p.rms ? 0.0f : p.mean[i], rstd = p.rstd[i];
+            const float post_mean = p.post && !p.rms ? p.post_mean[i] : 0.0f;
+            const float post_rstd = p.post ? p.post_rstd[i] : 1.0f;
+            const float* m = p.rows + i * 4;
+            const float m1 = m[0], m2 = m[1], m3 = m[2], m4 = m[3];
+            settle<G, V, TAIL>(nh, lane, n);
+            settle<G, V, TAIL>(ny, lane, n);
+            settle<G, V, TAIL>(nn, lane, n);
+            if (p.dr.p) settle<G, V, TAIL>(nr, lane, n);
+            float g[E], yn[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float hh = ((float)nh.v[e] - mean) * rstd, d = (float)nn.v[e];
+                dw[e] = fmaf(d, hh, dw[e]);
+                db[e] += d;
+                g[e] = fmaf(rstd, d * w[e] - m1 - hh * m2, p.dr.p ? (float)nr.v[e] : 0.0f);
+                yn[e] = p.post ? ((float)ny.v[e] - post_mean) * post_rstd : (float)ny.v[e];
+            }
+            if (i + 1 < last) load(i + 1);
+            if (p.out) put<G, V, TAIL, E>(static_cast<T*>(p.out) + i * p.out_ld + c0, lane, n, g);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                s1[e] = fmaf(g[e], yn[e], s1[e]);
+                s2[e] += g[e];
+                g[e] *= gate[e];
+                if (p.post) g[e] = post_rstd * (g[e] * pw[e] - m3 - yn[e] * m4);
+            }
+            if (p.normed) put<G, V, TAIL, E>(static_cast<T*>(p.normed) + i * p.normed_ld + c0, lane, n, g);
+        }
+        float pb[E];
+        vector<W, G, V, TAIL, E>(pb, columns_of(p.post_bias), lane, n, 0.0f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            dpw[e] = fmaf(gate[e], s1[e], dpw[e]);
+            dpb[e] = fmaf(gate[e], s2[e], dpb[e]);
+            s1[e] = p.scale * (p.post ? fmaf(pw[e], s1[e], pb[e] * s2[e]) : s1[e]);
+            s2[e] = 0.0f;
+        }
+        if (p.d_gate) {
+            if (p.chunks)
+                put<G, V, TAIL, E>(part + (VECTORS - 1) * p.N, lane, n, s1);
+            else if (p.gate_f32)
+                put<G, V, TAIL, E>(static_cast<float*>(p.d_gate) + group * p.d_gate_ld + c0, lane, n, s1);
+            else
+                put<G, V, TAIL, E>(static_cast<T*>(p.d_gate) + group * p.d_gate_ld + c0, lane, n, s1);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) s1[e] = 0.0f;
+    }
+    if (p.dweight) put<G, V, TAIL, E>(part, lane, n, dw);
+    if (p.dbias) put<G, V, TAIL, E>(part + p.N, lane, n, db);
+    if (p.dpost_weight) put<G, V, TAIL, E>(part + 2 * p.N, lane, n, dpw);
+    if (p.dpost_bias) put<G, V, TAIL, E>(part + 3 * p.N, lane, n, dpb);
+}
+
+// The workgroups' sums added up: 128 columns a workgroup, by 32 threads of 4 neighbours,
+// 32 times with 8 loads each in flight.  blockIdx.y: a vector's sums over all parts,
+// or from the fifth on a group's gate over its chunks.
 template <class T, class W>
 __global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
 {
-    __shared__ float sums[64][17];
-    const int col = threadIdx.x % 16, row = threadIdx.x / 16;
-    const int64_t j = (int64_t)blockIdx.x * 16 + col, n = p.N;
+    constexpr int U = 8;
+    typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+    __shared__ float sums[32][128];
+    const int lane = threadIdx.x % 32, row = threadIdx.x / 32, n = (int)p.N;
+    const int c0 = (int)blockIdx.x * 128, own = c0 + lane * 4;
+    const int j = max(0, min(own, n - 4));   // (the last thread's four end with the width)
     const int vector = min((int)blockIdx.y, VECTORS - 1);
     void* const of[4] = {p.dweight, p.dbias, p.dpost_weight, p.dpost_bias};
     const int64_t group = (int64_t)blockIdx.y - (VECTORS - 1);
@@ -343,28 +554,39 @@ __global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
     if (!gate && !of[vector & 3]) return;
     const int first = gate ? (int)group * p.chunks : 0, count = gate ? p.chunks : p.parts;
     const float* part = p.part + ((int64_t)first * VECTORS + vector) * n + j;
-    float t[8] = {};
-    if (j < n)
-        for (int k = row; k < count; k += 512)
+    Four t[U] = {};
+    if (own < n && n >= 4) {
+        for (int k = row; k < count; k += 32 * U)
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (k + 64 * u < count) t[u] += part[(int64_t)(k + 64 * u) * VECTORS * n];
-    sums[row][col] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+            for (int u = 0; u < U; ++u)
+                if (k + 32 * u < count) t[u] += *(const Four*)(part + (int64_t)(k + 32 * u) * VECTORS * n);
+    } else if (own < n) {
+        for (int k = row; k < count; k += 32)
+            for (int e = 0; e < n; ++e) t[0][e] += part[(int64_t)k * VECTORS * n + e];
+    }
+#pragma unroll
+    for (int d = U / 2; d > 0; d /= 2)
+#pragma unroll
+        for (int u = 0; u < d; ++u) t[u] += t[u + d];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (j + e >= own && j + e < n) sums[row][j + e - c0] = t[0][e];
     __syncthreads();
-    if (threadIdx.x >= 16 || j >= n) return;
+    const int column = c0 + (int)threadIdx.x;
+    if (threadIdx.x >= 128 || column >= n) return;
     float s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 64; ++k) s += sums[k][col];
+    for (int k = 0; k < 32; ++k) s += sums[k][threadIdx.x];
     if (!gate)
-        static_cast<W*>(of[vector & 3])[j] = (W)s;
+        static_cast<W*>(of[vector & 3])[column] = (W)s;
     else if (p.gate_f32)
-        static_cast<float*>(p.d_gate)[group * p.d_gate_ld + j] = s;
+        static_cast<float*>(p.d_gate)[group * p.d_gate_ld + column] = s;
     else
-        static_cast<T*>(p.d_gate)[group * p.d_gate_ld + j] = (T)s;
+        static_cast<T*>(p.d_gate)[group * p.d_gate_ld + column] = (T)s;
 }
 
 // ------------------------------------------------- rows that no registers hold
-// Too wide, or with elements that are not neighbours: read element by element, two or
+// Too wide or narrow, or with elements that are not neighbours: read element by element, two or
 // three times, the later ones from L2.
 
 template <class T>
@@ -546,9 +768,10 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_wide(ResidualNorm p
 
 bool neighbours(const Strided& m, int64_t n) { return !m.p || n <= 1 || m.cs == 1; }
 
-// threads of a row of width n, and rows that a workgroup takes at a time
-int threads_of(int64_t n) { return n <= 512 ? 64 : n <= 2048 ? 256 : n <= 4096 ? 512 : 1024; }
-int rows_at_once(int64_t n) { return n <= 512 ? 4 : 1; }
+// threads of a row of width n, and rows that a workgroup takes at a time (48,000 x 1,024
+// backward by 256 threads, half of them idle, 168 us, by 128 130 us)
+int threads_of(int64_t n) { return n <= 512 ? 64 : n <= 1024 ? 128 : n <= 2048 ? 256 : n <= 4096 ? 512 : 1024; }
+int rows_at_once(int64_t n) { return n <= 512 ? 4 : n <= 1024 ? 2 : 1; }
 
 template <class T, class W, int V, bool TAIL>
 void forward_held(const ResidualNorm& p, hipStream_t stream)
@@ -559,6 +782,8 @@ void forward_held(const ResidualNorm& p, hipStream_t stream)
     const dim3 grid((unsigned)std::min(rounds, most));
     if (G == 64)
         hipLaunchKernelGGL((k_residual_norm<T, W, 64, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 128)
+        hipLaunchKernelGGL((k_residual_norm<T, W, 128, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 256)
         hipLaunchKernelGGL((k_residual_norm<T, W, 256, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 512)
@@ -574,16 +799,24 @@ void backward_held(const ResidualNorm& p, hipStream_t stream)
 {
     const dim3 grid((unsigned)p.parts);
     const int G = threads_of(p.N);
+    if (p.N > MOST_SUMMED) {
+        if (p.M > 0)
+            hipLaunchKernelGGL((k_residual_norm_back_sums<T, W, V, TAIL>), dim3((unsigned)std::min<int64_t>(p.M, 1024)),
+                               dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back_walk<T, W, V, TAIL>),
+                           dim3((unsigned)((p.N + 2047) / 2048), (unsigned)p.parts), dim3(256), 0, stream, p);
+        return;
+    }
     if (G == 64)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 64, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 64, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+    else if (G == 128)
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 128, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 256)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 256, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 256, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 512)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 512, 8, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
-    else if (p.N <= 8192)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 1024, 8, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 512, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 1024, 16, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, W, 1024, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
 }
 
 // workgroups that walk M rows, one at a time each
@@ -591,7 +824,7 @@ dim3 wide_grid(int64_t M) { return dim3((unsigned)std::min<int64_t>(M, 1 << 16))
 
 bool wide(const ResidualNorm& p)
 {
-    return p.N > MOST_HELD || !neighbours(p.h, p.N) || !neighbours(p.y, p.N) || !neighbours(p.dn, p.N) ||
+    return p.N < 8 || p.N > MOST_HELD || !neighbours(p.h, p.N) || !neighbours(p.y, p.N) || !neighbours(p.dn, p.N) ||
            !neighbours(p.dr, p.N);
 }
 
@@ -630,7 +863,7 @@ hipError_t backward(const ResidualNorm& p, hipStream_t stream)
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (sums) {
         const int64_t jobs = VECTORS - 1 + (p.d_gate && p.chunks ? p.groups : 0);
-        hipLaunchKernelGGL((k_residual_norm_columns<T, W>), dim3((unsigned)((p.N + 15) / 16), (unsigned)jobs),
+        hipLaunchKernelGGL((k_residual_norm_columns<T, W>), dim3((unsigned)((p.N + 127) / 128), (unsigned)jobs),
                            dim3(1024), 0, stream, p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
@@ -647,7 +880,7 @@ RowParts residual_norm_parts(const ResidualNorm& p)
 {
     const bool by_element = wide(p);
     const int64_t rows = by_element ? 1 : rows_at_once(p.N);
-    const int64_t most = !by_element && p.N > 4096 ? 256 : 512;
+    const int64_t most = by_element || p.N <= 4096 ? 512 : p.N <= MOST_SUMMED ? 256 : 128;
     if (p.M == 0) return {1, 0, by_element};
     if (2 * p.groups > most) return {(int)std::min(most, p.groups), 0, by_element};
     const int64_t rounds = (p.length + rows - 1) / rows;
