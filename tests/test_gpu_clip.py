@@ -202,3 +202,13 @@ def test_refusals():
     refused(lambda: mag.clip_gradients([x], 1.0, norm=torch.empty(2, device="cuda")))
     refused(lambda: mag.clip_gradients([x], 1.0, workspace=torch.empty(0, dtype=torch.uint8, device="cuda")), -1)
     assert bool((x == 1).all()) and bool((y == 1).all())
+
+
+def test_clip_past_the_caches():
+    """a list that no cache holds: other stores, and none where nothing is clipped in place"""
+    torch = _torch()
+    for kind in (2, math.inf):
+        for most in (1.0, 1e9):
+            tensors = _tensors(8, [(8192, 4099), (3,), (8192, 4100), (1021, 7)], 0.3)
+            check_clip(tensors, most, kind, out=[torch.full_like(t, 7.0) for t in tensors])
+            check_clip(tensors, most, kind)
