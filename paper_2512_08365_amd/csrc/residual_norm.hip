@@ -77,6 +77,16 @@ __device__ __forceinline__ float centre(float* v, float& mean, bool rms, int lan
     return 1.0f / sqrtf(s / (float)n + eps);
 }
 
+// h + g a in fp32, then in T (for halves the compiler has an instruction that leaves the
+// first step out: another number in 1 of 16,000)
+template <class T>
+__device__ __forceinline__ T stored_sum(float g, float a, float h)
+{
+    float s = fmaf(g, a, h);
+    if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(s));
+    return (T)s;
+}
+
 // rows [from, to) of a workgroup that takes ROWS at a time
 template <int ROWS>
 __device__ __forceinline__ void my_rows(int64_t M, int64_t& from, int64_t& to)
@@ -145,7 +155,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            v[e] = (float)(T)fmaf(gate[e], y[e], v[e]);
+            v[e] = (float)stored_sum<T>(gate[e], y[e], v[e]);
             if (column<G, V>(lane, e) >= n) v[e] = 0.0f;
         }
         if (on) put<G, V, TAIL, E>(static_cast<T*>(p.out) + i * p.out_ld, lane, n, v);
@@ -643,7 +653,7 @@ __global__ __launch_bounds__(1024) void k_residual_norm_wide(ResidualNorm p)
             float y = at<T>(p.y, i, j);
             if (p.post)
                 y = fmaf((y - post_mean) * post_rstd, at<W>(p.post_weight, j, 1.0f), at<W>(p.post_bias, j, 0.0f));
-            out[j] = (T)fmaf(gate_at<T>(p, group, j), y, at<T>(p.h, i, j));
+            out[j] = stored_sum<T>(gate_at<T>(p, group, j), y, at<T>(p.h, i, j));
         }
         // (each thread reads what it wrote itself)
         rstd = centre_wide([&](int64_t j) { return (float)out[j]; }, n, p.rms, p.eps, mean, lds, turn);
