@@ -383,3 +383,37 @@ def test_gradients_of_a_layer():
     along = (dx.double() * step).sum()
     bound = ((8 * V + 7 * 2.0 ** -13 + _u("bf16")) * (e.abs() @ b.abs()) * step.abs()).sum()
     assert abs(float(change - along)) <= float(bound)
+
+
+@pytest.mark.parametrize("inner", [1, 100, 129, 1021, 2100])
+def test_linear_of_many_tiles(inner):
+    """more tiles than CUs, the last ones cut, reductions of one block and of odd lengths"""
+    for i, by_row in enumerate((False, True)):
+        check_linear(8200, inner, 4500, ("bf16", "f16")[i], ACTS[inner % 5], pre=not by_row, whole=True, by_row=by_row,
+                     lx=("plain", "gap16")[i], formats=(("e4m3", "e4m3"), ("e5m2", "e4m3"))[i])
+
+
+def test_linear_split_reductions():
+    """few tiles and long reductions: partial sums and their sum"""
+    for size in ((40, 20000, 70), (300, 30000, 300), (257, 16385, 130)):
+        for by_row in (False, True):
+            check_linear(*size, act="silu", whole=True, by_row=by_row)
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("cols", [8, 9, 15, 120, 127, 1016, 1023])
+def test_quantize_ends_of_rows(cols, ty):
+    """every place at which a row can end amid eight neighbours, what follows it NaN"""
+    import paper_2512_08365_amd as mag
+    torch = _torch()
+    for pitch in (0, 1, 8):
+        y = torch.full((140, cols + pitch), float("nan"), dtype=_dt(ty), device="cuda")
+        y[:, :cols] = _normal(_gen(cols), (140, cols), 1.0, _dt(ty))
+        x = y[:, :cols]
+        for block_rows in (1, BLOCK):
+            q, s, qt, st = mag.quantize_fp8(x, block_rows, transposed=True)
+            _check_cut(x.contiguous(), q, s, block_rows, "e4m3")
+            if block_rows == 1:
+                _check_cut(x.t().contiguous(), qt, st, 1, "e4m3")
+                rows = mag.quantize_fp8(x)
+                assert torch.equal(rows[0].float(), q.float()) and torch.equal(rows[1], s)
