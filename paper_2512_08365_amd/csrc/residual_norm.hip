@@ -545,17 +545,18 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
     if (p.dpost_bias) put<G, V, TAIL, E>(part + 3 * p.N, lane, n, dpb);
 }
 
-// The workgroups' sums added up: 128 columns a workgroup, by 32 threads of 4 neighbours,
-// 32 times with 8 loads each in flight.  blockIdx.y: a vector's sums over all parts,
-// or from the fifth on a group's gate over its chunks.
-template <class T, class W>
+// The workgroups' sums added up: 4 LANES columns a workgroup, by LANES threads of 4
+// neighbours, ROWS times with 8 loads each in flight (widths up to 2,048 by 8 lanes: for
+// 1,021 of them 8 workgroups of 32 lanes a vector took 7.9 us).  blockIdx.y: a vector's
+// sums over all parts, or from the fifth on a group's gate over its chunks.
+template <class T, class W, int LANES>
 __global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
 {
-    constexpr int U = 8;
+    constexpr int U = 8, COLUMNS = 4 * LANES, ROWS = 1024 / LANES;
     typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
-    __shared__ float sums[32][128];
-    const int lane = threadIdx.x % 32, row = threadIdx.x / 32, n = (int)p.N;
-    const int c0 = (int)blockIdx.x * 128, own = c0 + lane * 4;
+    __shared__ float sums[ROWS][COLUMNS], some[ROWS / 4][COLUMNS];
+    const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES, n = (int)p.N;
+    const int c0 = (int)blockIdx.x * COLUMNS, own = c0 + lane * 4;
     const int j = max(0, min(own, n - 4));   // (the last thread's four end with the width)
     const int vector = min((int)blockIdx.y, VECTORS - 1);
     void* const of[4] = {p.dweight, p.dbias, p.dpost_weight, p.dpost_bias};
@@ -566,12 +567,12 @@ __global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
     const float* part = p.part + ((int64_t)first * VECTORS + vector) * n + j;
     Four t[U] = {};
     if (own < n && n >= 4) {
-        for (int k = row; k < count; k += 32 * U)
+        for (int k = row; k < count; k += ROWS * U)
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (k + 32 * u < count) t[u] += *(const Four*)(part + (int64_t)(k + 32 * u) * VECTORS * n);
+                if (k + ROWS * u < count) t[u] += *(const Four*)(part + (int64_t)(k + ROWS * u) * VECTORS * n);
     } else if (own < n) {
-        for (int k = row; k < count; k += 32)
+        for (int k = row; k < count; k += ROWS)
             for (int e = 0; e < n; ++e) t[0][e] += part[(int64_t)k * VECTORS * n + e];
     }
 #pragma unroll
@@ -582,11 +583,16 @@ __global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
     for (int e = 0; e < 4; ++e)
         if (j + e >= own && j + e < n) sums[row][j + e - c0] = t[0][e];
     __syncthreads();
+    {
+        const int c = threadIdx.x % COLUMNS, r = threadIdx.x / COLUMNS;
+        some[r][c] = (sums[4 * r][c] + sums[4 * r + 1][c]) + (sums[4 * r + 2][c] + sums[4 * r + 3][c]);
+    }
+    __syncthreads();
     const int column = c0 + (int)threadIdx.x;
-    if (threadIdx.x >= 128 || column >= n) return;
+    if (threadIdx.x >= COLUMNS || column >= n) return;
     float s = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) s += sums[k][threadIdx.x];
+    for (int k = 0; k < ROWS / 4; ++k) s += some[k][threadIdx.x];
     if (!gate)
         static_cast<W*>(of[vector & 3])[column] = (W)s;
     else if (p.gate_f32)
@@ -875,8 +881,12 @@ hipError_t backward(const ResidualNorm& p, hipStream_t stream)
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (sums) {
         const int64_t jobs = VECTORS - 1 + (p.d_gate && p.chunks ? p.groups : 0);
-        hipLaunchKernelGGL((k_residual_norm_columns<T, W>), dim3((unsigned)((p.N + 127) / 128), (unsigned)jobs),
-                           dim3(1024), 0, stream, p);
+        if (p.N <= 2048)
+            hipLaunchKernelGGL((k_residual_norm_columns<T, W, 8>), dim3((unsigned)((p.N + 31) / 32), (unsigned)jobs),
+                               dim3(1024), 0, stream, p);
+        else
+            hipLaunchKernelGGL((k_residual_norm_columns<T, W, 32>), dim3((unsigned)((p.N + 127) / 128), (unsigned)jobs),
+                               dim3(1024), 0, stream, p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (by_element && p.M > 0 && (p.out || p.normed))
