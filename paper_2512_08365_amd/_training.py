@@ -41,12 +41,20 @@ def _vectors(tensors, dtype, index, width):
     return [0 if x is None else _vector(x, dtype, index, width, name) for name, x in tensors]
 
 
+_NO_STATISTICS = (0, 0, 0, 0)
+
+
 def _statistics(stats, index, rows):
     if stats is None:
-        return [0] * 4
+        return _NO_STATISTICS
     if len(stats) != 4:
         raise MagnetonError(N.MAG_E_SIZE, "statistics must be (mean, rstd, post_mean, post_rstd)")
-    return _vectors(zip(("mean", "rstd", "post_mean", "post_rstd"), stats), torch.float32, index, rows)
+    mean, rstd, post_mean, post_rstd = stats
+    ty = torch.float32
+    return (0 if mean is None else _vector(mean, ty, index, rows, "mean"),
+            0 if rstd is None else _vector(rstd, ty, index, rows, "rstd"),
+            0 if post_mean is None else _vector(post_mean, ty, index, rows, "post_mean"),
+            0 if post_rstd is None else _vector(post_rstd, ty, index, rows, "post_rstd"))
 
 
 def residual_norm(residual, branch, weight=None, bias=None, *, kind="rms", gate=None, scale=1.0,
@@ -77,14 +85,23 @@ def residual_norm(residual, branch, weight=None, bias=None, *, kind="rms", gate=
         layer = k == N.MAG_NORM_LAYER
         statistics = tuple(torch.empty(rows, device=branch.device) if on else None
                            for on in (layer, True, post and layer, post))
-    named = (("weight", weight), ("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias))
-    wdt, wt = _first_dtype(named, (dt, ty))
-    gdt, gt = _first_dtype((("gate", gate),), (dt, ty))
+    # (a decode step calls this at every layer: no loops over what is mostly None)
+    if weight is not None:
+        wdt, wt = _dtype(weight, "weight"), weight.dtype
+    else:
+        wdt, wt = _first_dtype((("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias)),
+                               (dt, ty))
+    gdt, gt = (dt, ty) if gate is None else (_dtype(gate, "gate"), gate.dtype)
     args = N.RESIDUAL_NORM_ARGS.pack(
         dt, wdt, gdt, k, bool(post), 0, *mr, *_matrix(branch, ty, dev, "branch"),
         *_matrix(out[0], ty, dev, "stream"), *_matrix(out[1], ty, dev, "normed"),
-        *_optional(gate, gt, dev, "gate"), *_vectors(named, wt, dev, width),
-        *_statistics(statistics, dev, rows), float(scale), float(eps))
+        *(_NONE if gate is None else _matrix(gate, gt, dev, "gate")),
+        0 if weight is None else _vector(weight, wt, dev, width, "weight"),
+        0 if bias is None else _vector(bias, wt, dev, width, "bias"),
+        0 if post_weight is None else _vector(post_weight, wt, dev, width, "post_weight"),
+        0 if post_bias is None else _vector(post_bias, wt, dev, width, "post_bias"),
+        *(_NO_STATISTICS if statistics is None else _statistics(statistics, dev, rows)),
+        float(scale), float(eps))
     _launch(dev, lib.mag_residual_norm, args)
     return (*out,) if statistics is None else (*out, tuple(statistics))
 
