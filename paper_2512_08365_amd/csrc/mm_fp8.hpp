@@ -321,6 +321,11 @@ __device__ __forceinline__ void walk8(Mm8 p, const Arrays& lds)
     }
 }
 
+template <class T>
+struct Result {
+    using Type = T;
+};
+
 struct Lds8 {
     char *la0, *lb0, *la1, *lb1;
     float *sa0, *sb0, *sa1, *sb1;

@@ -133,7 +133,7 @@ constexpr int BLOCKS = 4;   // of a row, by each 16 lanes
 // blocks of rows whose elements are neighbours: 16 rows by 4 blocks a workgroup (16
 // rows' scales are then neighbours where they lie by columns)
 template <class T, int FORMAT, bool WHOLE>
-__global__ __launch_bounds__(256) void k_quantize_rows(QuantizeParams p, uint32_t across)
+__device__ __forceinline__ void quantize_rows(const QuantizeParams& p, uint32_t across)
 {
     const int64_t r = (int64_t)(blockIdx.x / across) * 16 + threadIdx.x / 16;
     const int64_t b0 = (int64_t)(blockIdx.x % across) * BLOCKS;
@@ -163,12 +163,11 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeParams p, uint32_
 }
 
 // tiles of 128 x 128, of any strides
+constexpr int PITCH = FP8_BLOCK + 8;
 template <class T, int FORMAT, bool SQUARE, bool WHOLE>
-__global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_t across)
+__device__ __forceinline__ void quantize_tile(const QuantizeParams& p, uint32_t across,
+                                              float (&most_lds)[4][FP8_BLOCK], uint8_t* turned)
 {
-    constexpr int PITCH = FP8_BLOCK + 8;
-    __shared__ float most_lds[4][FP8_BLOCK];
-    __shared__ __attribute__((aligned(16))) uint8_t turned[FP8_BLOCK * PITCH];
     const int64_t bi = blockIdx.x / across, bj = blockIdx.x % across;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int rg = threadIdx.x / 16 * 8, cg = threadIdx.x % 16 * 8;   // first of this thread's rows and columns
@@ -254,39 +253,53 @@ __global__ __launch_bounds__(256) void k_quantize_tile(QuantizeParams p, uint32_
     }
 }
 
-template <class T, int FORMAT, bool WHOLE>
-hipError_t launch(const QuantizeParams& p, bool square, hipStream_t stream)
+template <class T, bool WHOLE>
+__global__ __launch_bounds__(256) void k_quantize_rows(QuantizeParams p, uint32_t across, int32_t format)
+{
+    if (format == MAG_E4M3)
+        quantize_rows<T, MAG_E4M3, WHOLE>(p, across);
+    else
+        quantize_rows<T, MAG_E5M2, WHOLE>(p, across);
+}
+
+template <class T, bool SQUARE, bool WHOLE>
+__global__ __launch_bounds__(256, 3) void k_quantize_tile(QuantizeParams p, uint32_t across, int32_t format)
+{
+    __shared__ float most_lds[4][FP8_BLOCK];
+    __shared__ __attribute__((aligned(16))) uint8_t turned[FP8_BLOCK * PITCH];
+    if (format == MAG_E4M3)
+        quantize_tile<T, MAG_E4M3, SQUARE, WHOLE>(p, across, most_lds, turned);
+    else
+        quantize_tile<T, MAG_E5M2, SQUARE, WHOLE>(p, across, most_lds, turned);
+}
+
+template <class T, bool WHOLE>
+hipError_t launch(const QuantizeParams& p, int format, bool square, hipStream_t stream)
 {
     const int64_t nb = (p.cols + FP8_BLOCK - 1) / FP8_BLOCK, mb = (p.rows + FP8_BLOCK - 1) / FP8_BLOCK;
     if (!square && !p.qt && (p.cs == 1 || p.cols <= 1)) {
         const int64_t across = (nb + BLOCKS - 1) / BLOCKS, down = (p.rows + 15) / 16;
         if (across > 0xffffff / down) return hipErrorInvalidConfiguration;
-        hipLaunchKernelGGL((k_quantize_rows<T, FORMAT, WHOLE>), dim3((unsigned)(across * down)), dim3(256), 0, stream,
-                           p, (uint32_t)across);
+        hipLaunchKernelGGL((k_quantize_rows<T, WHOLE>), dim3((unsigned)(across * down)), dim3(256), 0, stream,
+                           p, (uint32_t)across, format);
         return hipGetLastError();
     }
     if (nb > 0xffffff / mb) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)(nb * mb));
     if (square)
-        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, true, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
+        hipLaunchKernelGGL((k_quantize_tile<T, true, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb, format);
     else
-        hipLaunchKernelGGL((k_quantize_tile<T, FORMAT, false, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb);
+        hipLaunchKernelGGL((k_quantize_tile<T, false, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb, format);
     return hipGetLastError();
 }
 
 // (rows that end amid eight neighbours: 32,768 x 1,021 and its transpose 61 us by
 // element, so 46 us; its bounds cost whole blocks 5%)
-template <class T, int FORMAT>
-hipError_t launch(const QuantizeParams& p, bool square, hipStream_t stream)
-{
-    return p.cs == 1 && p.cols % FP8_BLOCK == 0 ? launch<T, FORMAT, true>(p, square, stream)
-                                                : launch<T, FORMAT, false>(p, square, stream);
-}
-
 template <class T>
 hipError_t launch(const QuantizeParams& p, int format, bool square, hipStream_t stream)
 {
-    return format == MAG_E4M3 ? launch<T, MAG_E4M3>(p, square, stream) : launch<T, MAG_E5M2>(p, square, stream);
+    return p.cs == 1 && p.cols % FP8_BLOCK == 0 ? launch<T, true>(p, format, square, stream)
+                                                : launch<T, false>(p, format, square, stream);
 }
 
 __global__ __launch_bounds__(256) void k_pack8(Pack8Params p)

@@ -25,17 +25,35 @@ constexpr int64_t MOST_HELD = 16384;   // width of a row that 1,024 threads hold
 constexpr int64_t MOST_SUMMED = 8192;  // ... with its columns' sums
 constexpr int VECTORS = 5;             // of partial sums
 
-// a vector's elements of this thread (ones or zeros: of one that is not there)
+// v[j], of fp32 or of the rows' type T
+template <class T>
+__device__ __forceinline__ const void* from(const void* v, bool f32, int64_t j)
+{
+    return static_cast<const char*>(v) + j * (f32 ? 4 : (int64_t)sizeof(T));
+}
+
+// A vector's elements of this thread (ones or zeros: of one that is not there).  Weights
+// are fp32 or of the rows' type; which, is looked at once a vector.
 template <class W, int G, int V, bool TAIL, int E>
-__device__ __forceinline__ void vector(float* to, const void* p, int lane, int n, float missing)
+__device__ __forceinline__ void vector_as(float* to, const void* p, int lane, int n)
 {
     Held<W, E> a{};
-    if (p) {
-        fetch<G, V, TAIL>(a, static_cast<const W*>(p), lane, n);
-        settle<G, V, TAIL>(a, lane, n);
-    }
+    fetch<G, V, TAIL>(a, static_cast<const W*>(p), lane, n);
+    settle<G, V, TAIL>(a, lane, n);
 #pragma unroll
-    for (int e = 0; e < E; ++e) to[e] = p ? (float)a.v[e] : missing;
+    for (int e = 0; e < E; ++e) to[e] = (float)a.v[e];
+}
+template <class T, int G, int V, bool TAIL, int E>
+__device__ __forceinline__ void vector(float* to, const void* p, bool f32, int lane, int n, float missing)
+{
+    if (!p) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) to[e] = missing;
+    } else if (sizeof(T) == 4 || f32) {
+        vector_as<float, G, V, TAIL, E>(to, p, lane, n);
+    } else {
+        vector_as<T, G, V, TAIL, E>(to, p, lane, n);
+    }
 }
 
 template <class T, int G, int V, bool TAIL, int E>
@@ -46,10 +64,7 @@ __device__ __forceinline__ void gate_of(float* to, const ResidualNorm& p, int64_
         for (int e = 0; e < E; ++e) to[e] = p.scale;
         return;
     }
-    if (p.gate_f32)
-        vector<float, G, V, TAIL, E>(to, static_cast<const float*>(p.gate) + group * p.gate_ld, lane, (int)p.N, 0.0f);
-    else
-        vector<T, G, V, TAIL, E>(to, static_cast<const T*>(p.gate) + group * p.gate_ld, lane, (int)p.N, 0.0f);
+    vector<T, G, V, TAIL, E>(to, from<T>(p.gate, p.gate_f32, group * p.gate_ld), p.gate_f32, lane, (int)p.N, 0.0f);
 #pragma unroll
     for (int e = 0; e < E; ++e) to[e] *= p.scale;
 }
@@ -96,7 +111,7 @@ __device__ __forceinline__ void my_rows(int64_t M, int64_t& from, int64_t& to)
     to = min(M, rounds * (blockIdx.x + 1) / gridDim.x * ROWS);
 }
 
-template <class T, class W, int G, int E, int V, bool TAIL, int THREADS>
+template <class T, int G, int E, int V, bool TAIL, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
 {
     constexpr int ROWS = THREADS / G;
@@ -111,12 +126,12 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
     my_rows<ROWS>(p.M, from, to);
     float w[E], b[E], pw[E], pb[E], gate[E];
     auto pre_vectors = [&] {
-        vector<W, G, V, TAIL, E>(w, p.weight, lane, n, 1.0f);
-        vector<W, G, V, TAIL, E>(b, p.bias, lane, n, 0.0f);
+        vector<T, G, V, TAIL, E>(w, p.weight, p.weight_f32, lane, n, 1.0f);
+        vector<T, G, V, TAIL, E>(b, p.bias, p.weight_f32, lane, n, 0.0f);
     };
     auto post_vectors = [&] {
-        vector<W, G, V, TAIL, E>(pw, p.post_weight, lane, n, 1.0f);
-        vector<W, G, V, TAIL, E>(pb, p.post_bias, lane, n, 0.0f);
+        vector<T, G, V, TAIL, E>(pw, p.post_weight, p.weight_f32, lane, n, 1.0f);
+        vector<T, G, V, TAIL, E>(pb, p.post_bias, p.weight_f32, lane, n, 0.0f);
     };
     if constexpr (KEEP) {
         pre_vectors();
@@ -204,7 +219,7 @@ struct Mine {
 // From 512 threads on, what a column has beside them lies in LDS, so that 128 registers do
 // and two workgroups of 512 fit a CU: 32,768 x 4,096 with 184 registers 427 us, so 335 us.
 // Smaller workgroups have registers for it (24,414 x 2,048 by LDS 136 us, so 129 us).
-template <class T, class W, int G, int V, bool TAIL, int THREADS>
+template <class T, int G, int V, bool TAIL, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) void k_residual_norm_back(ResidualNorm p)
 {
     constexpr int ROWS = THREADS / G, E = 8;
@@ -228,7 +243,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) 
     auto gate_of_column = [&](int e) { return HELD ? gate[HELD ? e : 0] : column_lds[GATE][e / 4][lane][e % 4]; };
     const Mine mine(p, blockIdx.x);
     float v[E];
-    vector<W, G, V, TAIL, E>(v, p.weight, lane, n, 1.0f);
+    vector<T, G, V, TAIL, E>(v, p.weight, p.weight_f32, lane, n, 1.0f);
     if constexpr (HELD)
 #pragma unroll
         for (int e = 0; e < E; ++e) w[e] = v[e];
@@ -272,7 +287,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) 
         gate_of<T, G, V, TAIL, E>(v, p, group, lane);
         {
             float pw[E];
-            vector<W, G, V, TAIL, E>(pw, p.post ? p.post_weight : nullptr, lane, n, 1.0f);
+            vector<T, G, V, TAIL, E>(pw, p.post ? p.post_weight : nullptr, p.weight_f32, lane, n, 1.0f);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 v[e] *= pw[e];
@@ -353,10 +368,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) 
             }
             if (p.d_gate) {
                 if (p.post) {
-                    vector<W, G, V, TAIL, E>(v, p.post_weight, lane, n, 1.0f);
+                    vector<T, G, V, TAIL, E>(v, p.post_weight, p.weight_f32, lane, n, 1.0f);
 #pragma unroll
                     for (int e = 0; e < E; ++e) s1[e] *= v[e];
-                    vector<W, G, V, TAIL, E>(v, p.post_bias, lane, n, 0.0f);
+                    vector<T, G, V, TAIL, E>(v, p.post_bias, p.weight_f32, lane, n, 0.0f);
 #pragma unroll
                     for (int e = 0; e < E; ++e) s1[e] = fmaf(v[e], s2[e], s1[e]);
                 }
@@ -392,7 +407,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) 
 // Rows above 8,192: a workgroup's registers hold one row, and not its columns' sums
 // (with both, 1,024 threads with 128 registers each, 3,051 x 16,384 took 720 us).  So the
 // means of a row's elements come first...
-template <class T, class W, int V, bool TAIL>
+template <class T, int V, bool TAIL>
 __global__ __launch_bounds__(1024) void k_residual_norm_back_sums(ResidualNorm p)
 {
     constexpr int G = 1024, E = 16;
@@ -402,10 +417,9 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_sums(ResidualNorm p
     for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
         const int64_t group = i / p.length;
         Held<T, E> nh{}, ny{}, nn{}, nr{};
-        Held<W, E> w{};
+        float w[E];
         fetch<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
         fetch<G, V, TAIL>(nn, static_cast<const T*>(p.dn.p) + i * p.dn.rs, lane, n);
-        if (p.weight) fetch<G, V, TAIL>(w, static_cast<const W*>(p.weight), lane, n);
         if (p.post) {
             fetch<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
             if (p.dr.p) fetch<G, V, TAIL>(nr, static_cast<const T*>(p.dr.p) + i * p.dr.rs, lane, n);
@@ -413,10 +427,10 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_sums(ResidualNorm p
         const float mean = p.rms ? 0.0f : p.mean[i], rstd = p.rstd[i];
         settle<G, V, TAIL>(nh, lane, n);
         settle<G, V, TAIL>(nn, lane, n);
-        settle<G, V, TAIL>(w, lane, n);
+        vector<T, G, V, TAIL, E>(w, p.weight, p.weight_f32, lane, n, 1.0f);
         float m1 = 0.0f, m2 = 0.0f, m3 = 0.0f, m4 = 0.0f;
         auto normed = [&](int e) { return column<G, V>(lane, e) < n ? ((float)nh.v[e] - mean) * rstd : 0.0f; };
-        auto above = [&](int e) { return (float)nn.v[e] * (p.weight ? (float)w.v[e] : 1.0f); };
+        auto above = [&](int e) { return (float)nn.v[e] * w[e]; };
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             m1 += above(e);
@@ -436,7 +450,7 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_sums(ResidualNorm p
             gate_of<T, G, V, TAIL, E>(by, p, group, lane);
 #pragma unroll
             for (int e = 0; e < E; ++e) g[e] *= by[e];
-            vector<W, G, V, TAIL, E>(by, p.post_weight, lane, n, 1.0f);
+            vector<T, G, V, TAIL, E>(by, p.post_weight, p.weight_f32, lane, n, 1.0f);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const bool in = column<G, V>(lane, e) < n;
@@ -457,7 +471,7 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_sums(ResidualNorm p
 
 // ... and with them every element stands for itself: 2,048 columns a workgroup, which
 // walks rows, sums up and writes over what it alone has read.
-template <class T, class W, int V, bool TAIL>
+template <class T, int V, bool TAIL>
 __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
 {
     constexpr int G = 256, E = 8;
@@ -465,10 +479,10 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
     const int64_t c0 = V == 8 ? 0 : (int64_t)blockIdx.x * (G * E);
     const int lane = (int)threadIdx.x + (V == 8 ? (int)blockIdx.x * G : 0), n = (int)(p.N - c0);
     const Mine mine(p, blockIdx.y);
-    auto columns_of = [&](const void* v) { return v ? static_cast<const W*>(v) + c0 : nullptr; };
+    auto columns_of = [&](const void* v) { return v ? from<T>(v, p.weight_f32, c0) : nullptr; };
     float w[E], pw[E], gate[E];
-    vector<W, G, V, TAIL, E>(w, columns_of(p.weight), lane, n, 1.0f);
-    vector<W, G, V, TAIL, E>(pw, columns_of(p.post ? p.post_weight : nullptr), lane, n, 1.0f);
+    vector<T, G, V, TAIL, E>(w, columns_of(p.weight), p.weight_f32, lane, n, 1.0f);
+    vector<T, G, V, TAIL, E>(pw, columns_of(p.post ? p.post_weight : nullptr), p.weight_f32, lane, n, 1.0f);
     float dw[E] = {}, db[E] = {}, dpw[E] = {}, dpb[E] = {}, s1[E] = {}, s2[E] = {};
     Held<T, E> nh{}, ny{}, nn{}, nr{};
     auto load = [&](int64_t i) {
@@ -483,7 +497,7 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
     if (begin < last) load(begin);
     for (int64_t group = mine.first; group < mine.last; ++group, begin = end, end += p.length) {
         ResidualNorm q{};
-        q.gate = p.gate ? (const char*)p.gate + c0 * (p.gate_f32 ? 4 : sizeof(T)) : nullptr;
+        q.gate = p.gate ? from<T>(p.gate, p.gate_f32, c0) : nullptr;
         q.gate_ld = p.gate_ld;
         q.gate_f32 = p.gate_f32;
         q.scale = p.scale;
@@ -520,7 +534,7 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
             if (p.normed) put<G, V, TAIL, E>(static_cast<T*>(p.normed) + i * p.normed_ld + c0, lane, n, g);
         }
         float pb[E];
-        vector<W, G, V, TAIL, E>(pb, columns_of(p.post_bias), lane, n, 0.0f);
+        vector<T, G, V, TAIL, E>(pb, columns_of(p.post_bias), p.weight_f32, lane, n, 0.0f);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             dpw[e] = fmaf(gate[e], s1[e], dpw[e]);
@@ -549,7 +563,7 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
 // neighbours, ROWS times with 8 loads each in flight (widths up to 2,048 by 8 lanes: for
 // 1,021 of them 8 workgroups of 32 lanes a vector took 7.9 us).  blockIdx.y: a vector's
 // sums over all parts, or from the fifth on a group's gate over its chunks.
-template <class T, class W, int LANES>
+template <class T, int LANES>
 __global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
 {
     constexpr int U = 8, COLUMNS = 4 * LANES, ROWS = 1024 / LANES;
@@ -593,12 +607,12 @@ __global__ __launch_bounds__(1024) void k_residual_norm_columns(ResidualNorm p)
     float s = 0.0f;
 #pragma unroll
     for (int k = 0; k < ROWS / 4; ++k) s += some[k][threadIdx.x];
-    if (!gate)
-        static_cast<W*>(of[vector & 3])[column] = (W)s;
-    else if (p.gate_f32)
-        static_cast<float*>(p.d_gate)[group * p.d_gate_ld + column] = s;
+    void* const to = gate ? p.d_gate : of[vector & 3];
+    const int64_t at = gate ? group * p.d_gate_ld + column : column;
+    if (gate ? p.gate_f32 : p.weight_f32)
+        static_cast<float*>(to)[at] = s;
     else
-        static_cast<T*>(p.d_gate)[group * p.d_gate_ld + column] = (T)s;
+        static_cast<T*>(to)[at] = (T)s;
 }
 
 // ------------------------------------------------- rows that no registers hold
@@ -610,10 +624,10 @@ __device__ __forceinline__ float at(const Strided& m, int64_t i, int64_t j)
 {
     return (float)static_cast<const T*>(m.p)[i * m.rs + j * m.cs];
 }
-template <class W>
-__device__ __forceinline__ float at(const void* v, int64_t j, float missing)
+template <class T>
+__device__ __forceinline__ float at(const void* v, bool f32, int64_t j, float missing)
 {
-    return v ? (float)static_cast<const W*>(v)[j] : missing;
+    return !v ? missing : f32 ? static_cast<const float*>(v)[j] : (float)static_cast<const T*>(v)[j];
 }
 template <class T>
 __device__ __forceinline__ float gate_at(const ResidualNorm& p, int64_t group, int64_t j)
@@ -643,7 +657,7 @@ __device__ __forceinline__ float centre_wide(F value, int64_t n, bool rms, float
     return 1.0f / sqrtf(s / (float)n + eps);
 }
 
-template <class T, class W>
+template <class T>
 __global__ __launch_bounds__(1024) void k_residual_norm_wide(ResidualNorm p)
 {
     __shared__ float2 lds[2][16];
@@ -658,14 +672,14 @@ __global__ __launch_bounds__(1024) void k_residual_norm_wide(ResidualNorm p)
         for (int64_t j = threadIdx.x; j < n; j += 1024) {
             float y = at<T>(p.y, i, j);
             if (p.post)
-                y = fmaf((y - post_mean) * post_rstd, at<W>(p.post_weight, j, 1.0f), at<W>(p.post_bias, j, 0.0f));
+                y = fmaf((y - post_mean) * post_rstd, at<T>(p.post_weight, p.weight_f32, j, 1.0f), at<T>(p.post_bias, p.weight_f32, j, 0.0f));
             out[j] = stored_sum<T>(gate_at<T>(p, group, j), y, at<T>(p.h, i, j));
         }
         // (each thread reads what it wrote itself)
         rstd = centre_wide([&](int64_t j) { return (float)out[j]; }, n, p.rms, p.eps, mean, lds, turn);
         for (int64_t j = threadIdx.x; j < n; j += 1024)
             static_cast<T*>(p.normed)[i * p.normed_ld + j] =
-                (T)fmaf(((float)out[j] - mean) * rstd, at<W>(p.weight, j, 1.0f), at<W>(p.bias, j, 0.0f));
+                (T)fmaf(((float)out[j] - mean) * rstd, at<T>(p.weight, p.weight_f32, j, 1.0f), at<T>(p.bias, p.weight_f32, j, 0.0f));
         if (threadIdx.x == 0) {
             if (p.mean) p.mean[i] = mean;
             if (p.rstd) p.rstd[i] = rstd;
@@ -676,7 +690,7 @@ __global__ __launch_bounds__(1024) void k_residual_norm_wide(ResidualNorm p)
 }
 
 // an element's normed row, its stream's gradient and its normed block output
-template <class T, class W>
+template <class T>
 struct Element {
     float hh, dn, g, yn;
     __device__ __forceinline__ Element(const ResidualNorm& p, int64_t i, int64_t j, float m1, float m2)
@@ -684,14 +698,14 @@ struct Element {
         const float rstd = p.rstd[i];
         hh = (at<T>(p.h, i, j) - (p.rms ? 0.0f : p.mean[i])) * rstd;
         dn = at<T>(p.dn, i, j);
-        g = fmaf(rstd, dn * at<W>(p.weight, j, 1.0f) - m1 - hh * m2, p.dr.p ? at<T>(p.dr, i, j) : 0.0f);
+        g = fmaf(rstd, dn * at<T>(p.weight, p.weight_f32, j, 1.0f) - m1 - hh * m2, p.dr.p ? at<T>(p.dr, i, j) : 0.0f);
         yn = at<T>(p.y, i, j);
         if (p.post) yn = (yn - (p.rms ? 0.0f : p.post_mean[i])) * p.post_rstd[i];
     }
 };
 
 // the means that a row's elements need of their neighbours
-template <class T, class W>
+template <class T>
 __global__ __launch_bounds__(1024) void k_residual_norm_back_means(ResidualNorm p)
 {
     __shared__ float2 lds[2][16];
@@ -701,8 +715,8 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_means(ResidualNorm 
         const int64_t group = i / p.length;
         float m1 = 0.0f, m2 = 0.0f, m3 = 0.0f, m4 = 0.0f;
         for (int64_t j = threadIdx.x; j < n; j += 1024) {
-            const Element<T, W> x(p, i, j, 0.0f, 0.0f);
-            const float t = x.dn * at<W>(p.weight, j, 1.0f);
+            const Element<T> x(p, i, j, 0.0f, 0.0f);
+            const float t = x.dn * at<T>(p.weight, p.weight_f32, j, 1.0f);
             m1 += t;
             m2 = fmaf(t, x.hh, m2);
         }
@@ -711,8 +725,8 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_means(ResidualNorm 
         m2 /= (float)n;
         if (p.post) {
             for (int64_t j = threadIdx.x; j < n; j += 1024) {
-                const Element<T, W> x(p, i, j, m1, m2);
-                const float d = x.g * gate_at<T>(p, group, j) * at<W>(p.post_weight, j, 1.0f);
+                const Element<T> x(p, i, j, m1, m2);
+                const float d = x.g * gate_at<T>(p, group, j) * at<T>(p.post_weight, p.weight_f32, j, 1.0f);
                 m3 += d;
                 m4 = fmaf(d, x.yn, m4);
             }
@@ -728,21 +742,21 @@ __global__ __launch_bounds__(1024) void k_residual_norm_back_means(ResidualNorm 
 }
 
 // the sums over the rows, by column...
-template <class T, class W>
+template <class T>
 __global__ __launch_bounds__(256) void k_residual_norm_back_wide_columns(ResidualNorm p)
 {
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x, n = p.N;
     if (j >= n) return;
     for (int64_t part = blockIdx.y; part < p.parts; part += gridDim.y) {
         const Mine mine(p, (uint32_t)part);
-        const float pw = at<W>(p.post_weight, j, 1.0f), pb = at<W>(p.post_bias, j, 0.0f);
+        const float pw = at<T>(p.post_weight, p.weight_f32, j, 1.0f), pb = at<T>(p.post_bias, p.weight_f32, j, 0.0f);
         float dw = 0.0f, db = 0.0f, dpw = 0.0f, dpb = 0.0f, dg = 0.0f;
         int64_t begin = mine.begin, end = mine.end;
         for (int64_t group = mine.first; group < mine.last; ++group, begin = end, end += p.length) {
             const float gate = gate_at<T>(p, group, j);
             float s1 = 0.0f, s2 = 0.0f;
             for (int64_t i = begin; i < end; ++i) {
-                const Element<T, W> x(p, i, j, p.rows[i * 4], p.rows[i * 4 + 1]);
+                const Element<T> x(p, i, j, p.rows[i * 4], p.rows[i * 4 + 1]);
                 dw = fmaf(x.dn, x.hh, dw);
                 db += x.dn;
                 s1 = fmaf(x.g, x.yn, s1);
@@ -764,16 +778,16 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_wide_columns(Residua
 }
 
 // ... and the rows' gradients, after them (they may be written over what was read)
-template <class T, class W>
+template <class T>
 __global__ __launch_bounds__(1024) void k_residual_norm_back_wide(ResidualNorm p)
 {
     for (int64_t i = blockIdx.x; i < p.M; i += gridDim.x) {
         const int64_t group = i / p.length;
         const float* m = p.rows + i * 4;
         for (int64_t j = threadIdx.x; j < p.N; j += 1024) {
-            const Element<T, W> x(p, i, j, m[0], m[1]);
+            const Element<T> x(p, i, j, m[0], m[1]);
             float d = x.g * gate_at<T>(p, group, j);
-            if (p.post) d = p.post_rstd[i] * (d * at<W>(p.post_weight, j, 1.0f) - m[2] - x.yn * m[3]);
+            if (p.post) d = p.post_rstd[i] * (d * at<T>(p.post_weight, p.weight_f32, j, 1.0f) - m[2] - x.yn * m[3]);
             if (p.out) static_cast<T*>(p.out)[i * p.out_ld + j] = (T)x.g;
             if (p.normed) static_cast<T*>(p.normed)[i * p.normed_ld + j] = (T)d;
         }
@@ -789,7 +803,7 @@ bool neighbours(const Strided& m, int64_t n) { return !m.p || n <= 1 || m.cs == 
 int threads_of(int64_t n) { return n <= 512 ? 64 : n <= 1024 ? 128 : n <= 2048 ? 256 : n <= 4096 ? 512 : 1024; }
 int rows_at_once(int64_t n) { return n <= 512 ? 4 : n <= 1024 ? 2 : 1; }
 
-template <class T, class W, int V, bool TAIL>
+template <class T, int V, bool TAIL>
 void forward_held(const ResidualNorm& p, hipStream_t stream)
 {
     const int64_t rounds = (p.M + rows_at_once(p.N) - 1) / rows_at_once(p.N);
@@ -797,20 +811,20 @@ void forward_held(const ResidualNorm& p, hipStream_t stream)
     const int64_t most = G == 1024 ? 512 : G == 512 ? 1024 : 2048;
     const dim3 grid((unsigned)std::min(rounds, most));
     if (G == 64)
-        hipLaunchKernelGGL((k_residual_norm<T, W, 64, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm<T, 64, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 128)
-        hipLaunchKernelGGL((k_residual_norm<T, W, 128, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm<T, 128, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 256)
-        hipLaunchKernelGGL((k_residual_norm<T, W, 256, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm<T, 256, 8, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 512)
-        hipLaunchKernelGGL((k_residual_norm<T, W, 512, 8, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm<T, 512, 8, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else if (p.N <= 8192)
-        hipLaunchKernelGGL((k_residual_norm<T, W, 1024, 8, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm<T, 1024, 8, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
     else
-        hipLaunchKernelGGL((k_residual_norm<T, W, 1024, 16, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm<T, 1024, 16, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
 }
 
-template <class T, class W, int V, bool TAIL>
+template <class T, int V, bool TAIL>
 void backward_held(const ResidualNorm& p, hipStream_t stream)
 {
     const dim3 grid((unsigned)p.parts);
@@ -819,22 +833,22 @@ void backward_held(const ResidualNorm& p, hipStream_t stream)
     const int G = p.length < rows_at_once(p.N) ? 256 : threads_of(p.N);
     if (p.N > MOST_SUMMED) {
         if (p.M > 0)
-            hipLaunchKernelGGL((k_residual_norm_back_sums<T, W, V, TAIL>), dim3((unsigned)std::min<int64_t>(p.M, 1024)),
+            hipLaunchKernelGGL((k_residual_norm_back_sums<T, V, TAIL>), dim3((unsigned)std::min<int64_t>(p.M, 1024)),
                                dim3(1024), 0, stream, p);
-        hipLaunchKernelGGL((k_residual_norm_back_walk<T, W, V, TAIL>),
+        hipLaunchKernelGGL((k_residual_norm_back_walk<T, V, TAIL>),
                            dim3((unsigned)((p.N + 2047) / 2048), (unsigned)p.parts), dim3(256), 0, stream, p);
         return;
     }
     if (G == 64)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 64, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, 64, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 128)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 128, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, 128, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 256)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 256, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, 256, V, TAIL, 256>), grid, dim3(256), 0, stream, p);
     else if (G == 512)
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 512, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, 512, V, TAIL, 512>), grid, dim3(512), 0, stream, p);
     else
-        hipLaunchKernelGGL((k_residual_norm_back<T, W, 1024, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back<T, 1024, V, TAIL, 1024>), grid, dim3(1024), 0, stream, p);
 }
 
 // workgroups that walk M rows, one at a time each
@@ -846,19 +860,19 @@ bool wide(const ResidualNorm& p)
            !neighbours(p.dr, p.N);
 }
 
-template <class T, class W>
+template <class T>
 hipError_t forward(const ResidualNorm& p, hipStream_t stream)
 {
     if (wide(p))
-        hipLaunchKernelGGL((k_residual_norm_wide<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_wide<T>), wide_grid(p.M), dim3(1024), 0, stream, p);
     else if (p.N % 8 == 0)
-        forward_held<T, W, 8, false>(p, stream);
+        forward_held<T, 8, false>(p, stream);
     else
-        forward_held<T, W, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, stream);
+        forward_held<T, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, stream);
     return hipGetLastError();
 }
 
-template <class T, class W>
+template <class T>
 hipError_t backward(const ResidualNorm& p, hipStream_t stream)
 {
     const bool sums = p.dweight || p.dbias || p.dpost_weight || p.dpost_bias || p.d_gate;
@@ -867,30 +881,30 @@ hipError_t backward(const ResidualNorm& p, hipStream_t stream)
     hipError_t e = hipSuccess;
     if (by_element) {
         if (p.M > 0)
-            hipLaunchKernelGGL((k_residual_norm_back_means<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
+            hipLaunchKernelGGL((k_residual_norm_back_means<T>), wide_grid(p.M), dim3(1024), 0, stream, p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         if (sums)
-            hipLaunchKernelGGL((k_residual_norm_back_wide_columns<T, W>),
+            hipLaunchKernelGGL((k_residual_norm_back_wide_columns<T>),
                                dim3((unsigned)((p.N + 255) / 256), (unsigned)std::min(p.parts, 1024)), dim3(256), 0,
                                stream, p);
     } else if (p.N % 8 == 0) {
-        backward_held<T, W, 8, false>(p, stream);
+        backward_held<T, 8, false>(p, stream);
     } else {
-        backward_held<T, W, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, stream);
+        backward_held<T, sizeof(T) == 4 ? 1 : 8, sizeof(T) == 2>(p, stream);
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (sums) {
         const int64_t jobs = VECTORS - 1 + (p.d_gate && p.chunks ? p.groups : 0);
         if (p.N <= 2048)
-            hipLaunchKernelGGL((k_residual_norm_columns<T, W, 8>), dim3((unsigned)((p.N + 31) / 32), (unsigned)jobs),
+            hipLaunchKernelGGL((k_residual_norm_columns<T, 8>), dim3((unsigned)((p.N + 31) / 32), (unsigned)jobs),
                                dim3(1024), 0, stream, p);
         else
-            hipLaunchKernelGGL((k_residual_norm_columns<T, W, 32>), dim3((unsigned)((p.N + 127) / 128), (unsigned)jobs),
+            hipLaunchKernelGGL((k_residual_norm_columns<T, 32>), dim3((unsigned)((p.N + 127) / 128), (unsigned)jobs),
                                dim3(1024), 0, stream, p);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (by_element && p.M > 0 && (p.out || p.normed))
-        hipLaunchKernelGGL((k_residual_norm_back_wide<T, W>), wide_grid(p.M), dim3(1024), 0, stream, p);
+        hipLaunchKernelGGL((k_residual_norm_back_wide<T>), wide_grid(p.M), dim3(1024), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -910,21 +924,17 @@ RowParts residual_norm_parts(const ResidualNorm& p)
     return {(int)(chunks * p.groups), (int)chunks, by_element};
 }
 
-hipError_t launch_residual_norm(const ResidualNorm& p, int dtype, int weight_dtype, hipStream_t stream)
+hipError_t launch_residual_norm(const ResidualNorm& p, int dtype, hipStream_t stream)
 {
     if (p.M == 0) return hipSuccess;
-    const bool full = weight_dtype == MAG_F32;
-    if (dtype == MAG_F32) return forward<float, float>(p, stream);
-    if (dtype == MAG_F16) return full ? forward<f16, float>(p, stream) : forward<f16, f16>(p, stream);
-    return full ? forward<bf16, float>(p, stream) : forward<bf16, bf16>(p, stream);
+    return dtype == MAG_F32 ? forward<float>(p, stream) : dtype == MAG_F16 ? forward<f16>(p, stream) : forward<bf16>(p, stream);
 }
 
-hipError_t launch_residual_norm_backward(const ResidualNorm& p, int dtype, int weight_dtype, hipStream_t stream)
+hipError_t launch_residual_norm_backward(const ResidualNorm& p, int dtype, hipStream_t stream)
 {
-    const bool full = weight_dtype == MAG_F32;
-    if (dtype == MAG_F32) return backward<float, float>(p, stream);
-    if (dtype == MAG_F16) return full ? backward<f16, float>(p, stream) : backward<f16, f16>(p, stream);
-    return full ? backward<bf16, float>(p, stream) : backward<bf16, bf16>(p, stream);
+    return dtype == MAG_F32   ? backward<float>(p, stream)
+           : dtype == MAG_F16 ? backward<f16>(p, stream)
+                              : backward<bf16>(p, stream);
 }
 
 }  // namespace mag

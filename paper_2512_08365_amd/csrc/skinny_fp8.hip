@@ -38,8 +38,8 @@ __device__ __forceinline__ i32x4 in_place(i32x4 v, int k, int K)
     return v;
 }
 
-template <int FA, int FB, bool BY_ROW, class T, int MF, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void k_skinny8(Mm8 p)
+template <int FA, int FB, bool BY_ROW, int MF, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_skinny8(Mm8 p, int32_t half)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int AHEAD = MF == 1 ? 4 : 2;
@@ -122,37 +122,43 @@ __global__ __launch_bounds__(WAVES * 64) void k_skinny8(Mm8 p)
 #pragma unroll
         for (int v = 1; v < WAVES; ++v) s += lds[v * MF * 64 + i];
         const Epilogue& e = p.e;
+        auto store = [&](auto type) __attribute__((always_inline)) {
+            using T = typename decltype(type)::Type;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (n + j >= p.S) break;
-            float z = s[j];
-            if (e.bias) z += (float)static_cast<const T*>(e.bias)[n + j];
-            if (e.pre) static_cast<T*>(e.pre)[m * e.pre_ld + n + j] = (T)z;
-            activate<T, 1>(&z, e.act);
-            if (e.res) z += (float)static_cast<const T*>(e.res)[m * e.res_rs + (n + j) * e.res_cs];
-            static_cast<T*>(e.y)[m * e.y_ld + n + j] = (T)z;
-        }
+            for (int j = 0; j < 4; ++j) {
+                if (n + j >= p.S) break;
+                float z = s[j];
+                if (e.bias) z += (float)static_cast<const T*>(e.bias)[n + j];
+                if (e.pre) static_cast<T*>(e.pre)[m * e.pre_ld + n + j] = (T)z;
+                activate<T, 1>(&z, e.act);
+                if (e.res) z += (float)static_cast<const T*>(e.res)[m * e.res_rs + (n + j) * e.res_cs];
+                static_cast<T*>(e.y)[m * e.y_ld + n + j] = (T)z;
+            }
+        };
+        if (half)
+            store(Result<f16>{});
+        else
+            store(Result<bf16>{});
     }
 #endif
 }
 
-template <int FA, int FB, bool BY_ROW, class T>
-hipError_t launch(const Mm8& p, hipStream_t stream)
+template <int FA, int FB, bool BY_ROW>
+hipError_t launch(const Mm8& p, int dtype, hipStream_t stream)
 {
     const dim3 grid((unsigned)((p.S + 15) / 16)), block(512);
+    const int32_t half = dtype == MAG_F16;
     if (p.R <= 16)
-        hipLaunchKernelGGL((k_skinny8<FA, FB, BY_ROW, T, 1, 8>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_skinny8<FA, FB, BY_ROW, 1, 8>), grid, block, 0, stream, p, half);
     else
-        hipLaunchKernelGGL((k_skinny8<FA, FB, BY_ROW, T, 2, 8>), grid, block, 0, stream, p);
+        hipLaunchKernelGGL((k_skinny8<FA, FB, BY_ROW, 2, 8>), grid, block, 0, stream, p, half);
     return hipGetLastError();
 }
 
 template <int FA, int FB>
 hipError_t launch(const Mm8& p, int dtype, hipStream_t stream)
 {
-    if (p.by_row)
-        return dtype == MAG_F16 ? launch<FA, FB, true, f16>(p, stream) : launch<FA, FB, true, bf16>(p, stream);
-    return dtype == MAG_F16 ? launch<FA, FB, false, f16>(p, stream) : launch<FA, FB, false, bf16>(p, stream);
+    return p.by_row ? launch<FA, FB, true>(p, dtype, stream) : launch<FA, FB, false>(p, dtype, stream);
 }
 
 }  // namespace

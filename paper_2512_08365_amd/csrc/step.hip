@@ -247,6 +247,7 @@ int mag_residual_norm(const mag_residual_norm_args* a, hipStream_t stream)
     take_gate(p, a->gate, a->gate_dtype);
     p.rms = a->kind == MAG_NORM_RMS;
     p.post = a->post;
+    p.weight_f32 = a->weight_dtype == MAG_F32;
     p.weight = a->weight;
     p.bias = a->bias;
     p.post_weight = a->post_weight;
@@ -257,7 +258,7 @@ int mag_residual_norm(const mag_residual_norm_args* a, hipStream_t stream)
     p.post_rstd = a->post_rstd;
     p.scale = (float)a->scale;
     p.eps = (float)a->eps;
-    TRY_HIP(mag::launch_residual_norm(p, a->dtype, a->weight_dtype, stream), "residual_norm launch");
+    TRY_HIP(mag::launch_residual_norm(p, a->dtype, stream), "residual_norm launch");
     return MAG_OK;
 }
 
@@ -315,6 +316,7 @@ int mag_residual_norm_backward(const mag_residual_norm_backward_args* a, void* w
     take_gate(p, a->gate, a->gate_dtype);
     p.rms = !layer;
     p.post = a->post;
+    p.weight_f32 = a->weight_dtype == MAG_F32;
     p.weight = a->weight;
     p.post_weight = a->post_weight;
     p.post_bias = a->post_bias;
@@ -335,7 +337,7 @@ int mag_residual_norm_backward(const mag_residual_norm_backward_args* a, void* w
     Carve c{static_cast<char*>(workspace)};
     p.part = c.take<float>((size_t)p.parts * 5 * (size_t)p.N * 4);
     p.rows = c.take<float>((size_t)p.M * 16);
-    TRY_HIP(mag::launch_residual_norm_backward(p, a->dtype, a->weight_dtype, stream), "residual_norm_backward launch");
+    TRY_HIP(mag::launch_residual_norm_backward(p, a->dtype, stream), "residual_norm_backward launch");
     return MAG_OK;
 }
 

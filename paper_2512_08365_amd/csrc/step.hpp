@@ -19,7 +19,7 @@ struct ResidualNorm {
     int64_t out_ld, normed_ld;
     const void* gate;      // [groups][gate_ld], or NULL: ones
     int64_t gate_ld;
-    int32_t gate_f32;      // gate is fp32, else of the rows' type
+    int32_t gate_f32, weight_f32;   // gate, weights and biases are fp32, else of the rows' type
     int32_t rms, post;
     int64_t M, N, groups, length;   // rows, width; groups of `length` rows
     const void *weight, *bias, *post_weight, *post_bias;   // or NULL
@@ -39,8 +39,8 @@ struct RowParts {
     bool wide;             // rows that no registers hold
 };
 RowParts residual_norm_parts(const ResidualNorm& p);
-hipError_t launch_residual_norm(const ResidualNorm& p, int dtype, int weight_dtype, hipStream_t stream);
-hipError_t launch_residual_norm_backward(const ResidualNorm& p, int dtype, int weight_dtype, hipStream_t stream);
+hipError_t launch_residual_norm(const ResidualNorm& p, int dtype, hipStream_t stream);
+hipError_t launch_residual_norm_backward(const ResidualNorm& p, int dtype, hipStream_t stream);
 
 // A tensor of a list: `count` elements from `in` to `out`, in rows of `cols` that are
 // ld apart (cols 0: neighbours all).
