@@ -5,15 +5,16 @@
 // block's output and writes the new stream and its normed rows, the backward one
 // reads four matrices and writes two.  Every row is read once into the registers of
 // 64 to 1,024 threads, 8 elements each (of rows above 8,192 16), the next one while the
-// present one's sums are taken.  Workgroups walk neighbouring rows, so that a
-// gate that many rows share is read once for them.  Of a copy's 5.1 TB/s: 32,768 x
-// 4,096 forward 5.0, backward 4.7; backward above 8,192 in two passes, 2.2 to 3.3.
+// present one's sums are taken.  A gate that many rows share is read once for a
+// workgroup's rows of it.  Of a copy's 6.2 TB/s: 32,768 x 4,096 forward 5.3, backward 4.7;
+// backward above 8,192 in two passes, 2.2 to 3.3.
 //
 // Sums over a row and over rows, statistics and gradients are fp32; the stream's sum
 // is rounded to its type before the norm behind it reads it, as a reader of the
 // stored rows would.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.hpp"
 #include "step.hpp"
@@ -102,15 +103,6 @@ __device__ __forceinline__ T stored_sum(float g, float a, float h)
     return (T)s;
 }
 
-// rows [from, to) of a workgroup that takes ROWS at a time
-template <int ROWS>
-__device__ __forceinline__ void my_rows(int64_t M, int64_t& from, int64_t& to)
-{
-    const int64_t rounds = (M + ROWS - 1) / ROWS;
-    from = rounds * blockIdx.x / gridDim.x * ROWS;
-    to = min(M, rounds * (blockIdx.x + 1) / gridDim.x * ROWS);
-}
-
 template <class T, int G, int E, int V, bool TAIL, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
 {
@@ -122,8 +114,14 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
     int turn = 0;
     const int lane = threadIdx.x % G, n = (int)p.N;
     const int sub = __builtin_amdgcn_readfirstlane((int)threadIdx.x / G);
-    int64_t from, to;
-    my_rows<ROWS>(p.M, from, to);
+    // Workgroups go through the rows side by side, so that all of them read one stretch of
+    // memory (32,768 x 4,096 by runs of neighbouring rows 218 us, so 204 us); where gates
+    // would change every few rows, each takes a run.
+    const int64_t rounds = (p.M + ROWS - 1) / ROWS;
+    const bool runs = p.groups > 1 && p.length < 8 * (int64_t)gridDim.x * ROWS;
+    const int64_t first = (runs ? rounds * blockIdx.x / gridDim.x : blockIdx.x) * ROWS;
+    const int64_t last = runs ? min(p.M, rounds * (blockIdx.x + 1) / gridDim.x * ROWS) : p.M;
+    const int64_t step = runs ? ROWS : (int64_t)gridDim.x * ROWS;
     float w[E], b[E], pw[E], pb[E], gate[E];
     auto pre_vectors = [&] {
         vector<T, G, V, TAIL, E>(w, p.weight, p.weight_f32, lane, n, 1.0f);
@@ -142,12 +140,12 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
         fetch<G, V, TAIL>(nh, static_cast<const T*>(p.h.p) + i * p.h.rs, lane, n);
         fetch<G, V, TAIL>(ny, static_cast<const T*>(p.y.p) + i * p.y.rs, lane, n);
     };
-    if (from + sub < to) load(from + sub);
+    if (first + sub < last) load(first + sub);
     int64_t group = -1, group_end = 0;
     // (the workgroup's rows go together: its barriers are everybody's)
-    for (int64_t base = from; base < to; base += ROWS) {
+    for (int64_t base = first; base < last; base += step) {
         const int64_t i = base + sub;
-        const bool on = i < to;
+        const bool on = i < last;
         if (on && (!KEEP || i >= group_end)) {
             group = i / p.length;
             group_end = (group + 1) * p.length;
@@ -161,7 +159,7 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
             v[e] = (float)nh.v[e];
             y[e] = (float)ny.v[e];
         }
-        if (i + ROWS < to) load(i + ROWS);
+        if (i + step < last) load(i + step);
         if (p.post) {
             post_rstd = centre<G, V, E>(y, post_mean, p.rms, lane, n, p.eps, lds, turn);
             if constexpr (!KEEP) post_vectors();
@@ -189,24 +187,34 @@ __global__ __launch_bounds__(THREADS) void k_residual_norm(ResidualNorm p)
     }
 }
 
-// The rows of a workgroup of the backward pass: groups [first, last), of each its
-// rows [from, to) (a chunk of one group, or whole groups).
+// The rows of a workgroup of the backward pass, ROWS at a time: whole groups [first,
+// last), or a chunk of one group's, whose workgroups (SIDE) go through it side by side:
+// 24,414 x 2,048 126 us, so 115 us.  From 512 threads on there is no register for a step.
+template <int ROWS, bool SIDE>
 struct Mine {
     int64_t first, last;
-    int64_t begin, end;   // of the first group's rows, chunks only
+    int64_t begin, end;   // of the first group's rows
+    typename std::conditional<SIDE, int64_t, std::integral_constant<int, ROWS>>::type step;
     __device__ __forceinline__ explicit Mine(const ResidualNorm& p, uint32_t part)
     {
         if (p.chunks) {
             first = part / (uint32_t)p.chunks;
             last = first + 1;
             const int64_t c = part % (uint32_t)p.chunks;
-            begin = first * p.length + p.length * c / p.chunks;
-            end = first * p.length + p.length * (c + 1) / p.chunks;
+            if constexpr (SIDE) {
+                begin = first * p.length + c * ROWS;
+                end = (first + 1) * p.length;
+                step = (int64_t)p.chunks * ROWS;
+            } else {
+                begin = first * p.length + p.length * c / p.chunks;
+                end = first * p.length + p.length * (c + 1) / p.chunks;
+            }
         } else {
             first = p.groups * part / p.parts;
             last = p.groups * (part + 1) / p.parts;
             begin = first * p.length;
             end = begin + p.length;
+            if constexpr (SIDE) step = ROWS;
         }
     }
 };
@@ -241,7 +249,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) 
     };
     auto weight_of = [&](int e) { return HELD ? w[HELD ? e : 0] : column_lds[WEIGHT][e / 4][lane][e % 4]; };
     auto gate_of_column = [&](int e) { return HELD ? gate[HELD ? e : 0] : column_lds[GATE][e / 4][lane][e % 4]; };
-    const Mine mine(p, blockIdx.x);
+    const Mine<ROWS, THREADS == 256> mine(p, blockIdx.x);
     float v[E];
     vector<T, G, V, TAIL, E>(v, p.weight, p.weight_f32, lane, n, 1.0f);
     if constexpr (HELD)
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) 
             }
         }
         if constexpr (!HELD) to_lds(GATE, v);
-        for (int64_t base = begin; base < end; base += ROWS) {
+        for (int64_t base = begin; base < end; base += mine.step) {
             const int64_t i = base + sub;
             const bool on = i < end;
             const float mean = on && !p.rms ? p.mean[i] : 0.0f, rstd = on ? p.rstd[i] : 0.0f;
@@ -322,8 +330,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 256 || sizeof(T) == 4 ? 2 : 4) 
                 if (p.post) yn[e] = in ? (yn[e] - post_mean) * post_rstd : 0.0f;
             }
             // the next row: of this group, or the next one's first
-            const int64_t next = min(base + ROWS, end) + sub;
-            const int64_t stop = base + ROWS < end ? end : group + 1 < mine.last ? end + p.length : 0;
+            const int64_t next = min(base + mine.step, end) + sub;
+            const int64_t stop = base + mine.step < end ? end : group + 1 < mine.last ? end + p.length : 0;
             if (next < stop) load(next);
             row_sums<G>(m1, m2, lds[turn ^= 1]);
             m1 = p.rms ? 0.0f : m1 / (float)n;
@@ -478,7 +486,7 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
     // (in vectors, lanes are counted through all workgroups: a row's last eight are whole)
     const int64_t c0 = V == 8 ? 0 : (int64_t)blockIdx.x * (G * E);
     const int lane = (int)threadIdx.x + (V == 8 ? (int)blockIdx.x * G : 0), n = (int)(p.N - c0);
-    const Mine mine(p, blockIdx.y);
+    const Mine<1, true> mine(p, blockIdx.y);
     auto columns_of = [&](const void* v) { return v ? from<T>(v, p.weight_f32, c0) : nullptr; };
     float w[E], pw[E], gate[E];
     vector<T, G, V, TAIL, E>(w, columns_of(p.weight), p.weight_f32, lane, n, 1.0f);
@@ -503,7 +511,7 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
         q.scale = p.scale;
         q.N = n;
         gate_of<T, G, V, TAIL, E>(gate, q, group, lane);
-        for (int64_t i = begin; i < end; ++i) {
+        for (int64_t i = begin; i < end; i += mine.step) {
             const float mean = p.rms ? 0.0f : p.mean[i], rstd = p.rstd[i];
             const float post_mean = p.post && !p.rms ? p.post_mean[i] : 0.0f;
             const float post_rstd = p.post ? p.post_rstd[i] : 1.0f;
@@ -522,7 +530,7 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_walk(ResidualNorm p)
                 g[e] = fmaf(rstd, d * w[e] - m1 - hh * m2, p.dr.p ? (float)nr.v[e] : 0.0f);
                 yn[e] = p.post ? ((float)ny.v[e] - post_mean) * post_rstd : (float)ny.v[e];
             }
-            if (i + 1 < last) load(i + 1);
+            if (i + mine.step < last) load(i + mine.step);
             if (p.out) put<G, V, TAIL, E>(static_cast<T*>(p.out) + i * p.out_ld + c0, lane, n, g);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -748,14 +756,14 @@ __global__ __launch_bounds__(256) void k_residual_norm_back_wide_columns(Residua
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x, n = p.N;
     if (j >= n) return;
     for (int64_t part = blockIdx.y; part < p.parts; part += gridDim.y) {
-        const Mine mine(p, (uint32_t)part);
+        const Mine<1, true> mine(p, (uint32_t)part);
         const float pw = at<T>(p.post_weight, p.weight_f32, j, 1.0f), pb = at<T>(p.post_bias, p.weight_f32, j, 0.0f);
         float dw = 0.0f, db = 0.0f, dpw = 0.0f, dpb = 0.0f, dg = 0.0f;
         int64_t begin = mine.begin, end = mine.end;
         for (int64_t group = mine.first; group < mine.last; ++group, begin = end, end += p.length) {
             const float gate = gate_at<T>(p, group, j);
             float s1 = 0.0f, s2 = 0.0f;
-            for (int64_t i = begin; i < end; ++i) {
+            for (int64_t i = begin; i < end; i += mine.step) {
                 const Element<T> x(p, i, j, p.rows[i * 4], p.rows[i * 4 + 1]);
                 dw = fmaf(x.dn, x.hh, dw);
                 db += x.dn;
