@@ -81,6 +81,8 @@ def residual_norm(residual, branch, weight=None, bias=None, *, kind="rms", gate=
     _, rows, width, _, _ = mr
     if out is None:
         out = tuple(torch.empty(branch.shape, dtype=ty, device=branch.device) for _ in range(2))
+    elif len(out) != 2:
+        raise MagnetonError(N.MAG_E_SIZE, "out must be (stream, normed)")
     if statistics is True:
         layer = k == N.MAG_NORM_LAYER
         statistics = tuple(torch.empty(rows, device=branch.device) if on else None

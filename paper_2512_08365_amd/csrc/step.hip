@@ -44,6 +44,14 @@ int check_same(const mag_matrix& m, const mag_matrix& x, bool out, int dtype)
     return check_data(m, dtype);
 }
 
+// (two outputs that begin together; where they overlap otherwise is not looked at)
+int check_apart(const mag_matrix& a, const mag_matrix& b)
+{
+    if (a.data && a.data == b.data && a.rows > 0 && a.cols > 0)
+        return set_error(MAG_E_SIZE, "two outputs are the same memory");
+    return MAG_OK;
+}
+
 void take_gate(mag::ResidualNorm& p, const mag_matrix& gate, int gate_dtype)
 {
     p.gate = gate.data;
@@ -229,6 +237,7 @@ int mag_residual_norm(const mag_residual_norm_args* a, hipStream_t stream)
     TRY(check_same(a->branch, a->residual, false, a->dtype));
     TRY(check_same(a->out, a->residual, true, a->dtype));
     TRY(check_same(a->normed, a->residual, true, a->dtype));
+    TRY(check_apart(a->out, a->normed));
     if (!(a->eps >= 0.0) || isinf(a->eps)) return set_error(MAG_E_SIZE, "eps must be finite and >= 0");
     if (!isfinite(a->scale)) return set_error(MAG_E_SIZE, "scale must be finite");
     if (!a->post && (a->post_weight || a->post_bias))
@@ -285,6 +294,7 @@ int mag_residual_norm_backward(const mag_residual_norm_backward_args* a, void* w
     if (a->d_out.data) TRY(check_same(a->d_out, x, false, a->dtype));
     if (a->d_residual.data) TRY(check_same(a->d_residual, x, true, a->dtype));
     if (a->d_branch.data) TRY(check_same(a->d_branch, x, true, a->dtype));
+    TRY(check_apart(a->d_residual, a->d_branch));
     if (!isfinite(a->scale)) return set_error(MAG_E_SIZE, "scale must be finite");
     const bool layer = a->kind == MAG_NORM_LAYER;
     if (x.rows > 0 && (!a->rstd || (layer && !a->mean) || (a->post && (!a->post_rstd || (layer && !a->post_mean)))))

@@ -439,3 +439,38 @@ def test_refusals():
     refused(lambda: mag.residual_norm_backward(h, h, h, h, (r, r), w), -2)
     refused(lambda: mag.residual_norm_backward(h, h, h, h, (None, r, None, None), w, workspace=torch.empty(
         8, dtype=torch.uint8, device="cuda")), -4)
+
+
+@pytest.mark.parametrize("size", [(131080, 72), (65540, 700), (32776, 1100), (16392, 2056)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_groups_of_many_rows(size):
+    """samples so long that workgroups go through them side by side"""
+    for groups in (2, "channel"):
+        check_forward(*size, "bf16", kind="layer", groups=groups)
+        check_backward(*size, "bf16", kind="rms", groups=groups)
+
+
+@pytest.mark.parametrize("width", [1, 3, 7, 8, 9, 15, 505, 513, 1023, 1025, 2041, 4089, 8191, 8193, 8199, 10241, 12295])
+def test_ends_of_rows(width):
+    """every place at which a row can end amid eight neighbours, around the widths where kernels
+    change, rows at any element"""
+    for ty in ("bf16", "f32"):
+        for at, lay in enumerate(("plain", "gap", "shifted")):
+            lays = ["plain"] * 4
+            lays[at] = lay
+            check_forward(9, width, ty, ty, KINDS[at % 2], lh=lay, ly="gap", groups=3, wide_out=at)
+            check_backward(9, width, ty, "f32", KINDS[at % 2], lays=lays, groups=(3, "row", "channel")[at])
+
+
+def test_more_refusals():
+    import paper_2512_08365_amd as mag
+    torch = _torch()
+    h, r = torch.zeros((12, 64), device="cuda"), torch.ones(12, device="cuda")
+    out = torch.full((12, 64), 7.0, device="cuda")
+    for call in (lambda: mag.residual_norm(h, h, out=(out, out)), lambda: mag.residual_norm(h, h, out=(out,)),
+                 lambda: mag.residual_norm_backward(h, h, h, h, (None, r, None, None),
+                                                    out=(out, out, None, None, None, None, None))):
+        with pytest.raises(mag.MagnetonError) as e:
+            call()
+        assert e.value.code == -2
+    assert bool((out == 7).all())
