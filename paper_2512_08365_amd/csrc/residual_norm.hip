@@ -837,8 +837,9 @@ void backward_held(const ResidualNorm& p, hipStream_t stream)
 {
     const dim3 grid((unsigned)p.parts);
     // (groups of fewer rows than a workgroup would take at a time: 65,536 x 512 with a gate
-    // for each row 807 us, so 557 us)
-    const int G = p.length < rows_at_once(p.N) ? 256 : threads_of(p.N);
+    // for each row 807 us, so 557 us; a row's columns have a thread each also where there
+    // are no rows, and sums of zero are left)
+    const int G = p.length < rows_at_once(p.N) ? std::max(256, threads_of(p.N)) : threads_of(p.N);
     if (p.N > MOST_SUMMED) {
         if (p.M > 0)
             hipLaunchKernelGGL((k_residual_norm_back_sums<T, V, TAIL>), dim3((unsigned)std::min<int64_t>(p.M, 1024)),

@@ -474,3 +474,26 @@ def test_more_refusals():
             call()
         assert e.value.code == -2
     assert bool((out == 7).all())
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("width", [3, 72, 700, 1500, 2056, 3001, 4096, 5000, 8192, 8200, 16384, 20000])
+def test_gradients_of_no_rows_are_zero(width, ty):
+    """whatever the outputs and the workspace held before"""
+    import paper_2512_08365_amd as mag
+    torch = _torch()
+    for groups in (None, 1, 3, 600):
+        for wt in (ty, "f32"):
+            x = torch.empty((0, width), dtype=_dt(ty), device="cuda")
+            w, gate = torch.ones(width, dtype=_dt(wt), device="cuda"), None
+            if groups:
+                gate = torch.ones((groups, width), dtype=_dt(wt), device="cuda")
+            stats = (torch.empty(0, device="cuda"),) * 4
+            nan = float("nan")
+            out = (x, x, None if gate is None else torch.full_like(gate, nan),
+                   *(torch.full_like(w, nan) for _ in range(4)))
+            ws = torch.full((mag.residual_norm_backward_workspace_size(x, gate) // 4 + 64,), nan, device="cuda")
+            got = mag.residual_norm_backward(x, x, x, x, stats, w, w, kind="layer", gate=gate, post=True, post_weight=w,
+                                             post_bias=w, out=out, workspace=ws)
+            for grad in got[2:]:
+                assert grad is None or bool((grad == 0).all()), (groups, wt)
