@@ -928,7 +928,7 @@ typedef struct mag_linear_fp8_args {
     mag_matrix residual;   /* [rows, out], data NULL: none; may be y itself        */
     mag_matrix pre;        /* output [rows, out], data NULL: none                  */
     mag_matrix y;          /* output [rows, out]                                   */
-    mag_matrix x_scale;    /* floats [rows, ceil(in / 128)], any strides           */
+    mag_matrix x_scale;    /* floats [rows, ceil(in / 128)], strides as said below */
     mag_matrix weight_scale; /* floats [ceil(out / 128), ceil(in / 128)], or a     */
                            /* scale for each output's block: [out, ceil(in / 128)] */
     const void* bias;      /* [out], contiguous, or NULL                           */
@@ -941,6 +941,9 @@ typedef struct mag_linear_fp8_args {
  * products too: of dy's rows and weight^T for x's, of dy's columns and x's columns
  * (both scaled row by row) for weight's, as mag_quantize_fp8 makes them.
  *   workspace_size: of x's and weight's sizes, strides and alignment.
+ * Rows that are packed first (those not of whole 16 bytes and less than 2^23 bytes
+ * apart) are packed at most 2^23 - 128 of the reduction at a time.  Scales of
+ * neighbouring rows are at most 2^22 floats apart.
  * A block's sum is the matrix instruction's: of eight neighbours' products those
  * below 2^-13 of their largest lose what is below that; blocks are added in fp32.
  * Results are therefore of two bytes.

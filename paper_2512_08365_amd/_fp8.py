@@ -121,7 +121,7 @@ def linear_fp8(x, x_scale, weight, weight_scale, bias=None, residual=None, *, ac
     x: [..., in], weight: [out, in], float8_e4m3fn or float8_e5m2, any strides (rows of
     whole 16 bytes are read where they lie).  x_scale: [rows, ceil(in / 128)];
     weight_scale: [ceil(out / 128), ceil(in / 128)], or one for each output's block, [out,
-    ceil(in / 128)]; float32, any strides.  bias: [out], residual: [..., out], of dtype
+    ceil(in / 128)]; float32, rows up to 2^22 values apart.  bias: [out], residual: [..., out], of dtype
     (float16 or bfloat16; out's, where it is given).  activation, pre, out: as in linear();
     residual may be `out` itself.  Returns out, or (out, pre), which carry no gradient.
     """

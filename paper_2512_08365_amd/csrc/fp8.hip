@@ -87,8 +87,11 @@ struct Plan {
     bool pack_x, pack_w;
     int64_t ld_x, ld_w;
     uint8_t *x, *w;
-    int tile, splits;
-    float* partial;
+    // tiles: the reduction in `slabs` launches of `slab` each (the last one what is left)
+    int64_t slab;
+    int slabs;
+    int tile, splits;   // splits: of a slab
+    float* partial;     // of slabs x splits
 };
 
 void choose(int64_t R, int64_t S, int64_t K, Plan& pl)
@@ -124,23 +127,37 @@ size_t plan_linear(const mag_linear_fp8_args* a, void* ws, Plan& pl)
     if (pl.skinny && a->x.cols > 0 && a->x.cols < 16) pl.pack_x = pl.pack_w = true;
     pl.ld_x = pl.pack_x ? packed_ld(a->x.cols) : a->x.rows > 1 ? a->x.row_stride : 0;
     pl.ld_w = pl.pack_w ? packed_ld(a->weight.cols) : a->weight.rows > 1 ? a->weight.row_stride : 0;
-    pl.splits = 1;
-    if (!pl.skinny) choose(a->x.rows, a->weight.rows, a->x.cols, pl);
+    pl.splits = pl.slabs = 1;
+    pl.slab = a->x.cols;
+    if (!pl.skinny) {
+        // Rows whose pitch a tile's offsets do not reach over are packed a part of the
+        // reduction at a time, each in the place of the one before.
+        if ((pl.pack_x && pl.ld_x >= MOST_LD) || (pl.pack_w && pl.ld_w >= MOST_LD)) {
+            constexpr int64_t MOST_SLAB = MOST_LD - MAG_FP8_BLOCK;
+            pl.slabs = (int)((a->x.cols + MOST_SLAB - 1) / MOST_SLAB);
+            pl.slab = blocks_of((a->x.cols + pl.slabs - 1) / pl.slabs) * MAG_FP8_BLOCK;
+            if (pl.pack_x) pl.ld_x = pl.slab;
+            if (pl.pack_w) pl.ld_w = pl.slab;
+        }
+        choose(a->x.rows, a->weight.rows, pl.slab, pl);
+    }
     Carve c{static_cast<char*>(ws)};
     pl.x = pl.pack_x ? c.take<uint8_t>((size_t)(a->x.rows * pl.ld_x)) : static_cast<uint8_t*>(a->x.data);
     pl.w = pl.pack_w ? c.take<uint8_t>((size_t)(a->weight.rows * pl.ld_w)) : static_cast<uint8_t*>(a->weight.data);
-    if (pl.splits > 1) pl.partial = c.take<float>((size_t)(pl.splits * a->x.rows * up8(a->weight.rows) * 4));
+    if (pl.slabs * pl.splits > 1)
+        pl.partial = c.take<float>((size_t)(pl.slabs * pl.splits * a->x.rows * up8(a->weight.rows) * 4));
     return c.off;
 }
 
-int pack(const mag_matrix& m, uint8_t* dst, int64_t ld, hipStream_t stream)
+// columns [from, from + n) of m
+int pack(const mag_matrix& m, int64_t from, int64_t n, uint8_t* dst, int64_t ld, hipStream_t stream)
 {
     mag::Pack8Params p{};
-    p.src = static_cast<const uint8_t*>(m.data);
     p.rs = m.rows > 1 ? m.row_stride : 0;
     p.cs = m.cols > 1 ? m.col_stride : 1;
+    p.src = static_cast<const uint8_t*>(m.data) + from * p.cs;
     p.rows = m.rows;
-    p.cols = m.cols;
+    p.cols = n;
     p.dst = dst;
     p.ld = ld;
     TRY_HIP(mag::launch_pack8(p, stream), "linear_fp8 launch");
@@ -244,23 +261,15 @@ int mag_linear_fp8(const mag_linear_fp8_args* a, void* workspace, size_t workspa
     TRY(check_workspace(workspace, workspace_bytes, plan_linear(a, nullptr, pl)));
     if (M == 0 || N == 0) return MAG_OK;
     plan_linear(a, workspace, pl);
-    if (K > 0 && pl.pack_x) TRY(pack(a->x, pl.x, pl.ld_x, stream));
-    if (K > 0 && pl.pack_w) TRY(pack(a->weight, pl.w, pl.ld_w, stream));
     mag::Mm8 p{};
-    p.a = pl.x;
     p.lda = pl.ld_x;
-    p.b = pl.w;
     p.ldb = pl.ld_w;
     p.R = M;
     p.S = N;
-    p.K = K;
-    p.sa = scales(a->x_scale);
-    p.sb = scales(a->weight_scale);
     p.by_row = by_row;
     p.fa = a->x_format;
     p.fb = a->weight_format;
     p.splits = pl.splits;
-    p.partial = pl.partial;
     p.partial_ld = up8(N);
     p.e.bias = a->bias;
     p.e.act = a->activation;
@@ -272,23 +281,37 @@ int mag_linear_fp8(const mag_linear_fp8_args* a, void* workspace, size_t workspa
     p.e.y = a->y.data;
     p.e.y_ld = a->y.row_stride;
     p.e.vec = !p.e.res || p.e.res_cs == 1;
-    if (pl.skinny) {
-        if (K > 0) p.K = std::max<int64_t>(K, 16);
-        TRY_HIP(mag::launch_skinny8(p, a->dtype, stream), "linear_fp8 launch");
-        return MAG_OK;
+    const int planes = pl.slabs * pl.splits;
+    const int dtype = planes > 1 ? MAG_F32 : a->dtype;
+    for (int i = 0; i < pl.slabs; ++i) {
+        const int64_t from = i * pl.slab;
+        p.K = std::min(pl.slab, K - from);
+        p.a = pl.pack_x ? pl.x : pl.x + from;
+        p.b = pl.pack_w ? pl.w : pl.w + from;
+        p.sa = scales(a->x_scale);
+        p.sb = scales(a->weight_scale);
+        p.sa.p += from / MAG_FP8_BLOCK * p.sa.cs;
+        p.sb.p += from / MAG_FP8_BLOCK * p.sb.cs;
+        if (planes > 1) p.partial = pl.partial + (int64_t)i * pl.splits * M * p.partial_ld;
+        if (K > 0 && pl.pack_x) TRY(pack(a->x, from, p.K, pl.x, pl.ld_x, stream));
+        if (K > 0 && pl.pack_w) TRY(pack(a->weight, from, p.K, pl.w, pl.ld_w, stream));
+        if (pl.skinny) {
+            if (K > 0) p.K = std::max<int64_t>(K, 16);
+            TRY_HIP(mag::launch_skinny8(p, a->dtype, stream), "linear_fp8 launch");
+            return MAG_OK;
+        }
+        TRY_HIP(pl.tile == mag::TILE_256   ? mag::launch_mm8_256(p, dtype, stream)
+                : pl.tile == mag::TILE_128 ? mag::launch_mm8_128(p, dtype, stream)
+                                           : mag::launch_mm8_64(p, dtype, stream),
+                "linear_fp8 launch");
     }
-    const int dtype = pl.splits > 1 ? MAG_F32 : a->dtype;
-    TRY_HIP(pl.tile == mag::TILE_256   ? mag::launch_mm8_256(p, dtype, stream)
-            : pl.tile == mag::TILE_128 ? mag::launch_mm8_128(p, dtype, stream)
-                                       : mag::launch_mm8_64(p, dtype, stream),
-            "linear_fp8 launch");
-    if (pl.splits > 1) {
+    if (planes > 1) {
         mag::Mm j{};
         j.R = M;
         j.S = N;
         j.K = K;
         j.batch = 1;
-        j.splits = pl.splits;
+        j.splits = planes;
         j.partial = pl.partial;
         j.partial_ld = up8(N);
         j.e = p.e;
