@@ -236,7 +236,8 @@ def _list(tensors, out=None):
 
 
 def clip_gradients_workspace_size(tensors) -> int:
-    return _size(_lib().mag_clip_gradients_workspace_size, _list(tensors)._args(2, 0.0, 0.0, None))
+    tensors = _list(tensors)   # (kept: the arguments hold its address)
+    return _size(_lib().mag_clip_gradients_workspace_size, tensors._args(2, 0.0, 0.0, None))
 
 
 def _run(call, tensors, kind, max_norm, eps, norm, workspace):

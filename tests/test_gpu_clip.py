@@ -212,3 +212,14 @@ def test_clip_past_the_caches():
             tensors = _tensors(8, [(8192, 4099), (3,), (8192, 4100), (1021, 7)], 0.3)
             check_clip(tensors, most, kind, out=[torch.full_like(t, 7.0) for t in tensors])
             check_clip(tensors, most, kind)
+
+
+def test_workspace_of_plain_tensors():
+    import paper_2512_08365_amd as mag
+    torch = _torch()
+    for n in (1, 3, 70, 1000):
+        tensors = [torch.ones(k % 50 + 1, device="cuda") for k in range(n)]
+        assert mag.clip_gradients_workspace_size(tensors) == mag.clip_gradients_workspace_size(mag.TensorList(tensors))
+        ws = torch.empty(mag.clip_gradients_workspace_size(tensors), dtype=torch.uint8, device="cuda")
+        want = math.sqrt(sum(t.numel() for t in tensors))
+        assert abs(float(mag.clip_gradients(tensors, 1.0, workspace=ws)) - want) <= 2.0 ** -23 * want

@@ -2,9 +2,15 @@
 device work (no GPU needed)."""
 import ctypes
 import math
+import os
+import subprocess
+import sys
+
+import pytest
 
 from test_block_abi import FAKE, NONE, _mat, _n
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 H = _mat(12, 64)
 OTHER = _mat(12, 64, data=FAKE + (1 << 20))
 ROWS = (FAKE,) * 4
@@ -97,3 +103,27 @@ def test_clip_refusals():
     # nothing to do
     assert _tensors(N, lib, [], norm=0) == N.MAG_OK
     assert _tensors(N, lib, [_ref(count=0)], norm=0) == N.MAG_OK
+
+
+def test_a_list_made_for_a_call_lives_as_long_as_the_call():
+    """the size of a workspace for plain tensors: their description, which the library reads
+    by address, must not be freed before (freed memory is overwritten here)"""
+    code = """
+import paper_2512_08365_amd as mag
+from paper_2512_08365_amd import _native as N, _training
+
+def described(n):
+    kept = object.__new__(_training.TensorList)
+    kept.tensors = kept.out = (None,) * n
+    kept._packed = N.TENSOR_REF.pack(4096, 4096, 20000, 0, 0, 0, 2, 0) * n
+    return kept
+
+_training._list = described
+for n in (1, 2, 40, 300):
+    launches = [64] * (n // 64) + [n % 64]
+    assert mag.clip_gradients_workspace_size(n) == 8 * sum(min(3 * k, 1024) for k in launches), n
+"""
+    pytest.importorskip("torch")
+    r = subprocess.run([sys.executable, "-c", code], env={**os.environ, "PYTHONMALLOC": "debug"}, cwd=ROOT,
+                       capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout + r.stderr
