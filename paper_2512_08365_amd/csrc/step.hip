@@ -78,26 +78,56 @@ size_t backward_bytes(const mag_matrix& x, const mag_matrix& gate)
 // -------------------------------------------------------------------- clipping
 
 struct Range {
-    uintptr_t from, to;
-    uintptr_t pitch, width;   // bytes; pitch 0: all of it
+    int64_t from, to;             // bytes: of the first row's begin and the last one's end
+    int64_t rows, pitch, width;   // bytes
     bool out;
 };
 
 Range range_of(const void* p, int64_t count, int64_t cols, int64_t ld, size_t size, bool out)
 {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    if (!cols || count <= cols) return {at, at + (uintptr_t)count * size, 0, 0, out};
-    const uintptr_t rows = (uintptr_t)(count / cols), pitch = (uintptr_t)ld * size, width = (uintptr_t)cols * size;
-    return {at, at + (rows - 1) * pitch + width, ld == cols ? 0 : pitch, width, out};
+    const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(p), e = (int64_t)size;
+    if (!cols || count <= cols || ld == cols) return {at, at + count * e, 1, 0, count * e, out};
+    const int64_t rows = count / cols;
+    return {at, at + ((rows - 1) * ld + cols) * e, rows, ld * e, cols * e, out};
 }
 
-// (columns of one buffer lie between one another's rows)
+// The least x >= 0 with l <= a x mod m <= r, of 0 < l <= r < m and 0 <= a < m, or -1.
+// Where no multiple of a lies in [l, r] itself, a x - m y in [l, r] is m y mod a in
+// [-r, -l] mod a: the same with a and at most half of it, as Euclid's algorithm.
+__int128 first_within(__int128 a, __int128 m, __int128 l, __int128 r)
+{
+    if (a == 0) return -1;
+    if (2 * a > m) return first_within(m - a, m, m - r, m - l);
+    const __int128 x = (l + a - 1) / a;
+    if (a * x <= r) return x;
+    const __int128 y = first_within((a - m % a) % a, a, l % a, r % a);
+    return y < 0 ? y : (l + m * y + a - 1) / a;
+}
+
+int64_t modulo(int64_t a, int64_t m) { return (a % m + m) % m; }
+
+// whether two tensors share a byte
 bool meet(const Range& a, const Range& b)
 {
     if (a.to <= b.from || b.to <= a.from) return false;
-    if (!a.pitch || a.pitch != b.pitch) return true;
-    const uintptr_t apart = (b.from - a.from) % a.pitch;   // (a.from <= b.from)
-    return apart < a.width || apart + b.width > a.pitch;
+    if (a.rows == 1 && b.rows > 1) return meet(b, a);
+    // a's rows that reach into the stretch from b's first byte to its last one
+    const int64_t d = a.from - b.from, span = b.to - b.from;
+    int64_t first = 0, last = a.rows - 1;
+    if (a.rows > 1) {
+        if (d + a.width <= 0) first = -(d + a.width) / a.pitch + 1;
+        last = std::min(last, (span - 1 - d) / a.pitch);
+    }
+    if (first > last) return false;
+    if (b.rows == 1 || d + first * a.pitch < 0 || d + last * a.pitch >= span - b.width) return true;
+    // each of them begins in a row of b, ends in the next one, or lies between the two
+    const int64_t free = b.pitch - a.width - b.width;
+    if (free < 0) return true;
+    const int64_t at = modulo(d + first * a.pitch - b.width, b.pitch);   // (of the first, behind a row's end)
+    const int64_t l = modulo(free + 1 - at, b.pitch), r = modulo(b.pitch - 1 - at, b.pitch);
+    if (l > r || l == 0) return true;
+    const __int128 x = first_within(a.pitch % b.pitch, b.pitch, l, r);
+    return x >= 0 && x <= last - first;
 }
 
 int check_list(const mag_tensors_args* a, bool scaled)
@@ -115,6 +145,9 @@ int check_list(const mag_tensors_args* a, bool scaled)
         for (int64_t ld : {t.in_stride, t.out_stride})
             if (t.cols && t.count > t.cols && (ld < t.cols || ld > (1LL << 32)))
                 return set_error(MAG_E_SIZE, "a tensor's rows overlap or are more than 2^32 elements apart");
+        for (int64_t ld : {t.in_stride, t.out_stride})
+            if (t.cols && t.count > t.cols && t.count / t.cols - 1 >= (MOST_SPAN - t.cols) / ld)
+                return set_error(MAG_E_SIZE, "a tensor spans 2^60 elements or more");
         if (!t.in || (scaled && !t.out)) return set_error(MAG_E_NULL, "a tensor's data is NULL");
         if (!aligned(t.in, element(t.dtype)) || (scaled && !aligned(t.out, element(t.dtype))))
             return set_error(MAG_E_ALIGN, "a tensor is not aligned to its elements");

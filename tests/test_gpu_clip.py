@@ -223,3 +223,19 @@ def test_workspace_of_plain_tensors():
         ws = torch.empty(mag.clip_gradients_workspace_size(tensors), dtype=torch.uint8, device="cuda")
         want = math.sqrt(sum(t.numel() for t in tensors))
         assert abs(float(mag.clip_gradients(tensors, 1.0, workspace=ws)) - want) <= 2.0 ** -23 * want
+
+
+def test_slices_of_one_buffer():
+    """slices that share no element: a single row's, every second row's, other columns'"""
+    torch = _torch()
+    for ty in TYPES:
+        buffer = _normal(_gen(9), (41, 777), 1.0, _dt(ty))
+        keep = buffer.clone()
+        tensors = [buffer[0:1, :256], buffer[1:, :256], buffer[::2, 256:600], buffer[1::2, 256:700], buffer[4:5, 600:650],
+                   buffer[6:20:2, 601:700]]
+        check_clip(tensors, 1.0)
+        left = torch.ones_like(buffer, dtype=torch.bool)
+        for t in (left[:, :256], left[::2, 256:600], left[1::2, 256:700], left[4:5, 600:650], left[6:20:2, 601:700]):
+            t[:] = False
+        assert torch.equal(buffer[left], keep[left])
+        check_clip([buffer[0:1, :256], buffer[:, 256:]], 0.5, out=[keep[7:8, 3:259], keep[8:, :].new_empty(41, 521)])

@@ -3,6 +3,7 @@ device work (no GPU needed)."""
 import ctypes
 import math
 import os
+import random
 import subprocess
 import sys
 
@@ -127,3 +128,69 @@ for n in (1, 2, 40, 300):
     r = subprocess.run([sys.executable, "-c", code], env={**os.environ, "PYTHONMALLOC": "debug"}, cwd=ROOT,
                        capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+def _bytes_of(ref, place, ld):
+    _, _, count, cols, *_ = ref
+    size = 4 if ref[6] == 0 else 2
+    rows = [(place, count)] if cols == 0 else [(place + k * ref[ld] * size, cols) for k in range(count // cols)]
+    return {b for at, n in rows for b in range(at, at + n * size)}
+
+
+def _overlap(refs):
+    """whether an output's bytes are another's of the list, byte by byte"""
+    out = [_bytes_of(r, r[1], 5) for r in refs]
+    own = [r[0] == r[1] and _bytes_of(r, r[0], 4) == o and (r[3] == 0 or r[2] == r[3] or r[4] == r[5])
+           for r, o in zip(refs, out)]
+    read = [set() if same else _bytes_of(r, r[0], 4) for r, same in zip(refs, own)]
+    return any(o & read[j] or (i != j and o & out[j]) for i, o in enumerate(out) for j in range(len(refs)))
+
+
+def test_tensors_overlap_where_they_share_a_byte_and_nowhere_else():
+    """slices of one buffer: columns, rows, single rows, every second row, rows of another
+    width, against their bytes one by one"""
+    N, lib = _n()
+
+    def refused(refs):
+        rc = _tensors(N, lib, refs, bytes_=0)
+        assert rc in (N.MAG_E_SIZE, N.MAG_E_WORKSPACE), rc
+        return rc == N.MAG_E_SIZE
+
+    def cut(row, rows, col, cols, pitch, step=1):
+        return _ref(4 * (row * pitch + col), rows * cols, cols, step * pitch, step * pitch)
+
+    # a row's slice beside other columns, every second row, rows of two pitches
+    assert not refused([cut(0, 1, 0, 3, 10), cut(0, 5, 3, 7, 10)])
+    assert not refused([_ref(12, 4), cut(0, 5, 7, 3, 10), cut(1, 4, 3, 4, 10)])
+    assert not refused([cut(0, 5, 0, 10, 10, 2), cut(1, 5, 0, 10, 10, 2)])
+    assert not refused([cut(0, 9, 0, 3, 10), cut(0, 5, 3, 7, 10, 2), cut(1, 4, 3, 7, 10, 2)])
+    assert refused([cut(0, 9, 0, 3, 10), cut(1, 4, 2, 7, 10, 2)])
+    assert refused([cut(0, 9, 0, 3, 10), cut(8, 1, 2, 1, 10)])
+    rng, seen = random.Random(11), [0] * 4
+    for _ in range(30000):
+        refs = []
+        for _ in range(rng.choice((2, 2, 2, 3))):
+            cols, dtype = rng.choice((0, 1, 1, 2, 3, 5)), rng.choice((0, 2))
+            count = rng.randint(1, 6) * max(cols, 1)
+            ld = [cols + rng.choice((0, 1, 2, 7, 12, 31)) for _ in range(2)]
+            if rng.random() < 0.7:
+                ld[1] = ld[0]
+            at = 4 * rng.randint(0, 60)
+            to = at if rng.random() < 0.7 else 4 * rng.randint(0, 60)
+            refs.append(_ref(at, count, cols, *ld, dtype, to=to))
+        want = _overlap(refs)
+        seen[want] += 1
+        assert refused(refs) == want, refs
+    assert min(seen[:2]) > 3000
+    # a million rows and some hundred of another pitch among them, which drift past them
+    a = (FAKE, FAKE, 3 * 1000003, 3, 7001, 7001, 0, 0)
+    for at in range(400):
+        start = 4 * (at + 5003 * 7001)
+        b = (FAKE + start, FAKE + start, 2 * 580, 2, 7013, 7013, 0, 0)
+        meets = any((5003 * 7001 + at + k * 7013 + 1) % 7001 <= 3 and 5003 * 7001 + at + k * 7013 < 1000002 * 7001 + 3
+                    for k in range(580))
+        assert refused([a, b]) == meets, at
+        seen[2 + meets] += 1
+    assert min(seen[2:]) > 20
+    # rows that no memory holds
+    assert _tensors(N, lib, [(FAKE, FAKE, 1 << 36, 1, 1 << 32, 1 << 32, 0, 0)], bytes_=0) == N.MAG_E_SIZE
