@@ -944,6 +944,9 @@ typedef struct mag_linear_fp8_args {
  * Rows that are packed first (those not of whole 16 bytes and less than 2^23 bytes
  * apart) are packed at most 2^23 - 128 of the reduction at a time.  Scales of
  * neighbouring rows are at most 2^22 floats apart.
+ * The two scales of a block are multiplied with each other first, in fp32: where that
+ * leaves its range, below 2^-126 digits are lost, above 2^128 results are infinite or,
+ * of a sum of zero, NaN.
  * A block's sum is the matrix instruction's: of eight neighbours' products those
  * below 2^-13 of their largest lose what is below that; blocks are added in fp32.
  * Results are therefore of two bytes.

@@ -21,8 +21,10 @@ __device__ __forceinline__ f32x4 mfma8(i32x8 a, i32x8 b)
 // out[r][s]: SIDE x SIDE of them a tile, WR x WS waves.  A step is a block of 128 k:
 // what the instruction sums of a block is multiplied by the operands' scales and
 // added to the sums in registers, so there is one multiplication and addition a
-// sum and step beside the products (of scales for each s two): half of the matrix
-// cores' time, and beside it as long as the products do not wait for their results.
+// sum and step beside the products: half of the matrix cores' time, and beside it as
+// long as the products do not wait for their results.  Scales for each s cost a
+// multiplication more, of the scales with each other: sums times one of them and then
+// the other would leave fp32's range where a tiny one meets a huge one.
 template <int SIDE_, int WR_, int WS_>
 struct Shape8 {
     static constexpr int SIDE = SIDE_, WR = WR_, WS = WS_;
@@ -230,9 +232,8 @@ __device__ __forceinline__ void walk8(Mm8 p, const Arrays& lds)
                 const int m = k - LATE, mi = m / SF, mj = m % SF;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float v = t[m % (LATE + 1)][e];
-                    if constexpr (BY_ROW) v *= sbv[mj][e];
-                    acc[mi][mj][e] = fmaf(v, s[mi & 1], acc[mi][mj][e]);
+                    const float by = BY_ROW ? s[mi & 1] * sbv[BY_ROW ? mj : 0][e] : s[mi & 1];
+                    acc[mi][mj][e] = fmaf(t[m % (LATE + 1)][e], by, acc[mi][mj][e]);
                     if constexpr (PINNED) asm volatile("" : "+v"(acc[mi][mj][e]));
                 }
             }

@@ -417,3 +417,47 @@ def test_quantize_ends_of_rows(cols, ty):
                 _check_cut(x.t().contiguous(), qt, st, 1, "e4m3")
                 rows = mag.quantize_fp8(x)
                 assert torch.equal(rows[0].float(), q.float()) and torch.equal(rows[1], s)
+
+
+@pytest.mark.parametrize("by_row", [False, True])
+@pytest.mark.parametrize("size", [(5, 300, 70), (24, 300, 70), (100, 300, 200), (700, 300, 1300), (40, 20000, 70)])
+def test_linear_scales_at_the_ends_of_their_range(size, by_row):
+    """The two scales of a block are multiplied with each other first, whatever kernel a
+    size takes: a tiny one and a huge one lose nothing, two tiny ones what their product's
+    subnormal number lacks, two huge ones are infinite."""
+    import paper_2512_08365_amd as mag
+    torch = _torch()
+    rows, inner, outer = size
+    g, blocks = _gen(11), _blocks(inner)
+    tall = outer if by_row else _blocks(outer)
+
+    def numbers(n, most, unit):
+        return (torch.randint(-most, most + 1, (n, inner), generator=g, device="cuda") * unit).to(_eight("e4m3"))
+
+    def scales(n, unit):
+        return (torch.randint(2, 4, (n, blocks), generator=g, device="cuda") / 2).float() * unit
+
+    # sums of -9 to 9 in units of 2^-18, times 1, 1.5 or 2.25, are exact in fp32
+    for a, b in ((2.0 ** 120, 2.0 ** -126), (2.0 ** -126, 2.0 ** 120), (2.0 ** 126, 2.0 ** -110)):
+        x, w, sx, sw = numbers(rows, 3, 2.0 ** -9), numbers(outer, 3, 2.0 ** -9), scales(rows, a), scales(tall, b)
+        want = torch.mm(x.double() * _each(sx, rows, inner),
+                        (w.double() * _each(sw, outer, inner, 1 if by_row else BLOCK)).t().contiguous())
+        assert torch.equal(mag.linear_fp8(x, sx, w, sw), want.bfloat16())
+    # products of scales between 2^-141 and 2^-137, whole numbers times 32 (which lose nothing)
+    x, w = numbers(rows, 14, 32.0), numbers(outer, 14, 32.0)
+    sx, sw = ((1 + torch.rand((n, blocks), generator=g, device="cuda")) * 2.0 ** -by for n, by in ((rows, 70), (tall, 71)))
+    want, mag64 = (torch.zeros((rows, outer), dtype=torch.float64, device="cuda") for _ in range(2))
+    for k in range(blocks):
+        each = sw[:, k] if by_row else sw[:, k].repeat_interleave(BLOCK)[:outer]
+        by = (sx[:, None, k].cpu() * each[None].cpu()).cuda().double()   # (rounded once, in fp32)
+        assert 2.0 ** -142 < float(by.min()) and float(by.max()) < 2.0 ** -138
+        a, b = (v[:, k * BLOCK:(k + 1) * BLOCK].double() for v in (x, w))
+        want += by * torch.mm(a, b.t().contiguous())
+        mag64 += by * torch.mm(a.abs(), b.abs().t().contiguous())
+    tol = (blocks + 4) * V * mag64
+    _close(mag.linear_fp8(x, sx, w, sw), want, tol + _u("bf16") * (want.abs() + tol) + _tiny("bf16"), "subnormal products")
+    # beyond fp32: infinite, and of a sum of zero NaN
+    x, w = numbers(rows, 3, 1.0), numbers(outer, 3, 1.0)
+    x[0] = 0
+    got = mag.linear_fp8(x, scales(rows, 2.0 ** 100), w, scales(tall, 2.0 ** 100))
+    assert bool(got[0].isnan().all()) and not bool(got.isfinite().any())
