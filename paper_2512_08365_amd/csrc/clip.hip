@@ -138,7 +138,15 @@ __global__ __launch_bounds__(THREADS) void k_clip_norm(Spans s, double* part)
 // PAST: stores go past the caches
 template <bool PAST>
 struct Scaling {
-    float by;
+    // The factor is the two's product: one below 2^-126 would lack digits as a float, and
+    // makes normal numbers of large ones all the same (below 2^-277 it makes zeros).
+    float by, then;
+    __device__ __forceinline__ explicit Scaling(double factor)
+    {
+        const double up = factor >= 0x1p-126 ? 1.0 : factor >= 0x1p-226 ? 0x1p100 : 0x1p149;
+        by = (float)(factor * up);
+        then = (float)(1.0 / up);
+    }
     // nothing to do: in place, and not clipped (eight bfloat16 tensors of 4,096 x 16,384
     // 595 us, so 214 us)
     __device__ __forceinline__ bool done(const Span& s) const
@@ -148,7 +156,7 @@ struct Scaling {
     template <class T>
     __device__ __forceinline__ void one(const Span& s, T x, int64_t i)
     {
-        static_cast<T*>(s.out)[i] = (T)((float)x * by);
+        static_cast<T*>(s.out)[i] = (T)((float)x * by * then);
     }
     template <class Any>
     __device__ __forceinline__ void whole(const Span& s, const Any& v, int64_t i)
@@ -156,7 +164,7 @@ struct Scaling {
         using T = typename std::remove_cv<typename std::remove_reference<decltype(v[0])>::type>::type;
         Any o;
 #pragma unroll
-        for (int k = 0; k < (int)(sizeof(Any) / sizeof(T)); ++k) o[k] = (T)((float)v[k] * by);
+        for (int k = 0; k < (int)(sizeof(Any) / sizeof(T)); ++k) o[k] = (T)((float)v[k] * by * then);
         Any* to = (Any*)(static_cast<T*>(s.out) + i);
         if constexpr (PAST)
             __builtin_nontemporal_store(o, to);
@@ -186,7 +194,7 @@ __global__ __launch_bounds__(THREADS) void k_clip_scale(Spans s, const double* p
     if (s.n == 0) return;
     const double by = most / (v + eps);
     // (a norm that is NaN makes all NaN)
-    Scaling<PAST> f{(float)(by > 1.0 ? 1.0 : by)};
+    Scaling<PAST> f(by > 1.0 ? 1.0 : by);
     over_chunks(s, true, f);
 }
 

@@ -239,3 +239,23 @@ def test_slices_of_one_buffer():
             t[:] = False
         assert torch.equal(buffer[left], keep[left])
         check_clip([buffer[0:1, :256], buffer[:, 256:]], 0.5, out=[keep[7:8, 3:259], keep[8:, :].new_empty(41, 521)])
+
+
+def test_factors_below_fp32():
+    """a factor that is a subnormal number of fp32, or none of it any more, still counts for
+    all its digits where its products are normal numbers"""
+    import paper_2512_08365_amd as mag
+    torch = _torch()
+    for ty in ("f32", "bf16"):
+        for kind in (2, math.inf):
+            for most in (1e-5, 3e-7, 1e-2, 5e-30, 1e-36):
+                g = _gen(12)
+                x = torch.cat([_normal(g, (9001,), 5e37, torch.float32).clamp(-3e38, 3e38),
+                               _normal(g, (300,), 1e36, torch.float32)]).to(_dt(ty))
+                keep = x.double()
+                norm = _norm64([x], kind)
+                for out in (None, [torch.empty_like(x)]):
+                    y = x.clone()
+                    mag.clip_gradients([y], most, kind=kind, out=out)
+                    want = keep * (most / (norm + 1e-6))
+                    _close((out or [y])[0], want, (2 * V + _u(ty) * (1 + V)) * want.abs() + 2 * _tiny(ty), f"{ty} {kind} {most}")
