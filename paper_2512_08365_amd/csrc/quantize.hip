@@ -273,24 +273,46 @@ __global__ __launch_bounds__(256, 3) void k_quantize_tile(QuantizeParams p, uint
         quantize_tile<T, MAG_E5M2, SQUARE, WHOLE>(p, across, most_lds, turned);
 }
 
-template <class T, bool WHOLE>
-hipError_t launch(const QuantizeParams& p, int format, bool square, hipStream_t stream)
+// n rows from r0 on (where scales go with 128 rows, at a multiple of them)
+template <class T>
+QuantizeParams rows_of(const QuantizeParams& all, bool square, int64_t r0, int64_t n)
 {
-    const int64_t nb = (p.cols + FP8_BLOCK - 1) / FP8_BLOCK, mb = (p.rows + FP8_BLOCK - 1) / FP8_BLOCK;
-    if (!square && !p.qt && (p.cs == 1 || p.cols <= 1)) {
-        const int64_t across = (nb + BLOCKS - 1) / BLOCKS, down = (p.rows + 15) / 16;
-        if (across > 0xffffff / down) return hipErrorInvalidConfiguration;
-        hipLaunchKernelGGL((k_quantize_rows<T, WHOLE>), dim3((unsigned)(across * down)), dim3(256), 0, stream,
-                           p, (uint32_t)across, format);
-        return hipGetLastError();
+    QuantizeParams p = all;
+    p.x = static_cast<const T*>(p.x) + r0 * p.rs;
+    p.rows = n;
+    if (p.q) {
+        p.q += r0 * p.q_ld;
+        p.scale.p += (square ? r0 / FP8_BLOCK : r0) * p.scale.rs;
     }
-    if (nb > 0xffffff / mb) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)(nb * mb));
-    if (square)
-        hipLaunchKernelGGL((k_quantize_tile<T, true, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb, format);
-    else
-        hipLaunchKernelGGL((k_quantize_tile<T, false, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb, format);
-    return hipGetLastError();
+    if (p.qt) {
+        p.qt += r0;
+        p.scale_t.p += r0 / FP8_BLOCK * p.scale_t.cs;
+    }
+    return p;
+}
+
+// (a launch has less than 2^32 threads: many millions of rows take several)
+template <class T, bool WHOLE>
+hipError_t launch(const QuantizeParams& all, int format, bool square, hipStream_t stream)
+{
+    constexpr int64_t MOST = 0xffffff;   // workgroups
+    const int64_t nb = (all.cols + FP8_BLOCK - 1) / FP8_BLOCK;
+    const bool by_rows = !square && !all.qt && (all.cs == 1 || all.cols <= 1);
+    const int64_t across = by_rows ? (nb + BLOCKS - 1) / BLOCKS : nb, each = by_rows ? 16 : FP8_BLOCK;
+    const int64_t most = MOST / across * each;   // (across: 2^23 at most)
+    for (int64_t r0 = 0; r0 < all.rows; r0 += most) {
+        const QuantizeParams p = rows_of<T>(all, square, r0, std::min(most, all.rows - r0));
+        const dim3 grid((unsigned)(across * ((p.rows + each - 1) / each)));
+        if (by_rows)
+            hipLaunchKernelGGL((k_quantize_rows<T, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)across, format);
+        else if (square)
+            hipLaunchKernelGGL((k_quantize_tile<T, true, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb, format);
+        else
+            hipLaunchKernelGGL((k_quantize_tile<T, false, WHOLE>), grid, dim3(256), 0, stream, p, (uint32_t)nb, format);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // (rows that end amid eight neighbours: 32,768 x 1,021 and its transpose 61 us by

@@ -39,3 +39,24 @@ def test_reductions_longer_than_a_tile_reaches_over(size, by_row):
             want += torch.mm(a, b.t().contiguous())
         assert float(want.abs().max()) < 2.0 ** 20
         assert torch.equal(y, want.bfloat16())
+
+
+def test_quantization_of_more_rows_than_a_launch_takes():
+    """2^28 rows of one number: each is its block's largest"""
+    torch = _torch()
+    import paper_2512_08365_amd as mag
+    rows = (1 << 28) + 1000
+    print(f"[case] quantize_fp8 {rows} x 1", flush=True)
+    x = torch.randn((rows, 1), generator=_gen(3), device="cuda").bfloat16()
+    x[rows - 5] = x[7] = 0
+    q = torch.full((rows, 1), 0x7f, dtype=torch.uint8, device="cuda")
+    scale = torch.full((rows, 1), float("nan"), device="cuda")
+    mag.quantize_fp8(x, out=(q.view(torch.float8_e4m3fn), scale))
+    step = 1 << 26
+    for at in range(0, rows, step):
+        v, s, b = (t[at:at + step, 0] for t in (x, scale, q))
+        most = v.double().abs()
+        exact = torch.clamp(most / 448, min=2.0 ** -126)
+        assert bool(((s.double() - exact).abs() <= 2.0 ** -24 * exact).all())
+        want = torch.where(v == 0, 0, torch.where(v < 0, 0xfe, 0x7e))   # (-448 and 448)
+        assert bool((b == want).all())

@@ -1,5 +1,6 @@
-"""The launches of the norms around a block: the library's host code in a child process
-over the stand-in runtime (hip_double.c), which writes them down (no GPU needed)."""
+"""The launches of the norms around a block and of quantization: the library's host code in
+a child process over the stand-in runtime (hip_double.c), which writes them down (no GPU
+needed)."""
 import ctypes
 import importlib.util
 import os
@@ -45,6 +46,34 @@ def _threads_of_a_row():
                 assert len(back) == 1 and back[0][2] * 8 >= width, (width, groups, each, back)
 
 
+def _workgroups_of_quantization():
+    """all rows have their workgroups, and no launch 2^32 threads"""
+    N, lib, log, launches = _native()
+    for rows, cols in ((1, 1), (1000, 700), ((1 << 28) - 16, 128), (1 << 28, 1), ((1 << 28) + 1, 513), (1 << 30, 100),
+                       (1 << 30, 5000), (1 << 23, 100_000), (3, 1 << 30)):
+        m, n = -(-rows // 128), -(-cols // 128)
+        for by_columns in (False, True):
+            x = (FAKE, rows, cols, 1, rows) if by_columns else (FAKE, rows, cols, cols, 1)
+            q, qt = (FAKE, rows, cols, cols, 1), (FAKE, cols, rows, rows, 1)
+            for block_rows in (1, 128):
+                s = (FAKE, rows if block_rows == 1 else m, n, 1, 1 << 30)
+                st = (FAKE, cols if block_rows == 1 else n, m, 1, 1 << 30)
+                for outputs in ((q, s, NONE, NONE), (q, s, qt, st), (NONE, NONE, qt, st)):
+                    log.double_clear()
+                    rc = lib.mag_quantize_fp8(N.QUANTIZE_ARGS.pack(2, 3, block_rows, 0, *x, *outputs[0], *outputs[1],
+                                                                   *outputs[2], *outputs[3]), None)
+                    assert rc == 0, (rows, cols, by_columns, lib.mag_last_error())
+                    made = launches()
+                    for name, grid, block in made:
+                        assert 0 < grid * block < 1 << 32, (rows, cols, made)
+                    whole = sum(grid for _, grid, _ in made)
+                    if "k_quantize_rows" in made[0][0]:
+                        r, c = (cols, rows) if by_columns and cols > 1 else (rows, cols)
+                        assert whole == -(-r // 16) * -(-(-(-c // 128)) // 4), (rows, cols, made)
+                    else:
+                        assert whole == m * n, (rows, cols, made)
+
+
 def _child(tmp_path, name):
     so = str(tmp_path / "hip_double.so")
     subprocess.check_call(["gcc", "-O1", "-shared", "-fPIC", "-o", so, os.path.join(HERE, "hip_double.c")])
@@ -57,6 +86,10 @@ def _child(tmp_path, name):
 
 def test_workgroups_of_the_backward_pass_hold_their_rows(tmp_path):
     _child(tmp_path, "_threads_of_a_row")
+
+
+def test_workgroups_of_quantization_fit_their_launches(tmp_path):
+    _child(tmp_path, "_workgroups_of_quantization")
 
 
 if __name__ == "__main__":
