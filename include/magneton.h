@@ -976,8 +976,8 @@ typedef struct mag_residual_norm_args {
     const void *post_weight, *post_bias; /* likewise, of the branch's norm         */
     float *mean, *rstd;           /* [rows], written where not NULL (an rms        */
     float *post_mean, *post_rstd; /* norm's mean is 0)                             */
-    double scale;         /* of the branch                                         */
-    double eps;           /* >= 0                                                  */
+    double scale;         /* of the branch; finite in fp32                         */
+    double eps;           /* >= 0, finite in fp32                                  */
 } mag_residual_norm_args;
 
 /*

@@ -3,6 +3,7 @@
 
 #include "step.hpp"
 
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -42,6 +43,12 @@ int check_same(const mag_matrix& m, const mag_matrix& x, bool out, int dtype)
     if (!same_shape(m, x.rows, x.cols)) return set_error(MAG_E_SIZE, "matrices must be [rows, width]");
     TRY(check_shape(m, out));
     return check_data(m, dtype);
+}
+
+int check_scale(double scale)
+{
+    if (!(fabs(scale) <= FLT_MAX)) return set_error(MAG_E_SIZE, "scale must be finite in fp32");
+    return MAG_OK;
 }
 
 // (two outputs that begin together; where they overlap otherwise is not looked at)
@@ -271,8 +278,8 @@ int mag_residual_norm(const mag_residual_norm_args* a, hipStream_t stream)
     TRY(check_same(a->out, a->residual, true, a->dtype));
     TRY(check_same(a->normed, a->residual, true, a->dtype));
     TRY(check_apart(a->out, a->normed));
-    if (!(a->eps >= 0.0) || isinf(a->eps)) return set_error(MAG_E_SIZE, "eps must be finite and >= 0");
-    if (!isfinite(a->scale)) return set_error(MAG_E_SIZE, "scale must be finite");
+    if (!(a->eps >= 0.0 && a->eps <= FLT_MAX)) return set_error(MAG_E_SIZE, "eps must be >= 0 and finite in fp32");
+    TRY(check_scale(a->scale));
     if (!a->post && (a->post_weight || a->post_bias))
         return set_error(MAG_E_SIZE, "post_weight and post_bias belong to a norm of the branch");
     for (const void* v : {a->weight, a->bias, a->post_weight, a->post_bias}) TRY(check_vector(v, a->weight_dtype));
@@ -328,7 +335,7 @@ int mag_residual_norm_backward(const mag_residual_norm_backward_args* a, void* w
     if (a->d_residual.data) TRY(check_same(a->d_residual, x, true, a->dtype));
     if (a->d_branch.data) TRY(check_same(a->d_branch, x, true, a->dtype));
     TRY(check_apart(a->d_residual, a->d_branch));
-    if (!isfinite(a->scale)) return set_error(MAG_E_SIZE, "scale must be finite");
+    TRY(check_scale(a->scale));
     const bool layer = a->kind == MAG_NORM_LAYER;
     if (x.rows > 0 && (!a->rstd || (layer && !a->mean) || (a->post && (!a->post_rstd || (layer && !a->post_mean)))))
         return set_error(MAG_E_NULL, "the norms' statistics are needed");

@@ -194,3 +194,15 @@ def test_tensors_overlap_where_they_share_a_byte_and_nowhere_else():
     assert min(seen[2:]) > 20
     # rows that no memory holds
     assert _tensors(N, lib, [(FAKE, FAKE, 1 << 36, 1, 1 << 32, 1 << 32, 0, 0)], bytes_=0) == N.MAG_E_SIZE
+
+
+def test_residual_norm_takes_no_number_that_is_infinite_in_fp32():
+    """the kernels take scale and eps as floats"""
+    N, lib = _n()
+    none = _mat(0, 64)
+    for bad in (1e39, -1e39, 3.5e38):
+        assert _forward(N, lib, scale=bad) == N.MAG_E_SIZE
+        assert _backward(N, lib, scale=bad) == N.MAG_E_SIZE
+    assert _forward(N, lib, eps=1e39) == N.MAG_E_SIZE
+    for good in (3.4e38, -3.4e38, 0.0):
+        assert _forward(N, lib, h=none, y=none, out=none, normed=none, scale=good, eps=abs(good)) == N.MAG_OK
