@@ -926,11 +926,11 @@ RowParts residual_norm_parts(const ResidualNorm& p)
     const bool by_element = wide(p);
     const int64_t rows = by_element ? 1 : rows_at_once(p.N);
     const int64_t most = by_element || p.N <= 4096 ? 512 : p.N <= MOST_SUMMED ? 256 : 128;
-    if (p.M == 0) return {1, 0, by_element};
-    if (2 * p.groups > most) return {(int)std::min(most, p.groups), 0, by_element};
+    if (p.M == 0) return {1, 0};
+    if (2 * p.groups > most) return {(int)std::min(most, p.groups), 0};
     const int64_t rounds = (p.length + rows - 1) / rows;
     const int64_t chunks = std::max<int64_t>(1, std::min(most / p.groups, rounds));
-    return {(int)(chunks * p.groups), (int)chunks, by_element};
+    return {(int)(chunks * p.groups), (int)chunks};
 }
 
 hipError_t launch_residual_norm(const ResidualNorm& p, int dtype, hipStream_t stream)

@@ -36,7 +36,6 @@ struct ResidualNorm {
 // how the backward pass deals out its rows
 struct RowParts {
     int parts, chunks;
-    bool wide;             // rows that no registers hold
 };
 RowParts residual_norm_parts(const ResidualNorm& p);
 hipError_t launch_residual_norm(const ResidualNorm& p, int dtype, hipStream_t stream);

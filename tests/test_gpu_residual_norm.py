@@ -497,3 +497,15 @@ def test_gradients_of_no_rows_are_zero(width, ty):
                                              post_bias=w, out=out, workspace=ws)
             for grad in got[2:]:
                 assert grad is None or bool((grad == 0).all()), (groups, wt)
+
+
+@pytest.mark.parametrize("ty", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [8200, 8207, 10240, 10241, 12289, 16384])
+def test_wide_rows_in_place(width, ty):
+    """rows that several workgroups share while they are written over, ends in a workgroup of
+    their own among them"""
+    for lay in ("plain", "gap"):
+        for kind, groups in (("layer", 2), ("rms", "row")):
+            check_forward(34, width, ty, kind=kind, groups=groups, lh=lay, ly=lay, in_place=True)
+            check_backward(34, width, ty, kind=kind, groups=groups, lays=(lay,) * 4, in_place=True)
+    check_backward(700, width, ty, groups="channel", post=False, in_place=True)
