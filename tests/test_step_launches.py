@@ -4,6 +4,7 @@ needed)."""
 import ctypes
 import importlib.util
 import os
+import re
 import subprocess
 import sys
 
@@ -90,6 +91,15 @@ def test_workgroups_of_the_backward_pass_hold_their_rows(tmp_path):
 
 def test_workgroups_of_quantization_fit_their_launches(tmp_path):
     _child(tmp_path, "_workgroups_of_quantization")
+
+
+def test_the_stand_in_runtime_has_a_place_for_every_kernel():
+    """(it leaves those beyond its table without a name)"""
+    from paper_2512_08365_amd import _native
+    with open(os.path.join(HERE, "hip_double.c")) as f:
+        places = int(re.search(r"g_fns\[(\d+)\];", f.read()).group(1))
+    symbols = subprocess.check_output(["nm", _native.LIB_PATH], text=True)
+    assert 0 < symbols.count("__device_stub__") <= places
 
 
 if __name__ == "__main__":
