@@ -73,7 +73,11 @@ bool in_place(const mag_matrix& m)
 int64_t packed_ld(int64_t n) { return (int64_t)(n > 128 ? round_up((size_t)n, 128) : round_up((size_t)n, 16)); }
 
 // What a workgroup's step, its tile beside the steps, and the call cost, in us, with
-// the CU to itself and with others on it.
+// the CU to itself and with others on it.  Of 44 sizes (33 to 16,384 rows, reductions of
+// 128 to 16,384, 64 to 16,384 outputs), every tile and split timed: what these choose is
+// within 3% of the fastest at 37 and 18% slower at the worst (7,781 x 208 by 1,842: tiles
+// of 256, 19.6 us, where tiles of 64 take 16.7); beyond the 8 us of the host's call they
+// foretell 7% more to 25% less than is measured, 11% less in the middle.
 struct TileCost {
     int per_cu;
     double step, tile;   // (of as many as fit)

@@ -316,7 +316,7 @@ hipError_t launch(const QuantizeParams& all, int format, bool square, hipStream_
 }
 
 // (rows that end amid eight neighbours: 32,768 x 1,021 and its transpose 61 us by
-// element, so 46 us; its bounds cost whole blocks 5%)
+// element, so 50 us; its bounds cost whole blocks 5%)
 template <class T>
 hipError_t launch(const QuantizeParams& p, int format, bool square, hipStream_t stream)
 {

@@ -6,7 +6,7 @@
 // reads four matrices and writes two.  Every row is read once into the registers of
 // 64 to 1,024 threads, 8 elements each (of rows above 8,192 16), the next one while the
 // present one's sums are taken.  A gate that many rows share is read once for a
-// workgroup's rows of it.  Of a copy's 6.2 TB/s: 32,768 x 4,096 forward 5.3, backward 4.7;
+// workgroup's rows of it.  Of a copy's 6.2 TB/s: 32,768 x 4,096 forward 5.2, backward 4.7;
 // backward above 8,192 in two passes, 2.2 to 3.3.
 //
 // Sums over a row and over rows, statistics and gradients are fp32; the stream's sum

@@ -55,7 +55,7 @@ __device__ __forceinline__ void get(Held<T, E>& r, const T* row, int lane, int n
 // The same, of rows of at least 8, in two steps without a wait between them: fetch() has the thread at a row's
 // end load the eight elements that end there, settle() moves them down to their
 // places (zeros behind).  By element, each of the seven is a load of its own that is
-// waited for: 48,000 x 1,021 forward 188 us, so 104 us (two-byte numbers).
+// waited for: 48,000 x 1,021 forward 188 us, so 95 us (two-byte numbers).
 template <int G, int V, bool TAIL, class T, int E>
 __device__ __forceinline__ void fetch(Held<T, E>& r, const T* row, int lane, int n)
 {
